@@ -248,6 +248,134 @@ cs_status cs_rollout_stats(cs_rollout* r, cs_rollout_stats_t* out);
 cs_status cs_rollout_export(cs_rollout* r, void* buf, size_t* bytes);
 cs_status cs_rollout_import(cs_rollout* r, const void* buf, size_t bytes);
 
+/* -------------------------------------------------------------- operators
+ *
+ * Operators of the transformer by themselves, on tensors the caller holds.
+ * They take and keep no handle.  Rules common to all of them:
+ *  - All tensors are device memory of the current device; dtype (cs_dtype)
+ *    is the type of the floating tensors.  Strides are counted in elements;
+ *    the channels of a head are contiguous.  Rows are moved 16 bytes at a
+ *    time: tensor pointers are 16-byte aligned and strides multiples of 16
+ *    bytes (CS_E_INVAL otherwise).  Strides are not negative.
+ *  - The work is enqueued on `stream` (hipStream_t or NULL); nothing is
+ *    allocated, copied or waited for, so calls can be captured into a HIP
+ *    graph.  Descriptors are read before the call returns.  Tensors must
+ *    stay valid until the enqueued work is done.
+ *  - Calls with nothing to do (no tokens, no queries) return CS_OK.
+ *  - A workspace (16-byte aligned, at least the size the _workspace function
+ *    gives) carries nothing from one call to the next, but calls that may
+ *    overlap (two streams, two graphs) need one each.
+ *  - Results do not depend on the batch: a token, or a query with its
+ *    context, gives bitwise the same output alone and among others. */
+
+/* Pairs a rotation turns: adjacent channels (2p, 2p + 1), or the first and
+ * the second half of the rotated channels (p, p + rot_dim / 2). */
+typedef enum { CS_ROPE_PAIRS = 0, CS_ROPE_HALVES = 1 } cs_rope_style;
+
+/* Tokens of cs_qk_norm_rope.  q is [tokens][heads_q][head_dim] with strides
+ * q_row and q_head, its output has qo_row and qo_head; k likewise (k_*, ko_*).
+ * head_dim: a multiple of 16 up to 256.  rot_dim: channels that turn, the first
+ * ones of a head, a multiple of 16 up to head_dim, 0 for none.  rope_rows: rows
+ * of the table.  q_gain_head, k_gain_head: stride of the gains from head to
+ * head, 0 if all heads share one. */
+typedef struct {
+  int32_t dtype;                 /* cs_dtype */
+  int32_t tokens, heads_q, heads_k, head_dim;
+  int32_t rot_dim, rope_rows, rope_style;
+  float eps;                     /* >= 0 */
+  int64_t q_row, q_head, k_row, k_head;
+  int64_t qo_row, qo_head, ko_row, ko_head;
+  int64_t q_gain_head, k_gain_head;
+} cs_qk_norm_desc;
+
+/* RMS norm of every head of q and k over its own channels, then the rotation:
+ *   y_c = x_c / sqrt(mean_c(x_c^2) + eps) * gain_c,
+ *   (a, b) -> (a cos - b sin, a sin + b cos) for the pairs of the first rot_dim
+ * channels, in fp32 and rounded once.  rope: device float
+ * [rope_rows][rot_dim / 2][2] (cos, sin); token t takes row pos[t] (device
+ * int32), or row t % rope_rows if pos is NULL.  A token whose position is
+ * negative is skipped: its outputs are left as they were (padding).  One whose
+ * position is not below rope_rows gets NaN.  Gains are fp32.  heads_q or heads_k
+ * may be 0: those pointers are then not read.  An output may be its input (same
+ * pointer and strides); other overlaps are not allowed. */
+cs_status cs_qk_norm_rope(const cs_qk_norm_desc* desc, const void* q, const void* k, void* q_out,
+                          void* k_out, const float* q_gain, const float* k_gain,
+                          const float* rope, const int32_t* pos, void* stream);
+
+/* Attention of queries to contexts: n_q query sets of lq queries each, n_kv
+ * contexts of up to lk keys and values.  heads_q is a multiple of heads_kv: query
+ * head h reads key head h / (heads_q / heads_kv).  head_dim 32, 64 or 128.
+ * Strides: set or context (_b), row (_r) and head (_h); mask_b is the stride of
+ * the mask from context to context (bytes, any alignment).  scale > 0 multiplies
+ * the products q.k. */
+typedef struct {
+  int32_t dtype;                 /* cs_dtype of q, o (and k, v) */
+  int32_t n_q, n_kv, lq, lk;
+  int32_t heads_q, heads_kv, head_dim;
+  float scale;
+  int64_t q_b, q_r, q_h, k_b, k_r, k_h, v_b, v_r, v_h, o_b, o_r, o_h;
+  int64_t mask_b;
+} cs_attn_desc;
+
+/* o = softmax(scale q k^T) v over the keys that are left of each set's context.
+ * kv_of: device int32 [n_q], the context of each query set; NULL: set i reads
+ * context i (n_kv >= n_q then).  kv_len: device int32 [n_kv], keys of each
+ * context (clamped to 0..lk); NULL: lk.  kv_mask: device bytes, row j at kv_mask +
+ * j * mask_b, key i of context j is left out where byte i is 0; NULL: none.  Keys
+ * that are left out are never met: their rows may hold anything, NaN included.  A
+ * query with no key left, or whose kv_of is not in 0..n_kv-1, gets zeros.  Scores
+ * and sums are fp32; in CS_BF16 mode the softmax weights are rounded to bf16 for
+ * the product with v and summed as rounded.  o must not overlap the inputs.
+ * cs_cross_attention_workspace gives the bytes of `work` (0: work may be NULL). */
+cs_status cs_cross_attention_workspace(const cs_attn_desc* desc, size_t* bytes);
+cs_status cs_cross_attention(const cs_attn_desc* desc, const void* q, const void* k, const void* v,
+                             const int32_t* kv_of, const int32_t* kv_len, const uint8_t* kv_mask,
+                             void* o, void* work, size_t work_bytes, void* stream);
+
+/* A key/value cache in 4 bits: n_kv contexts of cap rows, `heads` heads of
+ * head_dim (32, 64 or 128) channels.  A row of a head is held as e2m1 codes
+ * (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6; sign in bit 3), two to a byte with the
+ * even channel in the low half, and one scale byte b = 2^(b - 127) per 32
+ * channels:
+ *   codes  [n_kv][heads][cap][head_dim / 2], scales [n_kv][heads][cap][head_dim / 32]
+ * for the keys and for the values, contiguous, 16-byte aligned: 4.25 bits a
+ * channel.  The caller owns the four arrays; rows never stored hold what the
+ * caller left there. */
+typedef struct {
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  int32_t n_kv, heads, cap, head_dim;
+} cs_kv4_cache;
+
+/* Rows of keys and values, [n_rows][heads][head_dim] with the given strides, for
+ * cs_kv4_store and cs_kv4_load. */
+typedef struct {
+  int32_t dtype, n_rows;
+  int64_t k_row, k_head, v_row, v_head;
+} cs_kv4_rows;
+
+/* Store rows into the cache, or load the values that stored rows stand for.
+ * slots: device int32 [n_rows], row i belongs to slot (context * cap + row); a
+ * negative slot, or one not below n_kv * cap, skips the row (a loaded row is then
+ * left as it was).  NULL: row i belongs to slot i (n_rows <= n_kv * cap).  Slots
+ * named twice in one store end with an unspecified mix of the rows.
+ * Rounding: a group's scale is the power of two that puts its largest magnitude
+ * into [3.5, 7) (at least 2^-126), its codes are the nearest magnitudes, halfway
+ * values to the even code, values over 6 to 6.  A group that holds an infinity or
+ * a NaN gets scale byte 255 and stands for NaNs.  k and v, or their rows' pointers,
+ * may not be NULL unless n_rows is 0.  n_kv * cap is below 2^31. */
+cs_status cs_kv4_store(const cs_kv4_cache* cache, const cs_kv4_rows* rows, const void* k,
+                       const void* v, const int32_t* slots, void* stream);
+cs_status cs_kv4_load(const cs_kv4_cache* cache, const cs_kv4_rows* rows, void* k, void* v,
+                      const int32_t* slots, void* stream);
+
+/* cs_cross_attention over a 4-bit cache: context j is the cache's context j, and
+ * desc's n_kv, lk, heads_kv and head_dim are the cache's (its k_ and v_ strides are
+ * not read).  Rows that are left out may hold any bytes. */
+cs_status cs_kv4_attention_workspace(const cs_attn_desc* desc, size_t* bytes);
+cs_status cs_kv4_attention(const cs_attn_desc* desc, const void* q, const cs_kv4_cache* cache,
+                           const int32_t* kv_of, const int32_t* kv_len, const uint8_t* kv_mask,
+                           void* o, void* work, size_t work_bytes, void* stream);
+
 /* ---------------------------------------------------------------- ranking */
 
 /* Host only, thread-safe.  Orders candidates by decreasing score (equal

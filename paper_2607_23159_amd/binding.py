@@ -21,6 +21,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcachedse
 CS_OK, CS_E_INVAL, CS_E_NOMEM, CS_E_DEVICE, CS_E_STATE, CS_E_UNSUPPORTED = range(6)
 CS_BF16, CS_FP32 = 0, 1
 CS_CACHE_OFF, CS_CACHE_ADAPTIVE, CS_CACHE_STATIC, CS_CACHE_PAB = 0, 1, 2, 3
+CS_ROPE_PAIRS, CS_ROPE_HALVES = 0, 1
 (CS_K_SELF_ATTN, CS_K_CROSS_ATTN, CS_K_GEMM, CS_K_NORM, CS_K_DECIDE, CS_K_UPDATE, CS_K_SCORE,
  CS_K_OTHER) = range(8)
 KERNEL_FAMILIES = ["self_attn", "cross_attn", "gemm", "norm", "decide", "update", "score", "other"]
@@ -49,6 +50,30 @@ class cs_rollout_desc(C.Structure):
 class cs_rollout_stats_t(C.Structure):
     _fields_ = [("steps_done", C.c_int32), ("calls", C.c_int64), ("computed", C.c_int64),
                 ("self_reused", C.c_int64), ("cross_reused", C.c_int64), ("n_cand", C.c_int32)]
+
+
+class cs_qk_norm_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "tokens", "heads_q", "heads_k", "head_dim", "rot_dim",
+                                          "rope_rows", "rope_style")] + [("eps", C.c_float)] +
+                [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "qo_row", "qo_head", "ko_row",
+                                          "ko_head", "q_gain_head", "k_gain_head")])
+
+
+class cs_attn_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "n_q", "n_kv", "lq", "lk", "heads_q", "heads_kv", "head_dim")] +
+                [("scale", C.c_float)] +
+                [(n, C.c_int64) for n in ("q_b", "q_r", "q_h", "k_b", "k_r", "k_h", "v_b", "v_r", "v_h", "o_b",
+                                          "o_r", "o_h", "mask_b")])
+
+
+class cs_kv4_cache(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] +
+                [(n, C.c_int32) for n in ("n_kv", "heads", "cap", "head_dim")])
+
+
+class cs_kv4_rows(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "n_rows")] +
+                [(n, C.c_int64) for n in ("k_row", "k_head", "v_row", "v_head")])
 
 
 _lib: Optional[C.CDLL] = None
@@ -82,6 +107,13 @@ def lib() -> C.CDLL:
         "cs_rollout_export": (i32, [vp, vp, C.POINTER(sz)]),
         "cs_rollout_import": (i32, [vp, vp, sz]),
         "cs_rank": (i32, [pd, pd, i32, pi32, pi32, pd, pi32]),
+        "cs_qk_norm_rope": (i32, [C.POINTER(cs_qk_norm_desc)] + [vp] * 9),
+        "cs_cross_attention_workspace": (i32, [C.POINTER(cs_attn_desc), C.POINTER(sz)]),
+        "cs_cross_attention": (i32, [C.POINTER(cs_attn_desc)] + [vp] * 8 + [sz, vp]),
+        "cs_kv4_attention_workspace": (i32, [C.POINTER(cs_attn_desc), C.POINTER(sz)]),
+        "cs_kv4_attention": (i32, [C.POINTER(cs_attn_desc), vp, C.POINTER(cs_kv4_cache)] + [vp] * 5 + [sz, vp]),
+        "cs_kv4_store": (i32, [C.POINTER(cs_kv4_cache), C.POINTER(cs_kv4_rows)] + [vp] * 4),
+        "cs_kv4_load": (i32, [C.POINTER(cs_kv4_cache), C.POINTER(cs_kv4_rows)] + [vp] * 4),
         "cs_profile_enable": (i32, [vp, i32]),
         "cs_profile_reset": (i32, [vp]),
         "cs_profile_read": (i32, [vp, i32, pd, C.POINTER(i64)]),
@@ -313,6 +345,232 @@ def cs_rank(s_cached: Sequence[float], s_full: Optional[Sequence[float]]):
     _check(lib().cs_rank(a.ctypes.data_as(pd), b.ctypes.data_as(pd), n, oc.ctypes.data_as(pi),
                          of.ctypes.data_as(pi), C.byref(rho), C.byref(top1)))
     return oc.tolist(), of.tolist(), rho.value, top1.value
+
+
+# --------------------------------------------------------------- operators
+# Descriptors are made once from tensors and kept; a call then takes tensors of
+# the same shape, strides, type and device (or raw addresses, unchecked).  Tensors
+# must be on the current device.
+_DTYPES = {"bfloat16": CS_BF16, "float32": CS_FP32}
+
+
+def _sig(x):
+    return x.dtype, x.shape, x.stride(), x.device
+
+
+def _same(x, sig, name: str) -> Optional[int]:
+    """Address of a tensor that looks like the one its descriptor was made from."""
+    if x is None or isinstance(x, int):
+        return x
+    if (x.dtype, x.shape, x.stride(), x.device) != sig:
+        raise ValueError(f"{name}: the descriptor is for {sig}, got {_sig(x)}")
+    return x.data_ptr()
+
+
+def _on_current(device) -> None:
+    import torch
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+class _OpDesc:
+    """A descriptor with the tensors' signatures it stands for."""
+
+    def __init__(self, c, **sig):
+        self.c, self.ref, self.sig = c, C.byref(c), sig
+        self.device = next(s[3] for s in sig.values() if s is not None)
+
+
+def _op_tensors(dtype: str, ndim: int, **tensors):
+    """Signatures of device tensors of one type and rank whose last axis is contiguous."""
+    out, device = {}, None
+    for name, x in tensors.items():
+        if x is None:
+            out[name] = None
+            continue
+        if not getattr(x, "is_cuda", False):
+            raise ValueError(f"{name}: a device tensor is required (got {getattr(x, 'device', type(x))})")
+        if str(x.dtype).rsplit(".", 1)[-1] != dtype:
+            raise ValueError(f"{name}: dtype {x.dtype}, {dtype} required")
+        if x.dim() != ndim:
+            raise ValueError(f"{name}: {x.dim()} axes, {ndim} required")
+        if x.shape[-1] > 1 and x.stride(-1) != 1:
+            raise ValueError(f"{name}: the last axis must be contiguous")
+        if device is not None and x.device != device:
+            raise ValueError(f"{name}: on {x.device}, the others on {device}")
+        device = x.device
+        out[name] = _sig(x)
+    return out
+
+
+def _float_dtype(x) -> str:
+    d = str(x.dtype).rsplit(".", 1)[-1]
+    if d not in _DTYPES:
+        raise ValueError(f"dtype {x.dtype}, bfloat16 or float32 required")
+    return d
+
+
+def qk_norm_desc(q, k, q_out, k_out, q_gain, k_gain, rope=None, style: int = CS_ROPE_PAIRS,
+                 eps: float = 1e-6) -> _OpDesc:
+    """Descriptor of cs_qk_norm_rope.  q, q_out: [tokens][heads_q][head_dim]; k, k_out:
+    [tokens][heads_k][head_dim]; gains [heads or 1][head_dim]; rope [rope_rows][rot_dim / 2][2] or
+    None.  q with its output and gain, or k with its, may be None."""
+    one = q if q is not None else k
+    if one is None:
+        raise ValueError("q and k are both None")
+    t = _float_dtype(one)
+    sig = _op_tensors(t, 3, q=q, k=k, q_out=q_out, k_out=k_out)
+    sig.update(_op_tensors("float32", 2, q_gain=q_gain, k_gain=k_gain))
+    sig.update(_op_tensors("float32", 3, rope=rope))
+    tokens, dim = one.shape[0], one.shape[2]
+    dims = {}
+    for n, x, o, g in (("q", q, q_out, q_gain), ("k", k, k_out, k_gain)):
+        if (x is None) != (o is None) or (x is None) != (g is None):
+            raise ValueError(f"{n}, {n}_out and {n}_gain go together")
+        if x is None:
+            dims[n] = (0, 0, 0, 0, 0, 0)
+            continue
+        if x.shape[0] != tokens or x.shape[2] != dim or o.shape != x.shape:
+            raise ValueError(f"{n}: shape {tuple(x.shape)}, output {tuple(o.shape)}, {tokens} tokens of {dim} channels")
+        if g.shape[1] != dim or g.shape[0] not in (1, x.shape[1]):
+            raise ValueError(f"{n}_gain: shape {tuple(g.shape)}")
+        dims[n] = (x.shape[1], x.stride(0), x.stride(1), o.stride(0), o.stride(1), 0 if g.shape[0] == 1 else g.stride(0))
+    rows, rot = 0, 0
+    if rope is not None:
+        if rope.shape[2] != 2 or not rope.is_contiguous():
+            raise ValueError("rope: a contiguous [rows][rot_dim / 2][2] tensor is required")
+        rows, rot = rope.shape[0], 2 * rope.shape[1]
+    (hq, q0, q1, qo0, qo1, qg), (hk, k0, k1, ko0, ko1, kg) = dims["q"], dims["k"]
+    return _OpDesc(cs_qk_norm_desc(_DTYPES[t], tokens, hq, hk, dim, rot, rows, style, eps, q0, q1, k0, k1, qo0, qo1,
+                                   ko0, ko1, qg, kg), **sig)
+
+
+def cs_qk_norm_rope(desc: _OpDesc, q, k, q_out, k_out, q_gain, k_gain, rope=None, pos=None, stream=None) -> None:
+    """``pos``: int32 device tensor [tokens] or None."""
+    _on_current(desc.device)
+    s = desc.sig
+    _check(lib().cs_qk_norm_rope(desc.ref, _same(q, s["q"], "q"), _same(k, s["k"], "k"),
+                                 _same(q_out, s["q_out"], "q_out"), _same(k_out, s["k_out"], "k_out"),
+                                 _same(q_gain, s["q_gain"], "q_gain"), _same(k_gain, s["k_gain"], "k_gain"),
+                                 _same(rope, s["rope"], "rope"), _ptr(pos, desc.c.tokens, "int32", "pos"),
+                                 _stream(stream)))
+
+
+class Kv4Cache(_OpDesc):
+    """A 4-bit cache over four contiguous uint8 device tensors: codes
+    [n_kv][heads][cap][head_dim / 2] and scales [n_kv][heads][cap][head_dim / 32], of
+    the keys and of the values.  Keeps the tensors."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        sig = _op_tensors("uint8", 4, k_codes=k_codes, k_scales=k_scales, v_codes=v_codes, v_scales=v_scales)
+        n, h, cap, half = k_codes.shape
+        for name, x in (("k_codes", k_codes), ("v_codes", v_codes), ("k_scales", k_scales), ("v_scales", v_scales)):
+            want = (n, h, cap, half if name.endswith("codes") else half // 16)
+            if tuple(x.shape) != want or not x.is_contiguous():
+                raise ValueError(f"{name}: a contiguous {want} tensor is required, got {tuple(x.shape)}")
+        self.tensors = (k_codes, k_scales, v_codes, v_scales)
+        super().__init__(cs_kv4_cache(*(x.data_ptr() for x in self.tensors), n, h, cap, 2 * half), **sig)
+        self._rows = {}
+
+    def rows(self, k, v) -> _OpDesc:
+        """cs_kv4_rows of tensors [n_rows][heads][head_dim] shaped like k and v (kept)."""
+        key = (k.dtype, k.shape, k.stride(), k.device, v.dtype, v.shape, v.stride(), v.device)
+        d = self._rows.get(key)
+        if d is None:
+            t = _float_dtype(k)
+            sig = _op_tensors(t, 3, k=k, v=v)
+            want = (k.shape[0], self.c.heads, self.c.head_dim)
+            if tuple(k.shape) != want or tuple(v.shape) != want or k.device != self.device:
+                raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)}: {want} on {self.device} required")
+            d = _OpDesc(cs_kv4_rows(_DTYPES[t], want[0], k.stride(0), k.stride(1), v.stride(0), v.stride(1)), **sig)
+            if len(self._rows) >= 64:   # layouts of a serving loop are few
+                self._rows.clear()
+            self._rows[key] = d
+        return d
+
+
+def cs_kv4_store(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
+    """Rows k, v [n_rows][heads][head_dim] into the cache; ``slots``: int32 device tensor or None."""
+    _on_current(cache.device)
+    d = cache.rows(k, v)
+    _check(lib().cs_kv4_store(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _ptr(slots, d.c.n_rows, "int32", "slots"),
+                              _stream(stream)))
+
+
+def cs_kv4_load(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
+    """The values that rows of the cache stand for into k and v."""
+    _on_current(cache.device)
+    d = cache.rows(k, v)
+    _check(lib().cs_kv4_load(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _ptr(slots, d.c.n_rows, "int32", "slots"),
+                             _stream(stream)))
+
+
+def _attn_desc(q, o, n_kv, lk, heads_kv, dim, kv_strides, scale, sig) -> _OpDesc:
+    if o.shape != q.shape or q.shape[3] != dim:
+        raise ValueError(f"q {tuple(q.shape)}, o {tuple(o.shape)}, {dim} channels")
+    if scale is None:
+        scale = 1.0 / math.sqrt(dim)
+    n, lq, h, _ = q.shape
+    return _OpDesc(cs_attn_desc(_DTYPES[_float_dtype(q)], n, n_kv, lq, lk, h, heads_kv, dim, scale, *q.stride()[:3],
+                                *kv_strides, *o.stride()[:3], lk), **sig)
+
+
+def attn_desc(q, k, v, o, scale: Optional[float] = None) -> _OpDesc:
+    """Descriptor of cs_cross_attention.  q, o: [n_q][lq][heads_q][head_dim]; k, v:
+    [n_kv][lk][heads_kv][head_dim].  scale: None for 1 / sqrt(head_dim)."""
+    sig = _op_tensors(_float_dtype(q), 4, q=q, k=k, v=v, o=o)
+    if v.shape != k.shape:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    n_kv, lk, hkv, dim = k.shape
+    return _attn_desc(q, o, n_kv, lk, hkv, dim, (*k.stride()[:3], *v.stride()[:3]), scale, sig)
+
+
+def kv4_attn_desc(q, cache: Kv4Cache, o, scale: Optional[float] = None) -> _OpDesc:
+    """Descriptor of cs_kv4_attention over a cache."""
+    sig = _op_tensors(_float_dtype(q), 4, q=q, o=o)
+    if q.device != cache.device:
+        raise ValueError(f"q on {q.device}, the cache on {cache.device}")
+    c = cache.c
+    return _attn_desc(q, o, c.n_kv, c.cap, c.heads, c.head_dim, (0,) * 6, scale, sig)
+
+
+def cs_cross_attention_workspace(desc: _OpDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().cs_cross_attention_workspace(desc.ref, C.byref(n)))
+    return n.value
+
+
+def cs_kv4_attention_workspace(desc: _OpDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().cs_kv4_attention_workspace(desc.ref, C.byref(n)))
+    return n.value
+
+
+def _attn_rest(desc: _OpDesc, kv_of, kv_len, kv_mask, work):
+    """Addresses of the index tensors (int32), the mask ([n_kv][lk] uint8, contiguous) and the workspace."""
+    c = desc.c
+    nbytes = 0 if work is None else (work.numel() * work.element_size() if not isinstance(work, int) else 1 << 62)
+    return (_ptr(kv_of, c.n_q, "int32", "kv_of"), _ptr(kv_len, c.n_kv, "int32", "kv_len"),
+            _ptr(kv_mask, c.n_kv * c.lk, "uint8", "kv_mask"),
+            work if work is None or isinstance(work, int) else work.data_ptr(), nbytes)
+
+
+def cs_cross_attention(desc: _OpDesc, q, k, v, o, kv_of=None, kv_len=None, kv_mask=None, work=None,
+                       stream=None) -> None:
+    _on_current(desc.device)
+    s = desc.sig
+    of, ln, mask, w, nbytes = _attn_rest(desc, kv_of, kv_len, kv_mask, work)
+    _check(lib().cs_cross_attention(desc.ref, _same(q, s["q"], "q"), _same(k, s["k"], "k"), _same(v, s["v"], "v"), of, ln,
+                                    mask, _same(o, s["o"], "o"), w, nbytes, _stream(stream)))
+
+
+def cs_kv4_attention(desc: _OpDesc, q, cache: Kv4Cache, o, kv_of=None, kv_len=None, kv_mask=None, work=None,
+                     stream=None) -> None:
+    _on_current(desc.device)
+    s = desc.sig
+    of, ln, mask, w, nbytes = _attn_rest(desc, kv_of, kv_len, kv_mask, work)
+    _check(lib().cs_kv4_attention(desc.ref, _same(q, s["q"], "q"), cache.ref, of, ln, mask, _same(o, s["o"], "o"), w,
+                                  nbytes, _stream(stream)))
 
 
 def cs_profile_enable(model: int, on: bool) -> None:

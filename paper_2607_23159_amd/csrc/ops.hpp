@@ -1,0 +1,76 @@
+// Launchers of the stand-alone operators (cs_qk_norm_rope, cs_cross_attention,
+// cs_kv4_*).  Arguments are validated by ops.hip before any launch.
+#pragma once
+#include "../../include/cs.h"
+#include "common.hpp"
+
+namespace cs {
+
+// ---- per-head norms with rotation (k_qk_norm.hip)
+struct QkNormArgs {
+  const void *q, *k;
+  void *qo, *ko;
+  const float *q_gain, *k_gain, *rope;
+  const int* pos;
+  cs_qk_norm_desc d;
+};
+template <typename T> hipError_t qk_norm_rope(const QkNormArgs& a, hipStream_t st);
+
+// ---- rows of the 4-bit cache (k_kv4.hip)
+struct Kv4RowsArgs {
+  cs_kv4_cache c;
+  cs_kv4_rows r;
+  const void *k, *v;     // stored rows
+  void *ko, *vo;         // loaded rows
+  const int* slots;
+};
+template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
+template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);
+
+// ---- attention to contexts (k_xattn.hip)
+struct XAttnArgs {
+  const void *q, *k, *v;
+  void* o;
+  const int *kv_of, *kv_len;
+  const uint8_t* mask;
+  cs_kv4_cache c;        // 4-bit keys and values (k, v not read)
+  cs_attn_desc d;
+  float scale_log2;      // log2(e) * scale
+  void* work;
+};
+size_t xattn_workspace(const cs_attn_desc& d, bool kv4);
+template <typename T> hipError_t xattn(const XAttnArgs& a, bool kv4, hipStream_t st);
+
+// Keys of the context of query set i, and the context's index (0 keys if kv_of is out of range).
+CS_DEV int xattn_context(const XAttnArgs& a, int i, int* len) {
+  const int j = a.kv_of ? a.kv_of[i] : i;
+  if (j < 0 || j >= a.d.n_kv) {
+    *len = 0;
+    return 0;
+  }
+  *len = a.kv_len ? max(0, min(a.kv_len[j], a.d.lk)) : a.d.lk;
+  return j;
+}
+
+// ---- 4-bit values: e2m1 codes and their scale bytes.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+// Scale byte of a group whose largest magnitude has these fp32 bits: exponent of
+// the power of two that puts it into [3.5, 7).  A quarter added to the mantissa
+// carries into the exponent from 1.75 on.  255 for an infinity or a NaN.
+CS_DEV uint32_t kv4_scale_byte(uint32_t amax_bits) {
+  if (amax_bits >= 0x7F800000u) return 255;
+  return (uint32_t)max(1, (int)((amax_bits + 0x200000u) >> 23) - 2);
+}
+// Scale 2^(b - 127) of byte b; 255 gives infinity, which the conversions below turn into NaN.
+CS_DEV float kv4_scale(uint32_t b) { return __uint_as_float(b << 23); }
+// Eight codes of four bytes to bf16 (exact: a code has two significant bits).
+CS_DEV bf16x8 kv4_decode8(uint32_t codes, float scale) {
+  union { bf16x8 v; bf16x2 p[4]; } r;
+  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+  return r.v;
+}
+
+}  // namespace cs

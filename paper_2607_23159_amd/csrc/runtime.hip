@@ -14,7 +14,7 @@
 #include <string>
 #include <vector>
 
-#include "../../include/cs.h"
+#include "host.hpp"
 #include "kernels.hpp"
 
 using namespace cs;
@@ -22,7 +22,7 @@ using namespace cs;
 // ------------------------------------------------------------------ errors
 static thread_local std::string g_err;
 
-static cs_status fail(cs_status code, const char* fmt, ...) {
+cs_status cs::fail(cs_status code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -31,30 +31,6 @@ static cs_status fail(cs_status code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
-
-#define HIPC(call)                                                                   \
-  do {                                                                               \
-    hipError_t e_ = (call);                                                          \
-    if (e_ != hipSuccess) {                                                          \
-      if (e_ == hipErrorOutOfMemory)                                                 \
-        return fail(CS_E_NOMEM, "%s: %s", #call, hipGetErrorString(e_));            \
-      return fail(CS_E_DEVICE, "%s: %s (%d)", #call, hipGetErrorString(e_), (int)e_); \
-    }                                                                                \
-  } while (0)
-
-#define CHECK(cond, code, ...)                 \
-  do {                                         \
-    if (!(cond)) return fail(code, __VA_ARGS__); \
-  } while (0)
-
-#define GUARD(...)                                                         \
-  try {                                                                    \
-    __VA_ARGS__                                                            \
-  } catch (const std::bad_alloc&) {                                        \
-    return fail(CS_E_NOMEM, "host allocation failed");                     \
-  } catch (...) {                                                          \
-    return fail(CS_E_DEVICE, "unexpected exception in the runtime");       \
-  }
 
 // Test hook: cap on device bytes a single allocation may request (0 = none),
 // so that out-of-memory handling can be exercised without exhausting HBM.
@@ -74,12 +50,6 @@ static cs_status dmalloc(void** p, size_t bytes) {
   }
   return CS_OK;
 }
-
-#define TRY(x)                    \
-  do {                            \
-    cs_status s_ = (x);           \
-    if (s_ != CS_OK) return s_;   \
-  } while (0)
 
 // ---------------------------------------------------------------- profiler
 struct Profiler {
