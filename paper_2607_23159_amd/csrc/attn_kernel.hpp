@@ -474,32 +474,6 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_flash_dl(AttnArgs<bf16> a) {
 }
 
 
-// O^T accumulators of a wave's 32 queries, normalised and stored as row
-// query l32 of dst (row stride o_ld).  A lane holds 4 consecutive channels per
-// group of 8 and the lane 32 away the other 4: exchanging them between two
-// groups (v_permlane32_swap) gives each lane 8 consecutive channels of one
-// group, one 16-byte store instead of two of 8 bytes.  Measured with the Q
-// loads behind the first tile's: 32,760 queries x 512 keys x 12 heads, 8
-// streams 1045 -> 988 us, one stream 159 -> 144 us; 384 x 512, one stream 19.9
-// -> 17.6 us; neutral over 32,760 keys (bitwise equal).
-template <int NDT>
-CS_DEV void store_o_rows(const f32x16 (&o)[NDT], float inv, bf16* dst, int half, bool valid) {
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int g = 0; g < 4; g += 2) {
-      union { bf16x4 v; uint32_t u[2]; } x, y;   // groups g and g + 1
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x.v[r] = (bf16)(o[dt][4 * g + r] * inv);
-        y.v[r] = (bf16)(o[dt][4 * g + 4 + r] * inv);
-      }
-      const auto w0 = __builtin_amdgcn_permlane32_swap(x.u[0], y.u[0], false, false);
-      const auto w1 = __builtin_amdgcn_permlane32_swap(x.u[1], y.u[1], false, false);
-      if (valid) *reinterpret_cast<uint4*>(dst + dt * 32 + 8 * (g + half)) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
-    }
-}
-
 // ---------------------------------------------------------------------------
 // bf16 variant with padded LDS rows (head dims 64 and 128).
 //

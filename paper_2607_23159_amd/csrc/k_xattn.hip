@@ -1,129 +1,169 @@
-// Attention of queries to contexts of their own lengths, over keys and values in
-// the compute type or in 4 bits.
+// Attention of queries to contexts: choice of the kernel, workspace, join of the
+// parts of long contexts.
 #include "ops.hpp"
+
+#include <algorithm>
 
 namespace cs {
 
-// Channel values of key rows, per storage.
-template <typename T> struct KvPlain {
-  const T *k, *v;
-  long k_r, v_r;
-  CS_DEV KvPlain(const XAttnArgs& a, int ctx, int head)
-      : k((const T*)a.k + ctx * a.d.k_b + head * a.d.k_h), v((const T*)a.v + ctx * a.d.v_b + head * a.d.v_h),
-        k_r(a.d.k_r), v_r(a.d.v_r) {}
-  CS_DEV void key8(int key, int c, float* f) const {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)k[key * k_r + c + i];
+// A problem's keys are cut into parts by its own sizes, never by the batch, so that
+// results do not depend on it.
+static void cut(XAttnArgs& a) {
+  a.group = a.d.heads_q / a.d.heads_kv;
+  a.rows = a.d.lq * a.group;
+  a.parts = 1;
+  a.part_keys = a.d.lk;
+  const int least = 512, most = 128;   // keys of a part, parts
+  if (a.rows <= 1024 && a.d.lk > least) {
+    a.part_keys = (int)std::max<long>(least, round_up(cdiv(a.d.lk, most), 128));
+    a.parts = cdiv(a.d.lk, a.part_keys);
   }
-  CS_DEV float value(int key, int c) const { return (float)v[key * v_r + c]; }
-};
-
-template <int DH> struct Kv4Rows {
-  const uint8_t *kc, *ks, *vc, *vs;
-  CS_DEV Kv4Rows(const XAttnArgs& a, int ctx, int head) {
-    const long at = ((long)ctx * a.c.heads + head) * a.c.cap;
-    kc = a.c.k_codes + at * (DH / 2);
-    vc = a.c.v_codes + at * (DH / 2);
-    ks = a.c.k_scales + at * (DH / 32);
-    vs = a.c.v_scales + at * (DH / 32);
-  }
-  CS_DEV void key8(int key, int c, float* f) const {
-    const uint32_t codes = *reinterpret_cast<const uint32_t*>(kc + (long)key * (DH / 2) + c / 2);
-    const bf16x8 v = kv4_decode8(codes, kv4_scale(ks[(long)key * (DH / 32) + c / 32]));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)v[i];
-  }
-  CS_DEV float value(int key, int c) const {
-    const uint32_t code = vc[(long)key * (DH / 2) + c / 2] >> (4 * (c & 1));
-    return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, kv4_scale(vs[(long)key * (DH / 32) + c / 32]), 0)[0];
-  }
-};
-
-CS_DEV float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, WAVE));
-  return v;
 }
 
-// One wave per query and head: 64 keys at a time, a lane per key for the scores
-// (online softmax across the wave), a lane per channel for the values.
-template <typename T, int DH, typename KV>
-__global__ __launch_bounds__(256) void k_xattn_wave(XAttnArgs a) {
-  __shared__ float s_q[4][DH];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long item = (long)blockIdx.x * 4 + wave, n = (long)a.d.n_q * a.d.lq * a.d.heads_q;
-  const long it = item < n ? item : n - 1;
-  const int head = (int)(it % a.d.heads_q);
-  const long row = it / a.d.heads_q;
-  const int set = (int)(row / a.d.lq), qi = (int)(row - (long)set * a.d.lq);
+struct Work {
+  size_t part_o = 0, part_ml = 0, k = 0, v = 0, bytes = 0;
+};
+static Work layout(const XAttnArgs& a, bool kv4) {
+  Work w;
+  auto take = [&](size_t n) {
+    const size_t at = w.bytes;
+    w.bytes += (size_t)round_up((long)n, 256);
+    return at;
+  };
+  if (a.d.n_q == 0 || a.rows == 0) return w;
+  if (a.parts > 1) {
+    const size_t rows = (size_t)a.d.n_q * a.d.heads_kv * a.parts * a.rows;
+    w.part_o = take(rows * a.d.head_dim * sizeof(float));
+    w.part_ml = take(rows * sizeof(float2));
+  }
+  if (kv4 && a.rows > XATTN_FEW_ROWS) {
+    const size_t n = (size_t)a.d.n_kv * a.d.lk * a.d.heads_kv * a.d.head_dim * (a.d.dtype == CS_BF16 ? 2 : 4);
+    w.k = take(n);
+    w.v = take(n);
+  }
+  return w;
+}
+
+size_t xattn_workspace(const cs_attn_desc& d, bool kv4) {
+  XAttnArgs a = {};
+  a.d = d;
+  cut(a);
+  return layout(a, kv4).bytes;
+}
+
+// One row: the parts' outputs, each weighted with 2^(m_p - m).  Sixteen waves
+// take every sixteenth part, lanes the channels.
+template <typename T, int DH> __global__ __launch_bounds__(1024) void k_xattn_join(XAttnArgs a) {
+  constexpr int NW = 16, MAXP = 128;
+  __shared__ float s_w[MAXP], s_o[NW][DH], s_red[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const long pr = blockIdx.x / a.rows;              // problem
+  const int r = (int)(blockIdx.x - pr * a.rows);
+  const int set = (int)(pr / a.d.heads_kv), head = (int)(pr - (long)set * a.d.heads_kv);
   int len;
-  const int ctx = xattn_context(a, set, &len);
-  const KV kv(a, ctx, head / (a.d.heads_q / a.d.heads_kv));
-  const uint8_t* mask = a.mask ? a.mask + ctx * a.d.mask_b : nullptr;
-  const T* q = (const T*)a.q + set * a.d.q_b + qi * a.d.q_r + head * a.d.q_h;
-  for (int c = lane; c < DH; c += 64) s_q[wave][c] = (float)q[c];
-  __syncthreads();
-
+  xattn_context(a, set, &len);
+  const int n = (len + a.part_keys - 1) / a.part_keys;
+  const long base = pr * a.parts * a.rows + r;
   constexpr int NC = (DH + 63) / 64;
-  float m = -INFINITY, l = 0.0f, o[NC] = {};
-  for (int base = 0; base < len; base += 64) {
-    const int key = base + lane;
-    const bool left = key < len && (!mask || mask[key] != 0);
-    float s = -INFINITY;
-    if (left) {
-      s = 0.0f;
-      for (int c = 0; c < DH; c += 8) {
-        float f[8];
-        kv.key8(key, c, f);
+  float o[MAXP / NW][NC];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(s_q[wave][c + i], f[i], s);
-      }
-      s *= a.scale_log2;
-    }
-    const float m_new = fmaxf(m, wave_max(s));
-    if (m_new == -INFINITY) continue;
-    const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-    m = m_new;
-    const float p = left ? (float)to_t<T>(__builtin_amdgcn_exp2f(s - m)) : 0.0f;
-    l = l * alpha + wave_sum(p);
+  for (int i = 0; i < MAXP / NW; ++i) {
+    const int p = wave + NW * i;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) o[i] *= alpha;
-    for (int j = 0; j < 64 && base + j < len; ++j) {
-      const float pj = __shfl(p, j, WAVE);
-      if (pj == 0.0f) continue;
-#pragma unroll
-      for (int i = 0; i < NC; ++i)
-        if (lane + 64 * i < DH) o[i] = fmaf(pj, kv.value(base + j, lane + 64 * i), o[i]);
-    }
+    for (int c = 0; c < NC; ++c)
+      o[i][c] = p < n && lane + 64 * c < DH ? a.part_o[(base + (long)p * a.rows) * DH + lane + 64 * c] : 0.0f;
   }
-  if (item >= n) return;
-  T* dst = (T*)a.o + set * a.d.o_b + qi * a.d.o_r + head * a.d.o_h;
+  if (wave == 0) {
+    float m[2], l[2];
 #pragma unroll
-  for (int i = 0; i < NC; ++i)
-    if (lane + 64 * i < DH) dst[lane + 64 * i] = to_t<T>(l > 0.0f ? o[i] / l : 0.0f);
+    for (int i = 0; i < 2; ++i) {
+      const int p = lane + 64 * i;
+      const float2 ml = p < n ? a.part_ml[base + (long)p * a.rows] : make_float2(-INFINITY, 0.0f);
+      m[i] = ml.x;
+      l[i] = ml.y;
+    }
+    float mx = fmaxf(m[0], m[1]);
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor(mx, s, WAVE));
+    if (mx == -INFINITY) mx = 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float w = __builtin_amdgcn_exp2f(m[i] - mx);
+      s_w[lane + 64 * i] = w;
+      sum = fmaf(w, l[i], sum);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) s_red[0] = sum;
+  }
+  __syncthreads();
+  float acc[NC] = {};
+#pragma unroll
+  for (int i = 0; i < MAXP / NW; ++i)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (wave + NW * i < n) acc[c] = fmaf(s_w[wave + NW * i], o[i][c], acc[c]);
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    if (lane + 64 * c < DH) s_o[wave][lane + 64 * c] = acc[c];
+  __syncthreads();
+  if (tid < DH) {
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += s_o[w][tid];
+    const float l = s_red[0];
+    T* dst = (T*)a.o + set * a.d.o_b + xattn_row(a, r, head, a.d.o_r, a.d.o_h);
+    dst[tid] = to_t<T>(l != 0.0f ? v / l : 0.0f);
+  }
 }
 
-size_t xattn_workspace(const cs_attn_desc&, bool) { return 0; }
-
-template <typename T, int DH> static hipError_t launch(const XAttnArgs& a, bool kv4, hipStream_t st) {
-  const long blocks = ((long)a.d.n_q * a.d.lq * a.d.heads_q + 3) / 4;
-  if (blocks > 0xFFFFFFL) return hipErrorInvalidConfiguration;
-  if (kv4)
-    hipLaunchKernelGGL((k_xattn_wave<T, DH, Kv4Rows<DH>>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_xattn_wave<T, DH, KvPlain<T>>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+template <typename T> static hipError_t join(const XAttnArgs& a, hipStream_t st) {
+  const long blocks = (long)a.d.n_q * a.d.heads_kv * a.rows;
+  if (blocks > 0x3FFFFFL) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks), block(1024);
+  switch (a.d.head_dim) {
+    case 128: hipLaunchKernelGGL((k_xattn_join<T, 128>), grid, block, 0, st, a); break;
+    case 64: hipLaunchKernelGGL((k_xattn_join<T, 64>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_xattn_join<T, 32>), grid, block, 0, st, a); break;
+  }
   return hipGetLastError();
 }
 
-template <typename T> hipError_t xattn(const XAttnArgs& a, bool kv4, hipStream_t st) {
-  switch (a.d.head_dim) {
-    case 128: return launch<T, 128>(a, kv4, st);
-    case 64: return launch<T, 64>(a, kv4, st);
-    case 32: return launch<T, 32>(a, kv4, st);
-    default: return hipErrorInvalidValue;
+template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStream_t st) {
+  cut(a);
+  const Work w = layout(a, kv4);
+  a.part_o = (float*)((char*)work + w.part_o);
+  a.part_ml = (float2*)((char*)work + w.part_ml);
+  if (a.parts > 1 && (long)a.d.n_q * a.d.heads_kv * a.rows > 0x3FFFFFL) return hipErrorInvalidConfiguration;
+  hipError_t e;
+  if (a.rows <= XATTN_FEW_ROWS && (kv4 || sizeof(T) == 2)) {
+    e = xattn_rows<T>(a, kv4, st);
+  } else {
+    if (kv4) {
+      // many queries meet every key: unpack the cache once
+      Kv4RowsArgs l = {};
+      l.c = a.c;
+      const long hd = (long)a.d.heads_kv * a.d.head_dim;
+      l.r = {a.d.dtype, a.d.n_kv * a.d.lk, hd, a.d.head_dim, hd, a.d.head_dim};
+      l.ko = (char*)work + w.k;
+      l.vo = (char*)work + w.v;
+      e = kv4_load<T>(l, st);
+      if (e != hipSuccess) return e;
+      a.k = l.ko;
+      a.v = l.vo;
+      a.d.k_r = a.d.v_r = hd;
+      a.d.k_h = a.d.v_h = a.d.head_dim;
+      a.d.k_b = a.d.v_b = hd * a.d.lk;
+    }
+    if constexpr (sizeof(T) == 2)
+      e = xattn_tile(a, st);
+    else
+      e = xattn_f32(a, st);
   }
+  if (e == hipSuccess && a.parts > 1) e = join<T>(a, st);
+  return e;
 }
-template hipError_t xattn<bf16>(const XAttnArgs&, bool, hipStream_t);
-template hipError_t xattn<float>(const XAttnArgs&, bool, hipStream_t);
+template hipError_t xattn<bf16>(XAttnArgs, bool, void*, hipStream_t);
+template hipError_t xattn<float>(XAttnArgs, bool, void*, hipStream_t);
 
 }  // namespace cs

@@ -153,6 +153,9 @@ static cs_status check_attn(const cs_attn_desc* d, bool kv4) {
   // rows of a set: queries x the heads that share a key head
   CHECK((long)d->lq * (d->heads_q / d->heads_kv) < (1L << 30) && d->lk < (1 << 30), CS_E_UNSUPPORTED,
         "lq x heads and lk must be below 2^30");
+  // offsets inside a tile of keys are 32-bit byte counts
+  CHECK(kv4 || d->lk <= 1 || (d->k_r <= (1 << 23) && d->v_r <= (1 << 23)), CS_E_UNSUPPORTED,
+        "strides k_r and v_r must be at most 2^23");
   const int e = elem(d->dtype);
   TRY(check_stride(d->q_b, d->n_q, e, "q_b"));
   TRY(check_stride(d->q_r, d->lq, e, "q_r"));
@@ -188,11 +191,11 @@ static cs_status attn_call(const cs_attn_desc* d, const void* q, const void* k, 
     CHECK(work && aligned(work), CS_E_INVAL, "a 16-byte aligned workspace is needed");
     CHECK(work_bytes >= need, CS_E_INVAL, "the workspace holds %zu bytes, %zu needed", work_bytes, need);
   }
-  XAttnArgs a = {q, k, v, o, kv_of, kv_len, kv_mask, {}, *d, (float)(1.4426950408889634 * d->scale), work};
+  XAttnArgs a = {q, k, v, o, kv_of, kv_len, kv_mask, {}, *d, (float)(1.4426950408889634 * d->scale)};
   if (kv4) a.c = *cache;
   if (d->lk == 1) a.d.k_r = a.d.v_r = d->head_dim;   // never checked
   hipStream_t st = (hipStream_t)stream;
-  const hipError_t s = d->dtype == CS_BF16 ? xattn<bf16>(a, kv4, st) : xattn<float>(a, kv4, st);
+  const hipError_t s = d->dtype == CS_BF16 ? xattn<bf16>(a, kv4, work, st) : xattn<float>(a, kv4, work, st);
   CHECK(s != hipErrorInvalidConfiguration, CS_E_UNSUPPORTED, "too many queries and heads for one call");
   HIPC(s);
   return CS_OK;

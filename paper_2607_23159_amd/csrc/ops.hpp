@@ -27,7 +27,9 @@ struct Kv4RowsArgs {
 template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
 template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);
 
-// ---- attention to contexts (k_xattn.hip)
+// ---- attention to contexts (k_xattn*.hip)
+// The queries of a set that share a key head are the rows of one problem: row r is
+// query r / group, head (key head) * group + r % group.
 struct XAttnArgs {
   const void *q, *k, *v;
   void* o;
@@ -36,10 +38,24 @@ struct XAttnArgs {
   cs_kv4_cache c;        // 4-bit keys and values (k, v not read)
   cs_attn_desc d;
   float scale_log2;      // log2(e) * scale
-  void* work;
+  int rows, group;       // lq * group, heads_q / heads_kv
+  // Long contexts: part p of a problem takes keys [p * part_keys, (p + 1) *
+  // part_keys) and leaves its outputs relative to its maximum m and its sums l:
+  // part_o [problem][part][rows][head_dim], part_ml [problem][part][rows] (m, l).
+  int parts, part_keys;
+  float* part_o;
+  float2* part_ml;
 };
 size_t xattn_workspace(const cs_attn_desc& d, bool kv4);
-template <typename T> hipError_t xattn(const XAttnArgs& a, bool kv4, hipStream_t st);
+// work: xattn_workspace bytes.
+template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStream_t st);
+
+// The kernels' launchers: few rows (k_xattn_rows.hip), many rows in bf16
+// (k_xattn_tile.hip), fp32 (k_xattn_f32.hip), and the join of the parts.
+constexpr int XATTN_FEW_ROWS = 64;
+template <typename T> hipError_t xattn_rows(const XAttnArgs& a, bool kv4, hipStream_t st);
+hipError_t xattn_tile(const XAttnArgs& a, hipStream_t st);
+hipError_t xattn_f32(const XAttnArgs& a, hipStream_t st);
 
 // Keys of the context of query set i, and the context's index (0 keys if kv_of is out of range).
 CS_DEV int xattn_context(const XAttnArgs& a, int i, int* len) {
@@ -50,6 +66,12 @@ CS_DEV int xattn_context(const XAttnArgs& a, int i, int* len) {
   }
   *len = a.kv_len ? max(0, min(a.kv_len[j], a.d.lk)) : a.d.lk;
   return j;
+}
+
+// Offset of row r of problem (set, key head) in q or o.
+CS_DEV long xattn_row(const XAttnArgs& a, int r, int head, long stride_r, long stride_h) {
+  const int t = r / a.group;
+  return t * stride_r + ((long)head * a.group + (r - t * a.group)) * stride_h;
 }
 
 // ---- 4-bit values: e2m1 codes and their scale bytes.
