@@ -146,12 +146,41 @@ cs_status cs_model_init(const cs_model_desc* desc, const float* weights, size_t 
                         void* stream, cs_model** out);
 void cs_model_free(cs_model* model);
 
+/* RMS norm of q and k inside the transformer: over the whole hidden width
+ * (cs_model_init), or over each head's own channels (cs_qk_norm_rope).  The
+ * gains are the same [d] vectors either way. */
+typedef enum { CS_QK_NORM_FULL = 0, CS_QK_NORM_HEAD = 1 } cs_qk_norm;
+/* cs_model_init with the choice of the norm (cs_qk_norm).  Everything else,
+ * rollouts included, is as with cs_model_init. */
+cs_status cs_model_init_norm(const cs_model_desc* desc, int32_t qk_norm, const float* weights,
+                             size_t n_weights, void* stream, cs_model** out);
+
 /* One transformer evaluation v_theta(x, t, c) (Sec. Preliminaries) for n
  * latents sharing the timestep t and one text context.  x: device
  * [n][D] float32; ctx: device [text_len][text_dim] float32; v: device
  * [n][D] float32 (may not alias x).  Enqueued on the model's stream. */
 cs_status cs_velocity(cs_model* model, const float* x, int32_t n, float t, const float* ctx,
                       float* v);
+
+/* Contexts: the text of n_prompts prompts of their own lengths, projected to
+ * the keys and values of every block once and kept, in the model's compute type
+ * or in 4 bits (cs_kv4_cache: about a quarter of the memory, and its rounding).
+ * ctx: device [n_prompts][text_len][text_dim] float32, lens: host [n_prompts],
+ * the rows of each prompt (0..text_len; a prompt of none adds no attention), or
+ * NULL for text_len each; rows past a prompt's length may hold anything.
+ * Synchronises the model's stream.  The context belongs to its model and is freed
+ * before it. */
+typedef enum { CS_KV_NATIVE = 0, CS_KV_4BIT = 1 } cs_kv_format;
+typedef struct cs_context cs_context;
+cs_status cs_context_init(cs_model* model, const float* ctx, const int32_t* lens,
+                          int32_t n_prompts, int32_t kv_format, cs_context** out);
+void cs_context_free(cs_context* context);
+
+/* cs_velocity for n latents that attend to prompts of a context, each over its
+ * prompt's length: prompt: host [n], the prompt of each latent; NULL: latent i
+ * attends to prompt i (n <= n_prompts). */
+cs_status cs_velocity_context(cs_model* model, cs_context* context, const float* x,
+                              const int32_t* prompt, int32_t n, float t, float* v);
 
 /* -------------------------------------------------------------- rollout */
 
@@ -361,7 +390,8 @@ typedef struct {
  * Rounding: a group's scale is the power of two that puts its largest magnitude
  * into [3.5, 7) (at least 2^-126), its codes are the nearest magnitudes, halfway
  * values to the even code, values over 6 to 6.  A group that holds an infinity or
- * a NaN gets scale byte 255 and stands for NaNs.  k and v, or their rows' pointers,
+ * a NaN gets scale byte 255 and stands for NaNs (bf16 magnitudes from 1.75 x 2^127 on
+ * load as infinities).  k and v, or their rows' pointers,
  * may not be NULL unless n_rows is 0.  n_kv * cap is below 2^31. */
 cs_status cs_kv4_store(const cs_kv4_cache* cache, const cs_kv4_rows* rows, const void* k,
                        const void* v, const int32_t* slots, void* stream);

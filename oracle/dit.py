@@ -65,6 +65,12 @@ def rms_norm(z: np.ndarray, gain: np.ndarray, eps: float = EPS) -> np.ndarray:
     return z / np.sqrt(ms + eps) * as64(gain)
 
 
+def rms_norm_heads(z: np.ndarray, gain: np.ndarray, heads: int, eps: float = EPS) -> np.ndarray:
+    """RMS norm of every head over its own channels; the gain has one entry per channel of the row."""
+    h = z.reshape(z.shape[0], heads, z.shape[1] // heads)
+    return rms_norm(h, as64(gain).reshape(heads, -1), eps).reshape(z.shape)
+
+
 def gelu_tanh(x: np.ndarray) -> np.ndarray:
     """GELU, tanh approximation (Hendrycks & Gimpel)."""
     return 0.5 * x * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (x + 0.044715 * x ** 3)))
@@ -88,7 +94,9 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, heads: int) -> np.nda
     """
     lq, dm = q.shape
     dh = dm // heads
-    out = np.empty((lq, dm), dtype=np.float64)
+    out = np.zeros((lq, dm), dtype=np.float64)
+    if k.shape[0] == 0:      # an empty context adds nothing
+        return out
     scale = 1.0 / math.sqrt(dh)
     for h in range(heads):
         sl = slice(h * dh, (h + 1) * dh)
@@ -202,7 +210,7 @@ def text_embedding(ctx: np.ndarray, W: Dict[str, np.ndarray]) -> np.ndarray:
 def block_forward(z: np.ndarray, j: int, m6: np.ndarray, ctx_emb: np.ndarray,
                   ang: np.ndarray, W: Dict[str, np.ndarray], heads: int,
                   rows: Optional[np.ndarray] = None,
-                  attn_io: Optional[dict] = None) -> np.ndarray:
+                  attn_io: Optional[dict] = None, head_norm: bool = False) -> np.ndarray:
     """One transformer block.  z [L][d] float64; returns the new residual.
 
     ``rows`` (optional) restricts the output to those token rows: keys and
@@ -215,7 +223,12 @@ def block_forward(z: np.ndarray, j: int, m6: np.ndarray, ctx_emb: np.ndarray,
     taken after the branch's output projection and before the self-attention
     gate.  The outputs actually used are written back to "self_out" and
     "cross_out".
+
+    ``head_norm``: the RMS norms of q and k are taken per head.
     """
+    def norm(y, gain):
+        return rms_norm_heads(y, gain, heads) if head_norm else rms_norm(y, gain)
+
     p = f"blk{j}."
     d = z.shape[1]
     mod = m6.reshape(6, d) + as64(W[p + "mod"])
@@ -231,13 +244,13 @@ def block_forward(z: np.ndarray, j: int, m6: np.ndarray, ctx_emb: np.ndarray,
     else:
         u = layer_norm(z) * (1.0 + sc1) + sh1
         qkv = linear(u, W[p + "qkv_w"], W[p + "qkv_b"])
-        k = apply_rope(rms_norm(qkv[:, d:2 * d], W[p + "k_gain"]), ang, heads)
+        k = apply_rope(norm(qkv[:, d:2 * d], W[p + "k_gain"]), ang, heads)
         v = qkv[:, 2 * d:]
         if rows is None:
             zr, q_in, ang_q = z, qkv[:, :d], ang
         else:
             zr, q_in, ang_q = z[rows], qkv[rows, :d], ang[rows]
-        q = apply_rope(rms_norm(q_in, W[p + "q_gain"]), ang_q, heads)
+        q = apply_rope(norm(q_in, W[p + "q_gain"]), ang_q, heads)
         o = attention(q, k, v, heads)
         y = linear(o, W[p + "o_w"], W[p + "o_b"])
     zr = zr + g1 * y
@@ -249,8 +262,8 @@ def block_forward(z: np.ndarray, j: int, m6: np.ndarray, ctx_emb: np.ndarray,
         yc = as64(reuse_cross)
     else:
         u = layer_norm(zr) * as64(W[p + "ca_ln_g"]) + as64(W[p + "ca_ln_b"])
-        q = rms_norm(linear(u, W[p + "caq_w"], W[p + "caq_b"]), W[p + "caq_gain"])
-        kc = rms_norm(linear(ctx_emb, W[p + "cak_w"], W[p + "cak_b"]), W[p + "cak_gain"])
+        q = norm(linear(u, W[p + "caq_w"], W[p + "caq_b"]), W[p + "caq_gain"])
+        kc = norm(linear(ctx_emb, W[p + "cak_w"], W[p + "cak_b"]), W[p + "cak_gain"])
         vc = linear(ctx_emb, W[p + "cav_w"], W[p + "cav_b"])
         yc = linear(attention(q, kc, vc, heads), W[p + "cao_w"], W[p + "cao_b"])
     zr = zr + yc
@@ -266,7 +279,7 @@ def block_forward(z: np.ndarray, j: int, m6: np.ndarray, ctx_emb: np.ndarray,
 
 def velocity(x: np.ndarray, t: float, ctx_emb: np.ndarray, W: Dict[str, np.ndarray],
              cfg, last_block_rows: Optional[np.ndarray] = None,
-             attn_io: Optional[Sequence[dict]] = None) -> np.ndarray:
+             attn_io: Optional[Sequence[dict]] = None, head_norm: bool = False) -> np.ndarray:
     """v_theta(x, t, c) for one latent x [C][F][H][W] (float64 result).
 
     ``ctx_emb`` is the text embedding (output of :func:`text_embedding`).
@@ -283,7 +296,7 @@ def velocity(x: np.ndarray, t: float, ctx_emb: np.ndarray, W: Dict[str, np.ndarr
     for j in range(cfg.n_blocks):
         rows = last_block_rows if j == cfg.n_blocks - 1 else None
         z = block_forward(z, j, m, ctx_emb, ang, W, cfg.heads, rows,
-                          None if attn_io is None else attn_io[j])
+                          None if attn_io is None else attn_io[j], head_norm)
     hm = e[None, :] + as64(W["head_mod"])
     sh, sc = hm[0], hm[1]
     y = linear(layer_norm(z) * (1.0 + sc) + sh, W["head_w"], W["head_b"])

@@ -21,6 +21,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcachedse
 CS_OK, CS_E_INVAL, CS_E_NOMEM, CS_E_DEVICE, CS_E_STATE, CS_E_UNSUPPORTED = range(6)
 CS_BF16, CS_FP32 = 0, 1
 CS_CACHE_OFF, CS_CACHE_ADAPTIVE, CS_CACHE_STATIC, CS_CACHE_PAB = 0, 1, 2, 3
+CS_QK_NORM_FULL, CS_QK_NORM_HEAD = 0, 1
+CS_KV_NATIVE, CS_KV_4BIT = 0, 1
 CS_ROPE_PAIRS, CS_ROPE_HALVES = 0, 1
 (CS_K_SELF_ATTN, CS_K_CROSS_ATTN, CS_K_GEMM, CS_K_NORM, CS_K_DECIDE, CS_K_UPDATE, CS_K_SCORE,
  CS_K_OTHER) = range(8)
@@ -91,7 +93,11 @@ def lib() -> C.CDLL:
     sig = {
         "cs_model_weight_count": (i32, [C.POINTER(cs_model_desc), C.POINTER(sz)]),
         "cs_model_init": (i32, [C.POINTER(cs_model_desc), pf, sz, vp, C.POINTER(vp)]),
+        "cs_model_init_norm": (i32, [C.POINTER(cs_model_desc), i32, pf, sz, vp, C.POINTER(vp)]),
         "cs_model_free": (None, [vp]),
+        "cs_context_init": (i32, [vp, pf, pi32, i32, i32, C.POINTER(vp)]),
+        "cs_context_free": (None, [vp]),
+        "cs_velocity_context": (i32, [vp, vp, pf, pi32, i32, f32, pf]),
         "cs_velocity": (i32, [vp, pf, i32, f32, pf, pf]),
         "cs_rollout_init": (i32, [vp, C.POINTER(cs_rollout_desc), pf, pf, pf, C.POINTER(vp)]),
         "cs_rollout_free": (None, [vp]),
@@ -156,6 +162,7 @@ def _ptr(x, numel: Optional[int] = None, dtype: str = "float32", name: str = "bu
 # rollout handle, so that tensor arguments can be checked against the sizes
 # the library will read or write.
 _model_D = {}
+_model_text = {}
 _rollout_model = {}
 
 
@@ -205,16 +212,51 @@ def cs_model_weight_count(desc: cs_model_desc) -> int:
 
 
 def cs_model_init(desc: cs_model_desc, weights, n_weights: int, stream=None) -> int:
+    return cs_model_init_norm(desc, CS_QK_NORM_FULL, weights, n_weights, stream)
+
+
+def cs_model_init_norm(desc: cs_model_desc, qk_norm: int, weights, n_weights: int, stream=None) -> int:
     out = C.c_void_p()
-    _check(lib().cs_model_init(C.byref(desc), _ptr(weights, n_weights, name="weights"), n_weights,
-                               _stream(stream), C.byref(out)))
+    _check(lib().cs_model_init_norm(C.byref(desc), int(qk_norm), _ptr(weights, n_weights, name="weights"), n_weights,
+                                    _stream(stream), C.byref(out)))
     _model_D[out.value] = desc.in_ch * desc.lat_f * desc.lat_h * desc.lat_w
+    _model_text[out.value] = (desc.text_len, desc.text_dim)
     return out.value
 
 
 def cs_model_free(model: int) -> None:
     lib().cs_model_free(model)
     _model_D.pop(model, None)
+    _model_text.pop(model, None)
+
+
+def cs_context_init(model: int, ctx, n_prompts: int, lens: Optional[Sequence[int]] = None,
+                    kv_format: int = CS_KV_NATIVE) -> int:
+    """Context handle of ``n_prompts`` prompts ``ctx`` [n_prompts][text_len][text_dim]; ``lens``: rows of each."""
+    out = C.c_void_p()
+    rows = _model_text.get(model)
+    ln = None if lens is None else np.ascontiguousarray(np.asarray(lens, dtype=np.int32))
+    if ln is not None and ln.size != n_prompts:
+        raise ValueError(f"{ln.size} lengths for {n_prompts} prompts")
+    _check(lib().cs_context_init(model, _ptr(ctx, None if rows is None else n_prompts * rows[0] * rows[1], name="ctx"),
+                                 None if ln is None else ln.ctypes.data_as(C.POINTER(C.c_int32)), int(n_prompts),
+                                 int(kv_format), C.byref(out)))
+    return out.value
+
+
+def cs_context_free(context: int) -> None:
+    lib().cs_context_free(context)
+
+
+def cs_velocity_context(model: int, context: int, x, n: int, t: float, v, prompt: Optional[Sequence[int]] = None) -> None:
+    D = _latent_numel(model)
+    nD = None if D is None else n * D
+    of = None if prompt is None else np.ascontiguousarray(np.asarray(prompt, dtype=np.int32))
+    if of is not None and of.size != n:
+        raise ValueError(f"{of.size} prompts for {n} latents")
+    _check(lib().cs_velocity_context(model, context, _ptr(x, nD, name="x"),
+                                     None if of is None else of.ctypes.data_as(C.POINTER(C.c_int32)), n, float(t),
+                                     _ptr(v, nD, name="v")))
 
 
 def cs_velocity(model: int, x, n: int, t: float, ctx, v) -> None:

@@ -16,6 +16,7 @@
 
 #include "host.hpp"
 #include "kernels.hpp"
+#include "ops.hpp"
 
 using namespace cs;
 
@@ -221,6 +222,7 @@ struct cs_model {
   size_t esz = 2;        // bytes per matrix element
   long d = 0, L = 0, P = 0, D = 0, Lp = 0, Ltp = 0;
   int gf = 0, gh = 0, gw = 0;
+  int qk_norm = CS_QK_NORM_FULL;
   void* arena = nullptr;
   const void *patch_w, *text1_w, *text2_w, *time1_w, *time2_w, *mod_w, *head_w;
   const float *patch_b, *text1_b, *text2_b, *time1_b, *time2_b, *mod_b, *head_mod, *head_b;
@@ -238,6 +240,36 @@ struct cs_model {
     if (arena) hipFree(arena);
     if (rope) hipFree(rope);
     if (cond) hipFree(cond);
+  }
+};
+
+// Projected text of several prompts, rows [blocks][prompt][text_len][d] or 4-bit
+// caches [blocks] of [prompt][heads][text_len].
+struct cs_context {
+  cs_model* model = nullptr;
+  int n_prompts = 0, format = CS_KV_NATIVE;
+  void* arena = nullptr;
+  void *k = nullptr, *v = nullptr;   // native
+  cs_kv4_cache kv4 = {};             // of block 0; the blocks lie one after the other
+  int32_t* lens = nullptr;           // [n_prompts]
+  // grown by cs_velocity_context: the latents' prompts and the attention's workspace
+  int cap = 0;
+  void* call_arena = nullptr;
+  int32_t* prompt = nullptr;
+  void* work = nullptr;
+  std::vector<int32_t> prompt_host;  // what `prompt` holds
+  cs_kv4_cache block_cache(int j) const {
+    cs_kv4_cache c = kv4;
+    const long rows = (long)j * n_prompts * kv4.heads * kv4.cap;
+    c.k_codes += rows * (kv4.head_dim / 2);
+    c.v_codes += rows * (kv4.head_dim / 2);
+    c.k_scales += rows * (kv4.head_dim / 32);
+    c.v_scales += rows * (kv4.head_dim / 32);
+    return c;
+  }
+  ~cs_context() {
+    if (arena) hipFree(arena);
+    if (call_arena) hipFree(call_arena);
   }
 };
 
@@ -362,19 +394,57 @@ static cs_status ctx_alloc(cs_model* m, CtxKV& c, int B) {
 }
 
 // ---------------------------------------------------------- DiT sequence
+// The model's norm of `parts` consecutive d-wide vectors of each row (stride ld) in
+// place, with the rotation where rope is given: parts 2 are q and k.
+template <typename T>
+static hipError_t norm_rows(const cs_model* m, T* x, long rows, long ld, int parts, const float* gain0,
+                            const float* gain1, const float2* rope) {
+  const cs_model_desc& g = m->desc;
+  if (m->qk_norm == CS_QK_NORM_FULL)
+    return rmsnorm_rope<T>(x, rows, ld, (int)m->d, parts, gain0, gain1, rope, (int)m->L, g.head_dim, m->stream);
+  if (rows <= 0) return hipSuccess;
+  QkNormArgs a = {};
+  a.q = a.qo = x;
+  a.k = a.ko = x + m->d;
+  a.q_gain = gain0;
+  a.k_gain = gain1;
+  a.rope = (const float*)rope;
+  a.d.tokens = (int32_t)rows;
+  a.d.heads_q = g.heads;
+  a.d.heads_k = parts == 2 ? g.heads : 0;
+  a.d.head_dim = g.head_dim;
+  a.d.rot_dim = rope ? g.head_dim : 0;
+  a.d.rope_rows = rope ? (int32_t)m->L : 0;
+  a.d.rope_style = CS_ROPE_PAIRS;
+  a.d.eps = 1e-6f;
+  a.d.q_row = a.d.k_row = a.d.qo_row = a.d.ko_row = ld;
+  a.d.q_head = a.d.k_head = a.d.qo_head = a.d.ko_head = g.head_dim;
+  a.d.q_gain_head = a.d.k_gain_head = g.head_dim;
+  return qk_norm_rope<T>(a, m->stream);
+}
+
+// Text embeddings of rows [rows][text_dim]: emb [rows][d] (tmp0, tmp1: work arrays
+// [rows][text_dim] and [rows][d]).
+template <typename T>
+static cs_status embed_text(const cs_model* m, const float* ctx, long rows, T* tmp0, T* tmp1, T* emb) {
+  const cs_model_desc& g = m->desc;
+  hipStream_t st = m->stream;
+  const long d = m->d;
+  HIPC(cast_from_f32<T>(ctx, tmp0, rows * g.text_dim, st));
+  HIPC(gemm_store<T>(tmp0, g.text_dim, (const T*)m->text1_w, (int)rows, (int)d, g.text_dim, m->text1_b, 1, tmp1, d,
+                     st));
+  HIPC(gemm_store<T>(tmp1, d, (const T*)m->text2_w, (int)rows, (int)d, (int)d, m->text2_b, 0, emb, d, st));
+  return CS_OK;
+}
+
 template <typename T>
 static cs_status build_ctx(cs_model* m, CtxKV& c, int b, const float* ctx) {
   const cs_model_desc& g = m->desc;
   hipStream_t st = m->stream;
   const long Lt = g.text_len, d = m->d;
   ProfScope ps(m->prof, CS_K_OTHER, st);
-  T* tmp0 = (T*)c.tmp0;
-  T* tmp1 = (T*)c.tmp1;
   T* emb = (T*)c.emb;
-  HIPC(cast_from_f32<T>(ctx, tmp0, Lt * g.text_dim, st));
-  HIPC(gemm_store<T>(tmp0, g.text_dim, (const T*)m->text1_w, (int)Lt, (int)d, g.text_dim,
-                     m->text1_b, 1, tmp1, d, st));
-  HIPC(gemm_store<T>(tmp1, d, (const T*)m->text2_w, (int)Lt, (int)d, (int)d, m->text2_b, 0, emb, d, st));
+  TRY(embed_text<T>(m, ctx, Lt, (T*)c.tmp0, (T*)c.tmp1, emb));
   // Keys and values of all blocks: one batched product each and one norm pass
   // (a block's product alone is 96 to 288 small tiles: 30 blocks of the 1.3B
   // shape took 0.28 ms of 9.4 us launches for the keys, one launch takes 0.10
@@ -393,10 +463,63 @@ static cs_status build_ctx(cs_model* m, CtxKV& c, int b, const float* ctx) {
                              b0.cak_b + j * bk, bk, K + j * ks, d, ks, st));
     HIPC(gemm_store_t_batch<T>(emb, d, (const T*)b0.cav_w + j * wv, wv, n, (int)Lt, (int)d, (int)d,
                                b0.cav_b + j * bv, bv, VT + j * vs, m->Ltp, vs, st));
-    HIPC(rmsnorm_rope<T>(K + j * ks, Lt, d, (int)d, 1, b0.cak_gain + j * gk, nullptr, nullptr, 1, g.head_dim, st,
-                         {n, ks, gk}));
+    if (m->qk_norm == CS_QK_NORM_FULL)
+      HIPC(rmsnorm_rope<T>(K + j * ks, Lt, d, (int)d, 1, b0.cak_gain + j * gk, nullptr, nullptr, 1, g.head_dim, st,
+                           {n, ks, gk}));
+    for (int i = 0; m->qk_norm == CS_QK_NORM_HEAD && i < n; ++i)
+      HIPC(norm_rows<T>(m, K + (j + i) * ks, Lt, d, 1, b0.cak_gain + (j + i) * gk, nullptr, nullptr));
   }
   return CS_OK;
+}
+
+// Keys and values of every block for a context's prompts (tmp0, tmp1, emb: work
+// arrays of n_prompts * text_len rows).
+template <typename T>
+static cs_status build_context(cs_context* c, const float* ctx, T* tmp0, T* tmp1, T* emb) {
+  cs_model* m = c->model;
+  const cs_model_desc& g = m->desc;
+  hipStream_t st = m->stream;
+  ProfScope ps(m->prof, CS_K_OTHER, st);
+  const long rows = (long)c->n_prompts * g.text_len, d = m->d;
+  TRY(embed_text<T>(m, ctx, rows, tmp0, tmp1, emb));
+  for (int j = 0; j < g.n_blocks; ++j) {
+    const Block& b = m->blocks[j];
+    // in 4 bits the rows pass through the work arrays
+    T* K = c->format == CS_KV_4BIT ? tmp0 : (T*)c->k + j * rows * d;
+    T* V = c->format == CS_KV_4BIT ? tmp1 : (T*)c->v + j * rows * d;
+    HIPC(gemm_store<T>(emb, d, (const T*)b.cak_w, (int)rows, (int)d, (int)d, b.cak_b, 0, K, d, st));
+    HIPC(gemm_store<T>(emb, d, (const T*)b.cav_w, (int)rows, (int)d, (int)d, b.cav_b, 0, V, d, st));
+    HIPC(norm_rows<T>(m, K, rows, d, 1, b.cak_gain, nullptr, nullptr));
+    if (c->format == CS_KV_4BIT) {
+      Kv4RowsArgs a = {};
+      a.c = c->block_cache(j);
+      a.r = {g.dtype, (int32_t)rows, d, g.head_dim, d, g.head_dim};
+      a.k = K;
+      a.v = V;
+      HIPC(kv4_store<T>(a, st));
+    }
+  }
+  return CS_OK;
+}
+
+// Attention of n latents' queries to the prompts of a context, as one operator.
+static XAttnArgs context_attn(const cs_context* c, int j, int n, const void* q, void* o) {
+  const cs_model* m = c->model;
+  const cs_model_desc& g = m->desc;
+  const long d = m->d, L = m->L, kv = (long)g.text_len * d, at = (long)j * c->n_prompts * kv * m->esz;
+  XAttnArgs a = {};
+  a.q = q;
+  a.o = o;
+  a.k = (const char*)c->k + at;
+  a.v = (const char*)c->v + at;
+  a.kv_of = c->prompt;
+  a.kv_len = c->lens;
+  if (c->format == CS_KV_4BIT) a.c = c->block_cache(j);
+  a.d = {g.dtype, n, c->n_prompts, (int32_t)L, g.text_len, g.heads, g.heads, g.head_dim,
+         (float)(1.0 / sqrt((double)g.head_dim)), L * d, d, g.head_dim, kv, d, g.head_dim, kv, d, g.head_dim,
+         L * d, d, g.head_dim, 0};
+  a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)g.head_dim));
+  return a;
 }
 
 // Time conditioning for timestep t: per-block and head modulation.
@@ -422,10 +545,10 @@ struct PabIO {
 };
 
 // One transformer evaluation for n_slots streams.  Stream s reads latent
-// x + (slot_id[s] / cand_div) * D, attends to text branch kv_branch[s], and
-// writes its velocity to vout + slot_id[s] * D.
+// x + (slot_id[s] / cand_div) * D, attends to text branch kv_branch[s] of c, or to its
+// prompt of cx where that is given, and writes its velocity to vout + slot_id[s] * D.
 template <typename T>
-static cs_status dit_forward(cs_model* m, Workspace& w, CtxKV& c, const float* x,
+static cs_status dit_forward(cs_model* m, Workspace& w, const CtxKV* c, const cs_context* cx, const float* x,
                              const int32_t* slot_id, const int32_t* kv_branch, int n_slots,
                              int cand_div, float t, float* vout, const PabIO* pab) {
   const cs_model_desc& g = m->desc;
@@ -467,8 +590,7 @@ static cs_status dit_forward(cs_model* m, Workspace& w, CtxKV& c, const float* x
     { ProfScope ps(pf, CS_K_GEMM, st);
       HIPC(gemm_qkv<T>(U, (const T*)bk.qkv_w, (int)rows, (int)d, bk.qkv_b, (int)L, QK, VT, m->Lp, st)); }
     { ProfScope ps(pf, CS_K_NORM, st);
-      HIPC(rmsnorm_rope<T>(QK, rows, 2 * d, (int)d, 2, bk.q_gain, bk.k_gain, m->rope, (int)L,
-                           g.head_dim, st)); }
+      HIPC(norm_rows<T>(m, QK, rows, 2 * d, 2, bk.q_gain, bk.k_gain, m->rope)); }
     {
       ProfScope ps(pf, CS_K_SELF_ATTN, st);
       AttnArgs<T> a;
@@ -494,13 +616,16 @@ static cs_status dit_forward(cs_model* m, Workspace& w, CtxKV& c, const float* x
     { ProfScope ps(pf, CS_K_GEMM, st);
       HIPC(gemm_store<T>(U, d, (const T*)bk.caq_w, (int)rows, (int)d, (int)d, bk.caq_b, 0, Q2, d, st)); }
     { ProfScope ps(pf, CS_K_NORM, st);
-      HIPC(rmsnorm_rope<T>(Q2, rows, d, (int)d, 1, bk.caq_gain, nullptr, nullptr, (int)L, g.head_dim, st)); }
-    {
+      HIPC(norm_rows<T>(m, Q2, rows, d, 1, bk.caq_gain, nullptr, nullptr)); }
+    if (cx) {
+      ProfScope ps(pf, CS_K_CROSS_ATTN, st);
+      HIPC(xattn<T>(context_attn(cx, j, n_slots, Q2, O), cx->format == CS_KV_4BIT, cx->work, st));
+    } else {
       ProfScope ps(pf, CS_K_CROSS_ATTN, st);
       AttnArgs<T> a;
       a.q = Q2; a.q_ld = d; a.q_ss = L * d;
-      a.k = (const T*)c.k + (long)j * c.B * g.text_len * d; a.k_ld = d; a.k_ss = (long)g.text_len * d;
-      a.vt = (const T*)c.vt + (long)j * c.B * d * m->Ltp; a.vt_ld = m->Ltp; a.vt_ss = d * m->Ltp;
+      a.k = (const T*)c->k + (long)j * c->B * g.text_len * d; a.k_ld = d; a.k_ss = (long)g.text_len * d;
+      a.vt = (const T*)c->vt + (long)j * c->B * d * m->Ltp; a.vt_ld = m->Ltp; a.vt_ss = d * m->Ltp;
       a.kv_sel = kv_branch;
       a.o = O; a.o_ld = d; a.o_ss = L * d;
       a.lq = (int)L; a.lk = g.text_len; a.heads = H; a.n_streams = n_slots; a.scale_log2 = sl2;
@@ -526,12 +651,12 @@ static cs_status dit_forward(cs_model* m, Workspace& w, CtxKV& c, const float* x
   return CS_OK;
 }
 
-static cs_status dit_dispatch(cs_model* m, Workspace& w, CtxKV& c, const float* x,
+static cs_status dit_dispatch(cs_model* m, Workspace& w, const CtxKV* c, const cs_context* cx, const float* x,
                               const int32_t* slot_id, const int32_t* kv_branch, int n_slots,
                               int cand_div, float t, float* vout, const PabIO* pab = nullptr) {
   if (m->desc.dtype == CS_BF16)
-    return dit_forward<bf16>(m, w, c, x, slot_id, kv_branch, n_slots, cand_div, t, vout, pab);
-  return dit_forward<float>(m, w, c, x, slot_id, kv_branch, n_slots, cand_div, t, vout, pab);
+    return dit_forward<bf16>(m, w, c, cx, x, slot_id, kv_branch, n_slots, cand_div, t, vout, pab);
+  return dit_forward<float>(m, w, c, cx, x, slot_id, kv_branch, n_slots, cand_div, t, vout, pab);
 }
 
 static cs_status ctx_dispatch(cs_model* m, CtxKV& c, int b, const float* ctx) {
@@ -583,9 +708,10 @@ cs_status cs_model_weight_count(const cs_model_desc* desc, size_t* count) {
   })
 }
 
-static cs_status model_init_impl(const cs_model_desc* desc, const float* weights, size_t n_weights,
+static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const float* weights, size_t n_weights,
                                  void* stream, cs_model** out) {
   TRY(validate_desc(desc));
+  CHECK(qk_norm == CS_QK_NORM_FULL || qk_norm == CS_QK_NORM_HEAD, CS_E_INVAL, "unknown qk_norm %d", qk_norm);
   CHECK(out, CS_E_INVAL, "out is NULL");
   *out = nullptr;
   CHECK(weights, CS_E_INVAL, "weights is NULL");
@@ -596,6 +722,7 @@ static cs_status model_init_impl(const cs_model_desc* desc, const float* weights
 
   std::unique_ptr<cs_model> m(new cs_model());
   m->desc = *desc;
+  m->qk_norm = qk_norm;
   m->stream = (hipStream_t)stream;
   m->esz = desc->dtype == CS_BF16 ? 2 : 4;
   m->d = desc->hidden;
@@ -721,7 +848,12 @@ static cs_status model_init_impl(const cs_model_desc* desc, const float* weights
 
 cs_status cs_model_init(const cs_model_desc* desc, const float* weights, size_t n_weights,
                         void* stream, cs_model** out) {
-  GUARD({ return model_init_impl(desc, weights, n_weights, stream, out); })
+  GUARD({ return model_init_impl(desc, CS_QK_NORM_FULL, weights, n_weights, stream, out); })
+}
+
+cs_status cs_model_init_norm(const cs_model_desc* desc, int32_t qk_norm, const float* weights, size_t n_weights,
+                             void* stream, cs_model** out) {
+  GUARD({ return model_init_impl(desc, qk_norm, weights, n_weights, stream, out); })
 }
 
 void cs_model_free(cs_model* model) {
@@ -740,7 +872,144 @@ cs_status cs_velocity(cs_model* m, const float* x, int32_t n, float t, const flo
     TRY(ws_alloc(m, m->vel_ws, n));
     TRY(ctx_alloc(m, m->vel_ctx, 1));
     TRY(ctx_dispatch(m, m->vel_ctx, 0, ctx));
-    TRY(dit_dispatch(m, m->vel_ws, m->vel_ctx, x, m->vel_ws.ids, m->vel_ws.zeros, n, 1, t, v));
+    TRY(dit_dispatch(m, m->vel_ws, &m->vel_ctx, nullptr, x, m->vel_ws.ids, m->vel_ws.zeros, n, 1, t, v));
+    return CS_OK;
+  })
+}
+
+static void context_layout(const cs_model* m, cs_context* c, Layout& l) {
+  const cs_model_desc& g = m->desc;
+  const size_t rows = (size_t)g.n_blocks * c->n_prompts * g.text_len;   // of all heads
+  if (c->format == CS_KV_4BIT) {
+    c->kv4.n_kv = c->n_prompts;
+    c->kv4.heads = g.heads;
+    c->kv4.cap = g.text_len;
+    c->kv4.head_dim = g.head_dim;
+    l.take(c->kv4.k_codes, rows * m->d / 2);
+    l.take(c->kv4.v_codes, rows * m->d / 2);
+    l.take(c->kv4.k_scales, rows * m->d / 32);
+    l.take(c->kv4.v_scales, rows * m->d / 32);
+  } else {
+    l.take(c->k, rows * m->d * m->esz);
+    l.take(c->v, rows * m->d * m->esz);
+  }
+  l.take(c->lens, c->n_prompts * sizeof(int32_t));
+}
+
+static cs_status context_init_impl(cs_model* m, const float* ctx, const int32_t* lens, int32_t n, int32_t format,
+                                   cs_context** out) {
+  CHECK(out, CS_E_INVAL, "out is NULL");
+  *out = nullptr;
+  CHECK(m && ctx, CS_E_INVAL, "model and ctx must be non-NULL");
+  CHECK(n >= 1 && n <= 4096, CS_E_INVAL, "n_prompts must be in [1, 4096]");
+  CHECK(format == CS_KV_NATIVE || format == CS_KV_4BIT, CS_E_INVAL, "unknown kv_format %d", format);
+  const cs_model_desc& g = m->desc;
+  std::vector<int32_t> len(n, g.text_len);
+  for (int i = 0; lens && i < n; ++i) {
+    CHECK(lens[i] >= 0 && lens[i] <= g.text_len, CS_E_INVAL, "length %d of prompt %d is not in 0..%d", lens[i], i,
+          g.text_len);
+    len[i] = lens[i];
+  }
+  const long rows = (long)n * g.text_len;
+  CHECK(rows <= (1L << 24), CS_E_UNSUPPORTED, "too many prompt rows");
+  std::unique_ptr<cs_context> c(new cs_context());
+  c->model = m;
+  c->n_prompts = n;
+  c->format = format;
+  Layout l;
+  context_layout(m, c.get(), l);
+  TRY(dmalloc(&c->arena, l.bytes));
+  l = Layout{(char*)c->arena, 0};
+  context_layout(m, c.get(), l);
+  // work arrays, freed again below
+  struct Temp {
+    void* p = nullptr;
+    ~Temp() { if (p) hipFree(p); }
+  } temp;
+  void *tmp0 = nullptr, *tmp1 = nullptr, *emb = nullptr;
+  l = Layout{};
+  for (int pass = 0; pass < 2; ++pass) {
+    l.bytes = 0;
+    l.take(tmp0, rows * std::max<long>(g.text_dim, m->d) * m->esz);
+    l.take(tmp1, rows * m->d * m->esz);
+    l.take(emb, rows * m->d * m->esz);
+    if (pass == 0) {
+      TRY(dmalloc(&temp.p, l.bytes));
+      l.base = (char*)temp.p;
+    }
+  }
+  HIPC(hipMemcpyAsync(c->lens, len.data(), n * sizeof(int32_t), hipMemcpyHostToDevice, m->stream));
+  const cs_status s = g.dtype == CS_BF16
+                          ? build_context<bf16>(c.get(), ctx, (bf16*)tmp0, (bf16*)tmp1, (bf16*)emb)
+                          : build_context<float>(c.get(), ctx, (float*)tmp0, (float*)tmp1, (float*)emb);
+  // whatever was enqueued ends before the work arrays go
+  const hipError_t e = hipStreamSynchronize(m->stream);
+  TRY(s);
+  HIPC(e);
+  *out = c.release();
+  return CS_OK;
+}
+
+cs_status cs_context_init(cs_model* model, const float* ctx, const int32_t* lens, int32_t n_prompts,
+                          int32_t kv_format, cs_context** out) {
+  GUARD({ return context_init_impl(model, ctx, lens, n_prompts, kv_format, out); })
+}
+
+void cs_context_free(cs_context* context) {
+  if (!context) return;
+  hipStreamSynchronize(context->model->stream);
+  delete context;
+}
+
+// The latents' prompts on the device, and a workspace for n of them.
+static cs_status context_prepare(cs_context* c, const int32_t* prompt, int n) {
+  cs_model* m = c->model;
+  std::vector<int32_t> of(n);
+  for (int i = 0; i < n; ++i) of[i] = prompt ? prompt[i] : i;
+  if (c->cap < n) {
+    HIPC(hipStreamSynchronize(m->stream));   // earlier calls may still use the old one
+    if (c->call_arena) hipFree(c->call_arena);
+    c->call_arena = nullptr;
+    c->cap = 0;
+    c->prompt_host.clear();
+    const size_t need = xattn_workspace(context_attn(c, 0, n, nullptr, nullptr).d, c->format == CS_KV_4BIT);
+    Layout l;
+    for (int pass = 0; pass < 2; ++pass) {
+      l.bytes = 0;
+      l.take(c->prompt, n * sizeof(int32_t));
+      l.take(c->work, need);
+      if (pass == 0) {
+        TRY(dmalloc(&c->call_arena, l.bytes));
+        l.base = (char*)c->call_arena;
+      }
+    }
+    c->cap = n;
+  }
+  if (of.size() > c->prompt_host.size() || !std::equal(of.begin(), of.end(), c->prompt_host.begin())) {
+    c->prompt_host.clear();
+    HIPC(hipMemcpyAsync(c->prompt, of.data(), n * sizeof(int32_t), hipMemcpyHostToDevice, m->stream));
+    HIPC(hipStreamSynchronize(m->stream));   // `of` goes
+    c->prompt_host = of;
+  }
+  return CS_OK;
+}
+
+cs_status cs_velocity_context(cs_model* m, cs_context* c, const float* x, const int32_t* prompt, int32_t n, float t,
+                              float* v) {
+  GUARD({
+    CHECK(m && c, CS_E_INVAL, "model and context must be non-NULL");
+    CHECK(c->model == m, CS_E_INVAL, "the context belongs to another model");
+    CHECK(x && v, CS_E_INVAL, "x and v must be non-NULL");
+    CHECK(n >= 1 && n <= 4096, CS_E_INVAL, "n must be in [1, 4096]");
+    CHECK(prompt || n <= c->n_prompts, CS_E_INVAL, "%d latents and %d prompts need prompt", n, c->n_prompts);
+    for (int i = 0; prompt && i < n; ++i)
+      CHECK(prompt[i] >= 0 && prompt[i] < c->n_prompts, CS_E_INVAL, "prompt %d of latent %d is not in 0..%d",
+            prompt[i], i, c->n_prompts - 1);
+    CHECK(isfinite(t), CS_E_INVAL, "t must be finite");
+    CHECK(x != v, CS_E_INVAL, "v may not alias x");
+    TRY(ws_alloc(m, m->vel_ws, n));
+    TRY(context_prepare(c, prompt, n));
+    TRY(dit_dispatch(m, m->vel_ws, nullptr, c, x, m->vel_ws.ids, m->vel_ws.zeros, n, 1, t, v));
     return CS_OK;
   })
 }
@@ -958,13 +1227,13 @@ static cs_status step_impl(cs_rollout* r, int32_t step) {
     const bool cs_ = window || !r->pab_have_self || (step - d.k_warm) % d.pab_self_range == 0;
     const bool cc_ = window || !r->pab_have_cross || (step - d.k_warm) % d.pab_cross_range == 0;
     PabIO io{r->pab_self, r->pab_cross, cs_ ? PAB_STORE : PAB_REUSE, cc_ ? PAB_STORE : PAB_REUSE};
-    TRY(dit_dispatch(m, r->ws, r->ctx, r->x, r->slots, r->branch, r->n_compute, d.n_branch,
+    TRY(dit_dispatch(m, r->ws, &r->ctx, nullptr, r->x, r->slots, r->branch, r->n_compute, d.n_branch,
                      r->t[step - 1], r->vbuf, &io));
     r->pab_have_self = r->pab_have_cross = true;
     if (!cs_) r->self_reused += r->S;
     if (!cc_) r->cross_reused += r->S;
   } else if (r->n_compute > 0) {
-    TRY(dit_dispatch(m, r->ws, r->ctx, r->x, r->slots, r->branch, r->n_compute, d.n_branch,
+    TRY(dit_dispatch(m, r->ws, &r->ctx, nullptr, r->x, r->slots, r->branch, r->n_compute, d.n_branch,
                      r->t[step - 1], r->vbuf));
   }
   {

@@ -25,7 +25,8 @@ def _dev(a: np.ndarray, device: str = "cuda") -> torch.Tensor:
 class GpuModel:
     """A model handle whose weights were uploaded from a flat float32 array."""
 
-    def __init__(self, cfg, weights: np.ndarray, dtype: Optional[int] = None, stream=None):
+    def __init__(self, cfg, weights: np.ndarray, dtype: Optional[int] = None, stream=None,
+                 qk_norm: int = B.CS_QK_NORM_FULL):
         self.cfg = cfg
         self.desc = B.model_desc(cfg, dtype)
         n = B.cs_model_weight_count(self.desc)
@@ -33,7 +34,7 @@ class GpuModel:
             raise ValueError(f"weight array has {weights.size} values, model needs {n}")
         w = _dev(weights)
         self.stream = stream
-        self.h = B.cs_model_init(self.desc, w, n, stream)
+        self.h = B.cs_model_init_norm(self.desc, qk_norm, w, n, stream)
         del w
         torch.cuda.synchronize()
 
@@ -43,10 +44,40 @@ class GpuModel:
         torch.cuda.synchronize()
         return v
 
+    def prompts(self, ctx: torch.Tensor, lens=None, kv_format: int = B.CS_KV_NATIVE) -> "GpuPrompts":
+        """Prompts ctx [n][text_len][text_dim] of lengths ``lens``, projected once."""
+        return GpuPrompts(self, ctx, lens, kv_format)
+
     def close(self):
         if self.h:
             B.cs_model_free(self.h)
             self.h = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GpuPrompts:
+    """The projected text of several prompts of a model (cs_context)."""
+
+    def __init__(self, model: GpuModel, ctx: torch.Tensor, lens=None, kv_format: int = B.CS_KV_NATIVE):
+        self.model = model        # outlives its contexts
+        self.h = B.cs_context_init(model.h, ctx, ctx.shape[0], lens, kv_format)
+
+    def velocity(self, x: torch.Tensor, t: float, prompt=None) -> torch.Tensor:
+        """Velocities of the latents x, latent i attending to prompt[i] (None: prompt i)."""
+        v = torch.empty_like(x)
+        B.cs_velocity_context(self.model.h, self.h, x, x.shape[0], t, v, prompt)
+        torch.cuda.synchronize()
+        return v
+
+    def close(self):
+        if self.h and self.model.h:
+            B.cs_context_free(self.h)
+        self.h = 0
 
     def __del__(self):
         try:

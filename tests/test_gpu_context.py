@@ -1,0 +1,182 @@
+"""Prompts of their own lengths in one batch (cs_context, cs_velocity_context) and the
+per-head norm inside the transformer, against the float64 oracle."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import dit as odit
+from paper_2607_23159_amd import binding as B
+from paper_2607_23159_amd import synth
+from paper_2607_23159_amd.search import GpuModel
+from parity import TOL, rel_l2, token_errors
+import ops_ref as R
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+_made = {}
+
+
+def made(name, dtype, norm):
+    key = (name, dtype, norm)
+    if key not in _made:
+        m = synth.MODELS[name].with_dtype(dtype)
+        flat = synth.make_weights(m, init="stress")
+        W = {k: v.astype(np.float64) for k, v in synth.unflatten(m, flat).items()}
+        _made[key] = (m, GpuModel(m, flat, qk_norm=norm), W)
+    return _made[key]
+
+
+def _prompts(m, n):
+    return np.stack([synth.make_context(m, 40 + i) for i in range(n)])
+
+
+def _embedded(m, ctx, W, length):
+    return odit.text_embedding(ctx[:length], W)
+
+
+@pytest.mark.parametrize("norm", [B.CS_QK_NORM_FULL, B.CS_QK_NORM_HEAD])
+@pytest.mark.parametrize("dtype", [synth.DTYPE_FP32, synth.DTYPE_BF16])
+@pytest.mark.parametrize("name", ["tiny", "ragged"])
+def test_prompts_of_their_own_lengths(name, dtype, norm):
+    """Held to the bars of the method.  A quarter of them, as for the tiny shape, is not to be had in
+    bf16 in general: a block rounds some 20 operands (weights, activations, softmax weights), each
+    off by 2^-9 / sqrt(3) x 0.72 = 0.8e-3 of itself in the mean square; the 48 of two blocks and the
+    ends, with the stress weights all of about the same share, add up to sqrt(48) x 0.8e-3 = 5.6e-3."""
+    m, gm, W = made(name, dtype, norm)
+    Lt = m.text_len
+    lens = [Lt, 0, 1, Lt // 2 + 1]
+    ctx = _prompts(m, 4)
+    dev = torch.from_numpy(ctx).cuda()
+    for i, n in enumerate(lens):
+        dev[i, n:] = float("nan")          # rows past a prompt's length may hold anything
+    ps = gm.prompts(dev, lens)
+    of = [3, 0, 1, 2, 3]
+    x = synth.make_noise(m, len(of), seed0=700)
+    v = ps.velocity(torch.from_numpy(x.reshape(len(of), -1)).cuda(), 0.45, of).cpu().numpy().reshape(x.shape)
+    for i, p in enumerate(of):
+        emb = _embedded(m, ctx[p], W, lens[p])
+        ref = odit.velocity(x[i], 0.45, emb, W, m, head_norm=norm == B.CS_QK_NORM_HEAD)
+        assert rel_l2(v[i], ref) < TOL[dtype], (i, p)
+        assert token_errors(v[i], ref).max() < TOL[dtype], (i, p)
+    # one by one, and in the order of the prompts: bitwise the same
+    xs = torch.from_numpy(x.reshape(len(of), -1)).cuda()
+    for i, p in enumerate(of):
+        assert np.array_equal(ps.velocity(xs[i:i + 1].contiguous(), 0.45, [p]).cpu().numpy().ravel(), v[i].ravel())
+    a = ps.velocity(xs[:4].contiguous(), 0.45)
+    b = ps.velocity(xs[:4].contiguous(), 0.45, [0, 1, 2, 3])
+    assert torch.equal(a, b)
+    ps.close()
+
+
+@pytest.mark.parametrize("dtype", [synth.DTYPE_FP32, synth.DTYPE_BF16])
+def test_head_norm_in_velocity_and_rollout(dtype):
+    """cs_velocity and rollouts of a model with the per-head norm."""
+    m, gm, W = made("tiny", dtype, B.CS_QK_NORM_HEAD)
+    x = synth.make_noise(m, 2, seed0=900)
+    ctx = synth.make_context(m, 1)
+    xs = torch.from_numpy(x.reshape(2, -1)).cuda()
+    dev = torch.from_numpy(ctx).cuda()
+    emb = odit.text_embedding(ctx, W)
+    v = gm.velocity(xs, 1.0, dev).cpu().numpy().reshape(x.shape)
+    for i in range(2):
+        ref = odit.velocity(x[i], 1.0, emb, W, m, head_norm=True)
+        full = odit.velocity(x[i], 1.0, emb, W, m)
+        assert rel_l2(v[i], ref) < TOL[dtype] / 4
+        assert rel_l2(ref, full) > TOL[dtype]          # the choice matters
+    # one Euler step of an uncached rollout is x + (t1 - t0) v
+    ts = np.array([1.0, 0.0], np.float32)
+    r = synth.RolloutCfg(n_cand=2, n_steps=1, k_warm=0, k_cool=0, mode=synth.CACHE_OFF)
+    h = B.cs_rollout_init(gm.h, B.RolloutDesc(r, ts), xs, dev)
+    B.cs_denoise_step(h, 1)
+    lat = torch.empty_like(xs)
+    B.cs_rollout_latents(h, lat)
+    torch.cuda.synchronize()
+    B.cs_rollout_free(h)
+    assert rel_l2(lat.cpu().numpy(), (xs.cpu().numpy().astype(np.float64) - v.reshape(2, -1))) < 1e-6
+
+
+@pytest.mark.parametrize("dtype", [synth.DTYPE_FP32, synth.DTYPE_BF16])
+@pytest.mark.parametrize("name", ["tiny", "ragged"])
+def test_prompts_in_four_bits(name, dtype, monkeypatch):
+    """The oracle with its text keys and values rounded to the cache's grid.  In fp32 the kernels' keys
+    are the oracle's to 1e-6 and round alike but for one in a million.  In bf16 they are off by some
+    2^-7 of themselves against code steps of a sixth of the largest magnitude and up: a few percent
+    round to the neighbouring code, an error like the rounding's own (twelve times the variance of
+    a rounding for each that does), so up to its size is allowed."""
+    m, gm, W = made(name, dtype, B.CS_QK_NORM_FULL)
+    lens = [m.text_len, m.text_len // 3]
+    ctx = _prompts(m, 2)
+    ps = gm.prompts(torch.from_numpy(ctx).cuda(), lens, B.CS_KV_4BIT)
+    x = synth.make_noise(m, 2, seed0=800)
+    v = ps.velocity(torch.from_numpy(x.reshape(2, -1)).cuda(), 0.7).cpu().numpy().reshape(x.shape)
+    plain = odit.attention
+
+    def rounded(q, k, vv, heads):
+        if k.shape[0] == m.tokens:
+            return plain(q, k, vv, heads)
+        dh = k.shape[1] // heads
+        k, vv = (R.dequantise(*R.quantise(torch.from_numpy(y).reshape(-1, heads, dh))).reshape(y.shape).numpy()
+                 for y in (k, vv))
+        return plain(q, k, vv, heads)
+
+    for i in range(2):
+        emb = _embedded(m, ctx[i], W, lens[i])
+        exact = odit.velocity(x[i], 0.7, emb, W, m)
+        monkeypatch.setattr(odit, "attention", rounded)
+        ref = odit.velocity(x[i], 0.7, emb, W, m)
+        monkeypatch.setattr(odit, "attention", plain)
+        off = rel_l2(ref, exact)
+        got = rel_l2(v[i], ref)
+        print(f"4-bit text: {off:.3e} off the exact velocity, kernels {got:.3e} off the rounded one", flush=True)
+        assert got < TOL[dtype] + (off if dtype == synth.DTYPE_BF16 else 0.0)
+        assert rel_l2(v[i], exact) < 2 * off + TOL[dtype]
+    ps.close()
+
+
+def test_refusals_with_live_handles():
+    m, gm, _ = made("tiny", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
+    _, other, _ = made("ragged", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
+    ctx = torch.from_numpy(_prompts(m, 2)).cuda()
+    for bad in (dict(lens=[1, m.text_len + 1]), dict(lens=[-1, 0]), dict(kv_format=2)):
+        with pytest.raises(B.CsError) as e:
+            B.cs_context_init(gm.h, ctx, 2, **bad)
+        assert e.value.status == B.CS_E_INVAL
+    with pytest.raises(ValueError, match="elements"):
+        B.cs_context_init(gm.h, ctx, 3)
+    ps = gm.prompts(ctx, [3, 4])
+    x = torch.from_numpy(synth.make_noise(m, 3).reshape(3, -1)).cuda()
+    v = torch.empty_like(x)
+    for kw in (dict(prompt=[0, 2, 1]), dict(prompt=[0, -1, 1]), dict()):
+        with pytest.raises(B.CsError) as e:
+            B.cs_velocity_context(gm.h, ps.h, x, 3, 0.5, v, **kw)
+        assert e.value.status == B.CS_E_INVAL
+    with pytest.raises(B.CsError) as e:
+        B.lib() and B._check(B.lib().cs_velocity_context(other.h, ps.h, x.data_ptr(), None, 1, 0.5, v.data_ptr()))
+    assert "another model" in str(e.value)
+    B.cs_velocity_context(gm.h, ps.h, x, 3, 0.5, v, [1, 1, 0])
+    torch.cuda.synchronize()
+    assert torch.isfinite(v).all()
+    ps.close()
+
+
+@pytest.mark.parametrize("fmt", [B.CS_KV_NATIVE, B.CS_KV_4BIT])
+def test_context_out_of_memory(fmt):
+    m, gm, _ = made("tiny", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
+    ctx = torch.from_numpy(_prompts(m, 2)).cuda()
+    lib = B.lib()
+    try:
+        lib.cs_debug_set_alloc_cap(4096)
+        with pytest.raises(B.CsError) as e:
+            B.cs_context_init(gm.h, ctx, 2, None, fmt)
+        assert e.value.status == B.CS_E_NOMEM
+    finally:
+        lib.cs_debug_set_alloc_cap(0)
+    gm.prompts(ctx, None, fmt).close()

@@ -170,3 +170,18 @@ def test_binding_refuses_host_tensors_and_other_shapes():
     with pytest.raises(ValueError, match="the descriptor is for"):
         B._same(x, B._sig(x[:1]), "q")
     assert B._same(x, B._sig(x), "q") == x.data_ptr() and B._same(None, None, "q") is None and B._same(16, None, "q") == 16
+
+
+def test_contexts_and_norm_choice_refuse_null_and_unknown():
+    from paper_2607_23159_amd import synth
+    lib = B.lib()
+    out = C.c_void_p()
+    assert lib.cs_context_init(None, P, None, 1, 0, C.byref(out)) == B.CS_E_INVAL
+    assert lib.cs_context_init(None, P, None, 1, 0, None) == B.CS_E_INVAL
+    assert lib.cs_velocity_context(None, None, P, None, 1, 0.5, P + 64) == B.CS_E_INVAL
+    lib.cs_context_free(None)
+    m = synth.MODELS["tiny"]
+    d = B.model_desc(m)
+    assert lib.cs_model_init_norm(C.byref(d), 2, P, synth.weight_count(m), None, C.byref(out)) == B.CS_E_INVAL
+    assert "qk_norm" in B.cs_last_error()
+    assert lib.cs_model_init_norm(C.byref(d), 1, None, synth.weight_count(m), None, C.byref(out)) == B.CS_E_INVAL
