@@ -18,6 +18,9 @@ static void cut(XAttnArgs& a) {
     a.part_keys = (int)std::max<long>(least, round_up(cdiv(a.d.lk, most), 128));
     a.parts = cdiv(a.d.lk, a.part_keys);
   }
+  a.by_group = FastDiv(a.group);
+  a.by_parts = FastDiv(a.parts);
+  a.by_heads = FastDiv(a.d.heads_kv);
 }
 
 struct Work {

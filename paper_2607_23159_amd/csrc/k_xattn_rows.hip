@@ -17,11 +17,6 @@ namespace cs {
 
 CS_DEV f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-CS_DEV bf16x4 lds_read_tr(const char* p) {
-  typedef __attribute__((address_space(3))) bf16x4 lds_t;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t*)p);
-}
-
 // Maximum / sum over lanes l, l ^ 16, l ^ 32, l ^ 48.
 CS_DEV float max_groups16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -41,6 +36,8 @@ template <int NS> CS_DEV void split_bf16(float x, bf16* t) {
   }
 }
 
+typedef __attribute__((address_space(3))) bf16x8 lds_vec8;
+
 // Keys of a tile (bit i: key kv0 + i) that are left: below k1 and not masked.
 template <int KEYS, bool MASK>
 CS_DEV uint64_t tile_bits(const uint8_t* mask, int kv0, int k1, int lane) {
@@ -54,8 +51,8 @@ CS_DEV uint64_t tile_bits(const uint8_t* mask, int kv0, int k1, int lane) {
 }
 
 // V^T operand of 16 channels ct over 32 rows of VRS bytes in LDS.
-template <int VRS> CS_DEV bf16x8 read_values(const char* rows, int lane, int ct) {
-  const char* p = rows + (4 * (lane >> 4) + ((lane & 15) >> 2)) * VRS + ct * 32 + (lane & 3) * 8;
+template <int VRS> CS_DEV bf16x8 read_values(const lds_char* rows, int lane, int ct) {
+  const lds_char* p = rows + (4 * (lane >> 4) + ((lane & 15) >> 2)) * VRS + ct * 32 + (lane & 3) * 8;
   const bf16x4 x = lds_read_tr(p), y = lds_read_tr(p + 16 * VRS);
   return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
 }
@@ -71,12 +68,12 @@ template <int DH, bool MASK> struct TileBf16 {
   long k_r, v_r;
   const uint8_t* mask;
   int k1, lane;
-  char* lds;
+  lds_char* lds;
   bf16x8 kf[2][KS];
   int voff[V_INST];
   uint64_t bits_next;   // keys of the requested tile that are left
 
-  CS_DEV TileBf16(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_, char* lds_)
+  CS_DEV TileBf16(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_, lds_char* lds_)
       : k((const bf16*)a.k + ctx * a.d.k_b + head * a.d.k_h), v((const bf16*)a.v + ctx * a.d.v_b + head * a.d.v_h),
         k_r(a.d.k_r), v_r(a.d.v_r), mask(mask_), k1(k1_), lane(lane_), lds(lds_) {
 #pragma unroll
@@ -104,7 +101,7 @@ template <int DH, bool MASK> struct TileBf16 {
       if constexpr (MASK) {   // rows that the mask leaves out load as zeros: they may hold NaN
         if (!(bits_next >> ((i * 64 + lane) / CV) & 1)) off = 0x7FFFFFF0;
       }
-      buffer_load_lds16(base, bytes, lds + stage * KEYS * VRS + i * 1024, off, 0);
+      load_lds16(base, bytes, lds + stage * KEYS * VRS + i * 1024, off);
     }
   }
   // the requested tile is there: everything in flight was asked for one round ago
@@ -123,12 +120,12 @@ template <int DH, bool MASK> struct TileKv4 {
   const uint8_t *kc, *ks_, *vc, *vs_;
   const uint8_t* mask;
   int k1, lane;
-  char* lds;
+  lds_char* lds;
   uint32_t k[KT][KS], v[KT][KS];
   uint32_t kb[KT], vb[KT];
   uint64_t bits_next;
 
-  CS_DEV TileKv4(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_, char* lds_)
+  CS_DEV TileKv4(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_, lds_char* lds_)
       : mask(mask_), k1(k1_), lane(lane_), lds(lds_) {
     const long at = ((long)ctx * a.c.heads + head) * a.c.cap;
     kc = a.c.k_codes + at * (DH / 2);
@@ -167,10 +164,10 @@ template <int DH, bool MASK> struct TileKv4 {
       // rows that are left out may hold anything: they become zeros
       const bool left = bits >> (16 * kt + (lane & 15)) & 1;
       const float s = kv4_scale(left ? vb[kt] : 127);
-      char* p = lds + (16 * kt + (lane & 15)) * VRS + (lane >> 4) * (DH / 2);
+      lds_char* p = lds + (16 * kt + (lane & 15)) * VRS + (lane >> 4) * (DH / 2);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        *reinterpret_cast<bf16x8*>(p + 16 * ks) = kv4_decode8(left ? v[kt][ks] : 0, s);
+        *(lds_vec8*)(p + 16 * ks) = kv4_decode8(left ? v[kt][ks] : 0, s);
     }
   }
   CS_DEV bf16x8 key(int kt, int ks) const { return kv4_decode8(k[kt][ks], kv4_scale(kb[kt])); }
@@ -229,7 +226,7 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : 2) void k_xattn_rows(XA
     for (int ct = 0; ct < NCT; ++ct) o[rt][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  Tile tile(a, ctx, head, MASK ? a.mask + ctx * a.d.mask_b : nullptr, k1, lane, smem + wave * Tile::LDS);
+  Tile tile(a, ctx, head, MASK ? a.mask + ctx * a.d.mask_b : nullptr, k1, lane, (lds_char*)smem + wave * Tile::LDS);
   const int first = k0 + wave * Tile::KEYS, step = NW * Tile::KEYS;
   if (first < k1) tile.request(first, 0);
   int stage = 0;

@@ -15,76 +15,133 @@
 // that the four land on different banks without padding.
 #include "ops.hpp"
 
+#include <algorithm>
+
 namespace cs {
 
 template <int DH> CS_DEV int vswz(int row) { return DH == 128 ? row & 3 : DH == 64 ? (row >> 1) & 1 : 0; }
 
-CS_DEV bf16x4 tile_read_tr(const char* p) {
-  typedef __attribute__((address_space(3))) bf16x4 lds_t;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t*)p);
-}
+// Waits in a form that the compiler counts: it then knows that the register loads
+// from before have landed, and adds no wait of its own among the direct loads behind.
+CS_DEV void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt 0
+CS_DEV void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }     // lgkmcnt 0
 
-template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * NW, OCC) void k_xattn_tile(XAttnArgs a) {
+// One item of work: 32 NW rows of one part of a problem.
+struct TileItem {
+  int set, head, part, pr, r0, k0, k1;
+  const bf16 *kb, *vb;
+  const uint8_t* mask;
+};
+
+template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * NW, OCC) void k_xattn_tile(XAttnArgs a, FastDiv by_qt, int n_items) {
   typedef Mfma32<bf16> MF;
   typedef MF::frag frag;
-  constexpr int KVT = 64, STAGES = 3;
-  constexpr int CK = DH / 8 + 1, KRS = CK * 16, VRS = DH * 2;
-  constexpr int K_INSTR = KVT * CK / 64, V_INSTR = KVT * DH / 8 / 64;
-  static_assert(K_INSTR * 64 == KVT * CK, "whole 1 KB loads");
+  constexpr int KVT = 64, CK = DH / 8 + 1, KRS = CK * 16, VRS = DH * 2;
+  constexpr int K_INSTR = KVT * CK / 64, V_INSTR = KVT * DH / 8 / 64;   // 1 KB each
+  constexpr int K_NPW = (K_INSTR + NW - 1) / NW, V_NPW = (V_INSTR + NW - 1) / NW;
   constexpr int KB = K_INSTR * 1024, STAGE = KB + V_INSTR * 1024;
-  constexpr int TOT = K_INSTR + V_INSTR, NPW = (TOT + NW - 1) / NW, NBUSY = TOT - (NPW - 1) * NW;
   constexpr int NKT = KVT / 32, NDT = DH / 32, NKS = DH / 16, NPS = 2;
-  __shared__ __attribute__((aligned(1024))) char smem[STAGES * STAGE];
+  // Rows of q and o cross the wave's part of this on their way, 128 bytes of 32 rows at
+  // a time, so that memory sees whole lines (64 bytes with head dim 32, and with four
+  // waves, of which two workgroups share a CU's LDS).
+  constexpr int SEG = DH == 32 || NW == 4 ? 64 : 128, SRS = SEG + 16, NSEG = 2 * DH / SEG, CPS = SEG / 16, RPI = 64 / CPS;
+  constexpr int SI = 32 / RPI;   // instructions of a segment
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE + NW * 32 * SRS];
 
+  lds_char* const lds = (lds_char*)smem;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const int n_qt = (a.rows + NW * 32 - 1) / (NW * 32);
-  int id = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int qt = id % n_qt;
-  id /= n_qt;
-  const int part = id % a.parts, pr = id / a.parts;
-  const int set = pr / a.d.heads_kv, head = pr - set * a.d.heads_kv;
-  int len;
-  const int ctx = xattn_context(a, set, &len);
-  const int k0 = part * a.part_keys, k1 = min(len, k0 + a.part_keys);
-  if (k0 >= k1 && a.parts > 1) return;   // the join does not read it
-  const int r0 = (qt * NW + wave) * 32;
-  const bf16* kb = (const bf16*)a.k + ctx * a.d.k_b + head * a.d.k_h;
-  const bf16* vb = (const bf16*)a.v + ctx * a.d.v_b + head * a.d.v_h;
-  const uint8_t* mask = MASK ? a.mask + ctx * a.d.mask_b : nullptr;
   const int k_r = (int)a.d.k_r, v_r = (int)a.d.v_r;
 
-  // load instruction i of this wave fills slots [64g, 64g + 64) of the stage, g = wave + NW i
-  int voff[NPW];
+  auto row_offset = [&](const TileItem& it, int row, long stride_r, long stride_h) {
+    return xattn_row(a, min(it.r0 + wave * 32 + row, a.rows - 1), it.head, stride_r, stride_h);
+  };
+  // The next item of this workgroup with keys to read, from index i on; items without
+  // any get their zeros (in parts: nothing, the join does not read them).  Rows past
+  // the last are copies of it, here and below: they are stored to the same place.
+  const int per = gridDim.x >> 3, slot = blockIdx.x >> 3, xcd = blockIdx.x & 7;
+  auto find = [&](int& i, TileItem& it) {
+    for (;; ++i) {
+      const int id = (i * 8 + xcd) * per + slot;   // an XCD takes neighbouring items
+      if (id >= n_items) return false;
+      const int n = by_qt.div(id), qt = id - n * by_qt.d;
+      it.pr = a.by_parts.div(n);
+      it.part = n - it.pr * a.parts;
+      it.set = a.by_heads.div(it.pr);
+      it.head = it.pr - it.set * a.d.heads_kv;
+      it.r0 = qt * NW * 32;
+      int len;
+      const int ctx = xattn_context(a, it.set, &len);
+      it.k0 = it.part * a.part_keys;
+      it.k1 = min(len, it.k0 + a.part_keys);
+      it.kb = (const bf16*)a.k + ctx * a.d.k_b + it.head * a.d.k_h;
+      it.vb = (const bf16*)a.v + ctx * a.d.v_b + it.head * a.d.v_h;
+      it.mask = MASK ? a.mask + ctx * a.d.mask_b : nullptr;
+      if (it.k0 < it.k1) return true;
+      if (a.parts == 1) {
+        bf16* dst = (bf16*)a.o + it.set * a.d.o_b + row_offset(it, l32, a.d.o_r, a.d.o_h) + 8 * half;
 #pragma unroll
-  for (int i = 0; i < NPW; ++i) {
-    const int g = wave + NW * i;
-    if (g < K_INSTR) {
-      const int p = g * 64 + lane, row = p / CK, ch = p % CK;
-      voff[i] = ch < CK - 1 ? (row * k_r + ch * 8) * 2 : 0x7FFFFFF0;   // the padding loads nothing
-    } else {
-      const int p = (g - K_INSTR) * 64 + lane, row = p / (DH / 8), ch = p % (DH / 8);
-      voff[i] = (row * v_r + (ch ^ (vswz<DH>(row) << 2)) * 8) * 2;
-    }
-  }
-  const bool busy = wave < NBUSY;
-  auto issue = [&](int tile, int st) {
-    const int kv0 = k0 + tile * KVT, last = min(KVT, k1 - kv0) - 1;   // keys past k1 load as zeros
-    const bf16* kt = kb + (long)kv0 * k_r;
-    const bf16* vt = vb + (long)kv0 * v_r;
-    char* base = smem + st * STAGE;
-#pragma unroll
-    for (int i = 0; i < NPW; ++i) {
-      const int g = wave + NW * i;
-      if (i < NPW - 1 || busy) {
-        if (g < K_INSTR)
-          buffer_load_lds16(kt, (last * k_r + DH) * 2, base + g * 1024, voff[i], 0);
-        else
-          buffer_load_lds16(vt, (last * v_r + DH) * 2, base + g * 1024, voff[i], 0);
+        for (int c = 0; c < DH; c += 16) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
       }
     }
   };
+
+  // load instruction i of this wave fills slots [64g, 64g + 64) of a tile, g = wave + NW i
+  int koff[K_NPW], voff[V_NPW];
+#pragma unroll
+  for (int i = 0; i < K_NPW; ++i) {
+    const int p = (wave + NW * i) * 64 + lane, row = p / CK, ch = p % CK;
+    koff[i] = ch < CK - 1 ? (row * k_r + ch * 8) * 2 : 0x7FFFFFF0;   // the padding loads nothing
+  }
+#pragma unroll
+  for (int i = 0; i < V_NPW; ++i) {
+    const int p = (wave + NW * i) * 64 + lane, row = p / (DH / 8), ch = p % (DH / 8);
+    voff[i] = (row * v_r + (ch ^ (vswz<DH>(row) << 2)) * 8) * 2;
+  }
+  auto issue = [&](const bf16* kb, const bf16* vb, int kv0, int k1, int st) {
+    const int last = min(KVT, k1 - kv0) - 1;   // keys past k1 load as zeros
+    const bf16 *ks = kb + (long)kv0 * k_r, *vs = vb + (long)kv0 * v_r;
+    lds_char* base = lds + st * STAGE + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < K_NPW; ++i)
+      if ((i + 1) * NW <= K_INSTR || wave + NW * i < K_INSTR)
+        load_lds16(ks, (last * k_r + DH) * 2, base + NW * i * 1024, koff[i]);
+#pragma unroll
+    for (int i = 0; i < V_NPW; ++i)
+      if ((i + 1) * NW <= V_INSTR || wave + NW * i < V_INSTR)
+        load_lds16(vs, (last * v_r + DH) * 2, base + KB + NW * i * 1024, voff[i]);
+  };
+  char* const seg = smem + 2 * STAGE + wave * 32 * SRS;
+  static_assert(NSEG * SI == NKS, "as many operands as loads");
+  frag qf[NKS];   // between load_q and turn_q: the rows as they come from memory
+  auto load_q = [&](const TileItem& it) {
+    const bf16* src = (const bf16*)a.q + it.set * a.d.q_b + 8 * (lane % CPS);
+#pragma unroll
+    for (int i = 0; i < SI; ++i) {
+      const bf16* p = src + row_offset(it, i * RPI + lane / CPS, a.d.q_r, a.d.q_h);
+#pragma unroll
+      for (int s = 0; s < NSEG; ++s) qf[s * SI + i] = MF::load(p + s * (SEG / 2));
+    }
+  };
+  auto turn_q = [&]() {   // to operands: lane row l32, channels 16 ks + 8 half
+#pragma unroll
+    for (int s = 0; s < NSEG; ++s) {
+#pragma unroll
+      for (int i = 0; i < SI; ++i)
+        *reinterpret_cast<frag*>(seg + (i * RPI + lane / CPS) * SRS + 16 * (lane % CPS)) = qf[s * SI + i];
+#pragma unroll
+      for (int ks = 0; ks < SI; ++ks)
+        qf[s * SI + ks] = *reinterpret_cast<const frag*>(seg + l32 * SRS + 32 * ks + 16 * half);
+    }
+  };
+
+  TileItem cur, nxt;
+  int i = 0;
+  if (!find(i, cur)) return;
+  issue(cur.kb, cur.vb, cur.k0, cur.k1, 0);
+  load_q(cur);
+  bool more = find(++i, nxt);
 
   f32x16 o[NDT];
 #pragma unroll
@@ -92,21 +149,6 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
   float m_run = -INFINITY, l_run = 0.0f;
-
-  const int ntiles = k1 > k0 ? (k1 - k0 + KVT - 1) / KVT : 0;
-  if (ntiles > 0) issue(0, 0);
-  frag qf[NKS];
-  {
-    const int r = min(r0 + l32, a.rows - 1);
-    const bf16* src = (const bf16*)a.q + set * a.d.q_b + xattn_row(a, r, head, a.d.q_r, a.d.q_h) + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) qf[ks] = MF::load(src + ks * 16);
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ks]));
-  }
-#pragma unroll
-  for (int t = 1; t < STAGES - 1; ++t)
-    if (t < ntiles) issue(t, t);
 
   const int lane_k = l32 * KRS + half * 16;
   // transposing reads: 16 lanes address four rows of 32 bytes; of the two groups of a
@@ -118,25 +160,28 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
     lane_v[dt] = KB + vrow * VRS + (dt ^ vswz<DH>(vrow)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
 
-  for (int t = 0; t < ntiles; ++t) {
-    // tile t has landed once only the next one is in flight; past the barrier every
-    // wave has read tile t - 1, whose stage the load below refills
-    if (t + 1 < ntiles) {
-      if (busy) wait_all_barrier<NPW>();
-      else wait_all_barrier<NPW - 1>();
-    } else {
-      wait_all_barrier<0>();
-    }
-    if (t + STAGES - 1 < ntiles) issue(t + STAGES - 1, (t + STAGES - 1) % STAGES);
-    const char* pk = smem + (t % STAGES) * STAGE + lane_k;
-    const char* pv = smem + (t % STAGES) * STAGE;
-    const int kv0 = k0 + t * KVT;
+  // The tiles of all items in one stream: the next item's first tile and its queries
+  // are on their way while this one's last tile is worked on, and its output drains
+  // under the next one's.
+  int kv0 = cur.k0;
+  turn_q();
+  wait_loads();
+  for (int st = 0;; st ^= 1) {
+    // this wave's loads of the tile have landed (wait_loads below); past the barrier
+    // every wave's have, and every wave has read the other stage, which is refilled
+    wait_lds();
+    asm volatile("s_barrier" ::: "memory");
+    const bool last = kv0 + KVT >= cur.k1;
+    if (!last || more)
+      issue(last ? nxt.kb : cur.kb, last ? nxt.vb : cur.vb, last ? nxt.k0 : kv0 + KVT, last ? nxt.k1 : cur.k1, st ^ 1);
+    const char* pk = smem + st * STAGE + lane_k;
+    const lds_char* pv = lds + st * STAGE;
     uint64_t bits = ~0ull;
     if constexpr (MASK) {
       const int key = kv0 + lane;
-      bits = __ballot(key < k1 && mask[min(key, k1 - 1)] != 0);
-    } else if (k1 - kv0 < KVT) {
-      bits = (1ull << (k1 - kv0)) - 1;
+      bits = __ballot(key < cur.k1 && cur.mask[min(key, cur.k1 - 1)] != 0);
+    } else if (cur.k1 - kv0 < KVT) {
+      bits = (1ull << (cur.k1 - kv0)) - 1;
     }
 
     f32x16 sc[NKT];
@@ -144,11 +189,36 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
     for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[kt][r] = 0.0f;
+    // key operands are read four steps ahead of their products, and half of the values
+    // ahead of the softmax: read one at a time they leave the products waiting for LDS
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
         sc[kt] = MF::mma(MF::load(reinterpret_cast<const bf16*>(pk + kt * 32 * KRS + ks * 32)), qf[ks], sc[kt]);
+    constexpr int AHEAD = NKS < 4 ? NKS : 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, NKT * AHEAD, 0);
+#pragma unroll
+    for (int ks = 0; ks < NKS - AHEAD; ++ks) {
+      __builtin_amdgcn_sched_group_barrier(0x008, NKT, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, NKT, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, NKT * AHEAD, 0);
+    union ValueFrag { bf16x4 h[2]; frag f; uint32_t u[4]; };
+    auto value = [&](int kt, int ps, int dt) {
+      const lds_char* p = pv + lane_v[dt] + (kt * 32 + ps * 16) * VRS;
+      ValueFrag v;
+      v.h[0] = lds_read_tr(p);
+      v.h[1] = lds_read_tr(p + 8 * VRS);
+      return v;
+    };
+    ValueFrag vf[NPS][NDT];
+#pragma unroll
+    for (int ps = 0; ps < NPS; ++ps)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) vf[ps][dt] = value(0, ps, dt);
+    asm volatile("" ::: "memory");
+    if (last && more) load_q(nxt);
     if (bits != ~0ull) {
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
@@ -177,15 +247,13 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
     const float m_use = m_run == -INFINITY ? 0.0f : m_run;
     float lsum = 0.0f;
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) {
-      float p[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(sc[kt][r], a.scale_log2, -m_use));
+    for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int ps = 0; ps < NPS; ++ps) {
         frag f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (bf16)p[ps * 8 + i];
+        for (int i = 0; i < 8; ++i)
+          f[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(sc[kt][ps * 8 + i], a.scale_log2, -m_use));
         pf[kt][ps] = f;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -193,7 +261,6 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
           lsum = __builtin_amdgcn_fdot2_f32_bf16(pr2, one, lsum, false);
         }
       }
-    }
     l_run += lsum;
 
 #pragma unroll
@@ -202,10 +269,7 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
       for (int ps = 0; ps < NPS; ++ps)
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
-          const char* p = pv + lane_v[dt] + (kt * 32 + ps * 16) * VRS;
-          union { bf16x4 h[2]; frag f; uint32_t u[4]; } v;
-          v.h[0] = tile_read_tr(p);
-          v.h[1] = tile_read_tr(p + 8 * VRS);
+          ValueFrag v = kt == 0 ? vf[ps][dt] : value(kt, ps, dt);
           if constexpr (MASK) {
             if (bits != ~0ull) {   // rows that are left out may hold NaN: zeros
               const uint32_t b = (uint32_t)(bits >> (kt * 32 + ps * 16 + 4 * half));
@@ -218,13 +282,18 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
           }
           o[dt] = MF::mma(v.f, pf[kt][ps], o[dt]);
         }
-  }
+    if (!last) {
+      kv0 += KVT;
+      wait_loads();
+      continue;
+    }
 
-  const float l_tot = l_run + __shfl_xor(l_run, 32, WAVE);
-  const int r = r0 + l32;
-  if (a.parts > 1) {
-    if (r < a.rows) {
-      const long at = ((long)pr * a.parts + part) * a.rows + r;
+    // the next item's first tile and queries were asked for a round ago; the stores
+    // behind this wait then drain under its work
+    wait_loads();
+    const float l_tot = l_run + __shfl_xor(l_run, 32, WAVE);
+    if (a.parts > 1) {
+      const long at = ((long)cur.pr * a.parts + cur.part) * a.rows + min(cur.r0 + wave * 32 + l32, a.rows - 1);
       float* dst = a.part_o + at * DH + 4 * half;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
@@ -233,28 +302,69 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
           *reinterpret_cast<f32x4*>(dst + dt * 32 + 8 * g) =
               f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
       if (half == 0) a.part_ml[at] = make_float2(m_run, l_tot);
+    } else {
+      const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;
+      bf16* dst = (bf16*)a.o + cur.set * a.d.o_b + 8 * (lane % CPS);
+      constexpr int DPS = NDT / NSEG;   // 32-channel blocks of a segment
+#pragma unroll
+      for (int s = 0; s < NSEG; ++s) {
+        f32x16 os[DPS];
+#pragma unroll
+        for (int d = 0; d < DPS; ++d) os[d] = o[s * DPS + d];
+        store_o_rows(os, inv, reinterpret_cast<bf16*>(seg + l32 * SRS), half, true);
+#pragma unroll
+        for (int i = 0; i < SI; ++i) {
+          const int row = i * RPI + lane / CPS;
+          *reinterpret_cast<frag*>(dst + row_offset(cur, row, a.d.o_r, a.d.o_h) + s * (SEG / 2)) =
+              *reinterpret_cast<const frag*>(seg + row * SRS + 16 * (lane % CPS));
+        }
+      }
     }
-    return;
+    if (!more) return;
+    turn_q();
+    cur = nxt;
+    more = find(++i, nxt);
+    kv0 = cur.k0;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
+    m_run = -INFINITY;
+    l_run = 0.0f;
   }
-  bf16* dst = (bf16*)a.o + set * a.d.o_b + xattn_row(a, min(r, a.rows - 1), head, a.d.o_r, a.d.o_h);
-  store_o_rows(o, l_tot != 0.0f ? 1.0f / l_tot : 0.0f, dst, half, r < a.rows);
 }
 
-template <int DH, int NW, int OCC> static hipError_t launch_nw(const XAttnArgs& a, hipStream_t st) {
-  const long blocks = (long)a.d.n_q * a.d.heads_kv * a.parts * cdiv(a.rows, NW * 32);
-  if (blocks * 64 * NW > 0xFFFFFFFFL) return hipErrorInvalidConfiguration;
+// Items go round the workgroups that fill the chip's 256 CUs: one of 8 waves each, or
+// two of 4.
+template <int DH, int NW> static hipError_t launch_nw(const XAttnArgs& a, hipStream_t st) {
+  const long items = (long)a.d.n_q * a.d.heads_kv * a.parts * cdiv(a.rows, NW * 32);
+  if (items > 0x3FFFFFFFL) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)std::min<long>(round_up(items, 8), 256 * (8 / NW))), block(64 * NW);
+  const FastDiv by_qt(cdiv(a.rows, NW * 32));
   if (a.mask)
-    hipLaunchKernelGGL((k_xattn_tile<DH, NW, OCC, true>), dim3((unsigned)blocks), dim3(64 * NW), 0, st, a);
+    hipLaunchKernelGGL((k_xattn_tile<DH, NW, 2, true>), grid, block, 0, st, a, by_qt, (int)items);
   else
-    hipLaunchKernelGGL((k_xattn_tile<DH, NW, OCC, false>), dim3((unsigned)blocks), dim3(64 * NW), 0, st, a);
+    hipLaunchKernelGGL((k_xattn_tile<DH, NW, 2, false>), grid, block, 0, st, a, by_qt, (int)items);
   return hipGetLastError();
+}
+
+// 8 waves share a tile of keys between twice the rows, which a full chip runs 7%
+// faster (8 sets of 32,760 queries, 512 keys, 12 heads of 128: 0.96 against 1.03 ms; 4 x
+// 1,560: 39.2 against 40.7 us); 4 waves fill it sooner and leave smaller last rounds
+// (1 x 1,560: 14.3 against 17.6 us; 4 x 384, 40 heads: 24.1 against 38.5).  A wave's
+// arithmetic is the same in both, so results are bitwise equal.
+template <int DH> static hipError_t launch_dh(const XAttnArgs& a, hipStream_t st) {
+  const long pr = (long)a.d.n_q * a.d.heads_kv * a.parts;
+  const long i8 = pr * cdiv(a.rows, 256), i4 = pr * cdiv(a.rows, 128);
+  const double t8 = (double)cdiv(i8, 256), t4 = i4 <= 256 ? 0.82 : 1.07 * cdiv(i4, 512);
+  return t4 < t8 ? launch_nw<DH, 4>(a, st) : launch_nw<DH, 8>(a, st);
 }
 
 hipError_t xattn_tile(const XAttnArgs& a, hipStream_t st) {
   switch (a.d.head_dim) {
-    case 128: return launch_nw<128, 8, 2>(a, st);
-    case 64: return launch_nw<64, 8, 2>(a, st);
-    case 32: return launch_nw<32, 8, 2>(a, st);
+    case 128: return launch_dh<128>(a, st);
+    case 64: return launch_dh<64>(a, st);
+    case 32: return launch_dh<32>(a, st);
     default: return hipErrorInvalidValue;
   }
 }

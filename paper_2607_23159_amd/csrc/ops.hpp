@@ -27,6 +27,18 @@ struct Kv4RowsArgs {
 template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
 template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);
 
+// Division by d of numbers below 2^31: with 2^s >= d, the quotient is (umulhi(n, m) +
+// n) >> s for m = ceil(2^32 (2^s - d) / d), rounded up past exact values.
+struct FastDiv {
+  uint32_t d, m, s;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t d_) : d(d_), m(0), s(0) {
+    while ((1ull << s) < d) ++s;
+    m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
+  }
+  CS_DEV int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+};
+
 // ---- attention to contexts (k_xattn*.hip)
 // The queries of a set that share a key head are the rows of one problem: row r is
 // query r / group, head (key head) * group + r % group.
@@ -39,6 +51,7 @@ struct XAttnArgs {
   cs_attn_desc d;
   float scale_log2;      // log2(e) * scale
   int rows, group;       // lq * group, heads_q / heads_kv
+  FastDiv by_group, by_parts, by_heads;   // group, parts, heads_kv
   // Long contexts: part p of a problem takes keys [p * part_keys, (p + 1) *
   // part_keys) and leaves its outputs relative to its maximum m and its sums l:
   // part_o [problem][part][rows][head_dim], part_ml [problem][part][rows] (m, l).
@@ -57,21 +70,50 @@ template <typename T> hipError_t xattn_rows(const XAttnArgs& a, bool kv4, hipStr
 hipError_t xattn_tile(const XAttnArgs& a, hipStream_t st);
 hipError_t xattn_f32(const XAttnArgs& a, hipStream_t st);
 
-// Keys of the context of query set i, and the context's index (0 keys if kv_of is out of range).
+// Keys of the context of query set i, and the context's index (0 keys if kv_of is out
+// of range).  i is wave-uniform; the index tensors are only read by these kernels, so
+// they are read through the scalar cache.
 CS_DEV int xattn_context(const XAttnArgs& a, int i, int* len) {
-  const int j = a.kv_of ? a.kv_of[i] : i;
+  typedef const __attribute__((address_space(4))) int const_int;
+  const int j = a.kv_of ? ((const_int*)a.kv_of)[i] : i;
   if (j < 0 || j >= a.d.n_kv) {
     *len = 0;
     return 0;
   }
-  *len = a.kv_len ? max(0, min(a.kv_len[j], a.d.lk)) : a.d.lk;
+  *len = a.kv_len ? max(0, min(((const_int*)a.kv_len)[j], a.d.lk)) : a.d.lk;
   return j;
 }
 
-// Offset of row r of problem (set, key head) in q or o.
+// LDS by its own address (a generic pointer's conversion checks for null).
+typedef __attribute__((address_space(3))) char lds_char;
+
+// The direct load of buffer_load_lds16 as an instruction the compiler does not
+// count.  It makes every transposing LDS read wait for all direct loads that it
+// knows of, the next tiles' among them; here the kernels' own waits say which tile
+// has to be there.  (No register is written, and the operands are read at issue.)
+// base and bytes are wave-uniform.
+CS_DEV void load_lds16(const void* base, int bytes, lds_char* lds, int voff) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const uint64_t b = (uint64_t)base;
+  const i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32)) & 0xFFFF,
+                      __builtin_amdgcn_readfirstlane(bytes), 0x00020000};
+  const int at = __builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(voff), "s"(rsrc)
+               : "memory", "m0");
+}
+
+// Transposing read: of the 4 rows of 16 values that 16 lanes address (8 bytes each,
+// lane i row i / 4), lane i gets column i.
+CS_DEV bf16x4 lds_read_tr(const lds_char* p) {
+  typedef __attribute__((address_space(3))) bf16x4 lds_t;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t*)p);
+}
+
+// Offset of row r of problem (set, key head) in q or o (strides below 2^31).
 CS_DEV long xattn_row(const XAttnArgs& a, int r, int head, long stride_r, long stride_h) {
-  const int t = r / a.group;
-  return t * stride_r + ((long)head * a.group + (r - t * a.group)) * stride_h;
+  if (a.group == 1) return (long)r * (int)stride_r + (long)head * (int)stride_h;
+  const int t = a.by_group.div(r);
+  return (long)t * (int)stride_r + (long)(head * a.group + (r - t * a.group)) * (int)stride_h;
 }
 
 // ---- 4-bit values: e2m1 codes and their scale bytes.
