@@ -8,16 +8,15 @@ namespace cs {
 
 // A problem's keys are cut into parts by its own sizes, never by the batch, so that
 // results do not depend on it.
-static void cut(XAttnArgs& a) {
+static void cut(XAttnArgs& a, bool kv4) {
   a.group = a.d.heads_q / a.d.heads_kv;
   a.rows = a.d.lq * a.group;
   a.parts = 1;
-  a.part_keys = a.d.lk;
-  const int least = 512, most = 128;   // keys of a part, parts
-  if (a.rows <= 1024 && a.d.lk > least) {
-    a.part_keys = (int)std::max<long>(least, round_up(cdiv(a.d.lk, most), 128));
-    a.parts = cdiv(a.d.lk, a.part_keys);
-  }
+  // Keys of a full context's part: half as many bytes again in 4 bits (16 contexts of up
+  // to 32,768 rows: 512 keys 72.7 us, 1,024 66.6, 2,048 82.6; bf16, 8 of up to 8,192: 256
+  // keys 35.3, 512 34.2, 1,024 35.8).
+  const int keys = kv4 ? 1024 : 512, most = 128;
+  if (a.rows <= 1024 && a.d.lk > keys) a.parts = std::min(most, cdiv(a.d.lk, keys));
   a.by_group = FastDiv(a.group);
   a.by_parts = FastDiv(a.parts);
   a.by_heads = FastDiv(a.d.heads_kv);
@@ -50,7 +49,7 @@ static Work layout(const XAttnArgs& a, bool kv4) {
 size_t xattn_workspace(const cs_attn_desc& d, bool kv4) {
   XAttnArgs a = {};
   a.d = d;
-  cut(a);
+  cut(a, kv4);
   return layout(a, kv4).bytes;
 }
 
@@ -65,7 +64,7 @@ template <typename T, int DH> __global__ __launch_bounds__(1024) void k_xattn_jo
   const int set = (int)(pr / a.d.heads_kv), head = (int)(pr - (long)set * a.d.heads_kv);
   int len;
   xattn_context(a, set, &len);
-  const int n = (len + a.part_keys - 1) / a.part_keys;
+  const int pk = xattn_part(a, len), n = len > 0 ? (len + pk - 1) / pk : 0;
   const long base = pr * a.parts * a.rows + r;
   constexpr int NC = (DH + 63) / 64;
   float o[MAXP / NW][NC];
@@ -133,7 +132,7 @@ template <typename T> static hipError_t join(const XAttnArgs& a, hipStream_t st)
 }
 
 template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStream_t st) {
-  cut(a);
+  cut(a, kv4);
   const Work w = layout(a, kv4);
   a.part_o = (float*)((char*)work + w.part_o);
   a.part_ml = (float2*)((char*)work + w.part_ml);

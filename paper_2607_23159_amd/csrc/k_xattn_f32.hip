@@ -29,7 +29,7 @@ template <int DH, bool MASK> __global__ __launch_bounds__(256, 1) void k_xattn_f
   const int set = pr / a.d.heads_kv, head = pr - set * a.d.heads_kv;
   int len;
   const int ctx = xattn_context(a, set, &len);
-  const int k0 = part * a.part_keys, k1 = min(len, k0 + a.part_keys);
+  const int pk = xattn_part(a, len), k0 = part * pk, k1 = min(len, k0 + pk);
   if (k0 >= k1 && a.parts > 1) return;   // the join does not read it
   const int r0 = qt * 32;
 

@@ -37,6 +37,8 @@ template <int NS> CS_DEV void split_bf16(float x, bf16* t) {
 }
 
 typedef __attribute__((address_space(3))) bf16x8 lds_vec8;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // Keys of a tile (bit i: key kv0 + i) that are left: below k1 and not masked.
 template <int KEYS, bool MASK>
@@ -50,83 +52,90 @@ CS_DEV uint64_t tile_bits(const uint8_t* mask, int kv0, int k1, int lane) {
   }
 }
 
-// V^T operand of 16 channels ct over 32 rows of VRS bytes in LDS.
-template <int VRS> CS_DEV bf16x8 read_values(const lds_char* rows, int lane, int ct) {
-  const lds_char* p = rows + (4 * (lane >> 4) + ((lane & 15) >> 2)) * VRS + ct * 32 + (lane & 3) * 8;
-  const bf16x4 x = lds_read_tr(p), y = lds_read_tr(p + 16 * VRS);
-  return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-}
+// Values of a tile in LDS: rows of DH bf16, whose 16-byte chunks are permuted by the
+// row (chunk c of row r at c ^ swz(r)): 16 rows' writes of one chunk, and 8 rows'
+// reads of two, meet every bank once.
+template <int DH> struct ValueRows {
+  static constexpr int NC = DH / 8, BYTES = 2 * DH, PER256 = DH == 128 ? 0 : DH == 64 ? 1 : 2;   // log2 rows in 256 bytes
+  static CS_DEV int swz(int r) { return 2 * ((r >> PER256) & (NC / 2 - 1)) | ((r >> 3) & 1); }
+  static CS_DEV void put(lds_char* rows, int r, int chunk, bf16x8 v) {
+    *(lds_vec8*)(rows + r * BYTES + 16 * (chunk ^ swz(r))) = v;
+  }
+  // V^T operand of 16 channels ct over the 32 rows from `rows` on
+  static CS_DEV bf16x8 operand(const lds_char* rows, int lane, int ct) {
+    const int r = 4 * (lane >> 4) + ((lane & 15) >> 2);
+    const lds_char* p = rows + r * BYTES + 16 * ((2 * ct + ((lane >> 1) & 1)) ^ swz(r)) + 8 * (lane & 1);
+    const bf16x4 x = lds_read_tr(p), y = lds_read_tr(p + 16 * BYTES);   // row + 16 is permuted alike
+    return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  }
+};
 
-// Key tile of 32 keys in bf16: fragments straight from memory, the values through a
-// ring of two LDS stages filled by direct loads.
+// A tile of 32 keys on its way through the registers of a wave.  Lane l: keys l % 16 and
+// 16 + l % 16, every fourth chunk of a row.  Whole tiles are read at constant offsets
+// from a uniform address.  Each row is read once: the loads are marked as streaming
+// (2 GB: 7.0 TB/s against 6.2).
 template <int DH, bool MASK> struct TileBf16 {
-  static constexpr int H = 1, KEYS = 32 * H, KS = DH / 32, VRS = 2 * DH + 32;   // padded rows: conflict-free reads
-  static constexpr int LDS = 2 * KEYS * VRS;                         // bytes per wave
-  static constexpr int CV = VRS / 16, V_INST = KEYS * CV / 64;
-  static_assert(V_INST * 64 == KEYS * CV, "whole 1 KB loads");
-  const bf16 *k, *v;
-  long k_r, v_r;
+  static constexpr int KEYS = 32, KS = DH / 32, NC = DH / 8, WAVES = 2;
+  const char *kp, *vp;   // row k0
+  int k_b, v_b;          // bytes from row to row
   const uint8_t* mask;
-  int k1, lane;
-  lds_char* lds;
-  bf16x8 kf[2][KS];
-  int voff[V_INST];
-  uint64_t bits_next;   // keys of the requested tile that are left
+  int k0, k1, lane, koff;
+  bf16x8 k[2][KS], v[2][KS];
+  uint64_t bits;
 
-  CS_DEV TileBf16(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_, lds_char* lds_)
-      : k((const bf16*)a.k + ctx * a.d.k_b + head * a.d.k_h), v((const bf16*)a.v + ctx * a.d.v_b + head * a.d.v_h),
-        k_r(a.d.k_r), v_r(a.d.v_r), mask(mask_), k1(k1_), lane(lane_), lds(lds_) {
-#pragma unroll
-    for (int i = 0; i < V_INST; ++i) {
-      const int p = i * 64 + lane, row = p / CV, ch = p % CV;
-      // the padding slots' offset lies past every range: they load nothing
-      voff[i] = ch < DH / 8 ? (row * (int)v_r + ch * 8) * 2 : 0x7FFFFFF0;
-    }
+  CS_DEV TileBf16(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k0_, int k1_, int lane_)
+      : k_b(2 * (int)a.d.k_r), v_b(2 * (int)a.d.v_r), mask(mask_), k0(k0_), k1(k1_), lane(lane_) {
+    kp = (const char*)((const bf16*)a.k + ctx * a.d.k_b + head * a.d.k_h);
+    vp = (const char*)((const bf16*)a.v + ctx * a.d.v_b + head * a.d.v_h);
+    koff = (lane & 15) * k_b + 16 * (lane >> 4);
   }
-  // channel of element i of step ks in lane group g
+  // channel of element 0 of step ks in lane group g
   static CS_DEV int channel(int ks, int g) { return 32 * ks + 8 * g; }
-  CS_DEV void request(int kv0, int stage) {
-    bits_next = tile_bits<KEYS, MASK>(mask, kv0, k1, lane);
+  static CS_DEV bf16x8 fetch(const char* p) { return *reinterpret_cast<const bf16x8*>(p); }
+  CS_DEV void request(int kv0) {
+    const bool whole = k1 - kv0 >= KEYS;
+    const int last = k1 - 1 - kv0;
+    const char *kt = kp + (long)kv0 * k_b, *vt = vp + (long)kv0 * v_b;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const bf16* src = k + min(kv0 + 16 * kt + (lane & 15), k1 - 1) * k_r + 8 * (lane >> 4);
+    for (int t = 0; t < 2; ++t) {
+      uint32_t ko = koff + 16 * t * k_b;
+      if (!whole) ko = min(16 * t + (lane & 15), last) * k_b + 16 * (lane >> 4);   // past the last: the last again
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *reinterpret_cast<const bf16x8*>(src + 32 * ks);
+      for (int ks = 0; ks < KS; ++ks) k[t][ks] = fetch(kt + ko + 64 * ks);
     }
-    const bf16* base = v + kv0 * v_r;
-    const int bytes = ((min(KEYS, k1 - kv0) - 1) * (int)v_r + DH) * 2;
 #pragma unroll
-    for (int i = 0; i < V_INST; ++i) {
-      int off = voff[i];
-      if constexpr (MASK) {   // rows that the mask leaves out load as zeros: they may hold NaN
-        if (!(bits_next >> ((i * 64 + lane) / CV) & 1)) off = 0x7FFFFFF0;
-      }
-      load_lds16(base, bytes, lds + stage * KEYS * VRS + i * 1024, off);
+    for (int i = 0; i < 2 * KS; ++i) {
+      const uint32_t vo = min(row(i), whole ? KEYS : last) * v_b + 16 * (lane % NC);
+      v[i / KS][i % KS] = fetch(vt + vo);
+    }
+    bits = tile_bits<KEYS, MASK>(mask, kv0, k1, lane);
+  }
+  CS_DEV int row(int i) const { return (64 / NC) * i + lane / NC; }
+  CS_DEV bf16x8 key(int t, int ks) const { return k[t][ks]; }
+  // the values of the tile into LDS, whole rows at a time; those that are left out may
+  // hold anything: they become zeros
+  CS_DEV void stage(lds_char* rows, uint64_t bits, bool some) const {
+#pragma unroll
+    for (int i = 0; i < 2 * KS; ++i) {
+      const bool left = !some || (bits >> row(i) & 1);
+      ValueRows<DH>::put(rows, row(i), lane % NC, left ? v[i / KS][i % KS] : bf16x8{});
     }
   }
-  // the requested tile is there: everything in flight was asked for one round ago
-  CS_DEV void land(int) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-  CS_DEV bf16x8 key(int kt, int ks) const { return kf[kt][ks]; }
-  // V^T operand of 16 channels ct over 32 keys
-  CS_DEV bf16x8 values(int stage, int, int ct) const { return read_values<VRS>(lds + stage * KEYS * VRS, lane, ct); }
 };
 
 // The same of a 4-bit cache.  A lane reads a quarter of a key's codes, which lie
 // together and (from head dim 64 on) under one scale byte; the score product visits
-// the channels in that order.  Values are decoded on their way into LDS.
+// the channels in that order.
 template <int DH, bool MASK> struct TileKv4 {
-  static constexpr int H = 2, KEYS = 32 * H, KT = 2 * H, KS = DH / 32, VRS = 2 * DH + 32;
-  static constexpr int LDS = KEYS * VRS;
-  const uint8_t *kc, *ks_, *vc, *vs_;
+  static constexpr int KEYS = 32, KS = DH / 32, WAVES = 4;
+  const uint8_t *kc, *ks_, *vc, *vs_;   // row 0
   const uint8_t* mask;
-  int k1, lane;
-  lds_char* lds;
-  uint32_t k[KT][KS], v[KT][KS];
-  uint32_t kb[KT], vb[KT];
-  uint64_t bits_next;
+  int k0, k1, lane;
+  uint32_t k[2][KS], v[2][KS], kb[2], vb[2];
+  uint64_t bits;
 
-  CS_DEV TileKv4(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_, lds_char* lds_)
-      : mask(mask_), k1(k1_), lane(lane_), lds(lds_) {
+  CS_DEV TileKv4(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k0_, int k1_, int lane_)
+      : mask(mask_), k0(k0_), k1(k1_), lane(lane_) {
     const long at = ((long)ctx * a.c.heads + head) * a.c.cap;
     kc = a.c.k_codes + at * (DH / 2);
     vc = a.c.v_codes + at * (DH / 2);
@@ -136,50 +145,53 @@ template <int DH, bool MASK> struct TileKv4 {
   static CS_DEV int channel(int ks, int g) { return DH / 4 * g + 8 * ks; }
   static CS_DEV void fetch(const uint8_t* p, uint32_t* d) {
     if constexpr (KS == 4) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p);
-      d[0] = x.x; d[1] = x.y; d[2] = x.z; d[3] = x.w;
+      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+      d[0] = x[0]; d[1] = x[1]; d[2] = x[2]; d[3] = x[3];
     } else if constexpr (KS == 2) {
-      const uint2 x = *reinterpret_cast<const uint2*>(p);
-      d[0] = x.x; d[1] = x.y;
+      const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+      d[0] = x[0]; d[1] = x[1];
     } else {
-      d[0] = *reinterpret_cast<const uint32_t*>(p);
+      d[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
     }
   }
-  CS_DEV void request(int kv0, int) {
+  CS_DEV void request(int kv0) {
+    const bool whole = k1 - kv0 >= KEYS;
+    const uint8_t *kt = kc + (long)kv0 * (DH / 2), *vt = vc + (long)kv0 * (DH / 2);
+    const uint8_t *kst = ks_ + (long)kv0 * (DH / 32), *vst = vs_ + (long)kv0 * (DH / 32);
     const int g = lane >> 4;
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const long key = min(kv0 + 16 * kt + (lane & 15), k1 - 1);
-      fetch(kc + key * (DH / 2) + g * (DH / 8), k[kt]);
-      fetch(vc + key * (DH / 2) + g * (DH / 8), v[kt]);
-      kb[kt] = ks_[key * (DH / 32) + g * DH / 128];
-      vb[kt] = vs_[key * (DH / 32) + g * DH / 128];
+    for (int t = 0; t < 2; ++t) {
+      uint32_t row = 16 * t + (lane & 15);
+      if (!whole) row = min((int)row, k1 - 1 - kv0);
+      fetch(kt + (row * (DH / 2) + g * (DH / 8)), k[t]);
+      fetch(vt + (row * (DH / 2) + g * (DH / 8)), v[t]);
+      kb[t] = kst[row * (DH / 32) + g * DH / 128];
+      vb[t] = vst[row * (DH / 32) + g * DH / 128];
     }
-    bits_next = tile_bits<KEYS, MASK>(mask, kv0, k1, lane);
+    bits = tile_bits<KEYS, MASK>(mask, kv0, k1, lane);
   }
-  CS_DEV void land(int) {
-    const uint64_t bits = bits_next;
+  CS_DEV bf16x8 key(int t, int ks) const { return kv4_decode8(k[t][ks], kv4_scale(kb[t])); }
+  CS_DEV void stage(lds_char* rows, uint64_t bits, bool some) const {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      // rows that are left out may hold anything: they become zeros
-      const bool left = bits >> (16 * kt + (lane & 15)) & 1;
-      const float s = kv4_scale(left ? vb[kt] : 127);
-      lds_char* p = lds + (16 * kt + (lane & 15)) * VRS + (lane >> 4) * (DH / 2);
+    for (int t = 0; t < 2; ++t) {
+      const int row = 16 * t + (lane & 15);
+      const bool left = !some || (bits >> row & 1);
+      const float s = kv4_scale(left ? vb[t] : 127);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        *(lds_vec8*)(p + 16 * ks) = kv4_decode8(left ? v[kt][ks] : 0, s);
+        ValueRows<DH>::put(rows, row, DH / 32 * (lane >> 4) + ks, kv4_decode8(left ? v[t][ks] : 0, s));
     }
   }
-  CS_DEV bf16x8 key(int kt, int ks) const { return kv4_decode8(k[kt][ks], kv4_scale(kb[kt])); }
-  CS_DEV bf16x8 values(int, int half, int ct) const { return read_values<VRS>(lds + half * 32 * VRS, lane, ct); }
 };
 
 // NS: bf16 terms of a query and of a softmax weight (1: bf16; 3: fp32).
 template <typename T, int DH, int RT, int NS, bool MASK, typename Tile>
-__global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : 2) void k_xattn_rows(XAttnArgs a) {
-  constexpr int NW = 4, KS = DH / 32, NCT = DH / 16, OLD = DH + 4, H = Tile::H;
-  constexpr uint64_t FULL = Tile::KEYS == 64 ? ~0ull : (1ull << Tile::KEYS) - 1;
-  constexpr int LDS = Tile::LDS * NW > NW * 16 * OLD * 4 ? Tile::LDS * NW : NW * 16 * OLD * 4;
+__global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_xattn_rows(XAttnArgs a) {
+  typedef ValueRows<DH> Rows;
+  constexpr int NW = 4, KS = DH / 32, NCT = DH / 16, OLD = DH + 4, KEYS = Tile::KEYS;
+  constexpr uint64_t FULL = (1ull << KEYS) - 1;
+  constexpr int WAVE_LDS = KEYS * Rows::BYTES;
+  constexpr int LDS = WAVE_LDS > 16 * OLD * 4 ? WAVE_LDS * NW : 16 * OLD * 4 * NW;
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
   __shared__ float s_m[NW][16 * RT], s_l[NW][16 * RT];
 
@@ -190,7 +202,7 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : 2) void k_xattn_rows(XA
   const int set = pr / a.d.heads_kv, head = pr - set * a.d.heads_kv;
   int len;
   const int ctx = xattn_context(a, set, &len);
-  const int k0 = part * a.part_keys, k1 = min(len, k0 + a.part_keys);
+  const int pk = xattn_part(a, len), k0 = part * pk, k1 = min(len, k0 + pk);
   if (k0 >= k1 && a.parts > 1) return;   // the join does not read it
 
   // Q^T operands
@@ -226,45 +238,49 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : 2) void k_xattn_rows(XA
     for (int ct = 0; ct < NCT; ++ct) o[rt][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  Tile tile(a, ctx, head, MASK ? a.mask + ctx * a.d.mask_b : nullptr, k1, lane, (lds_char*)smem + wave * Tile::LDS);
-  const int first = k0 + wave * Tile::KEYS, step = NW * Tile::KEYS;
-  if (first < k1) tile.request(first, 0);
-  int stage = 0;
-  for (int kv0 = first; kv0 < k1; kv0 += step, stage ^= 1) {
-    tile.land(stage);
-    const uint64_t bits = tile.bits_next;
-    f32x4 sc[2 * H][RT];
+  lds_char* const rows = (lds_char*)smem + wave * WAVE_LDS;
+  Tile tile(a, ctx, head, MASK ? a.mask + ctx * a.d.mask_b : nullptr, k0, k1, lane);
+  const int first = k0 + wave * KEYS, step = NW * KEYS;
+  if (first < k1) tile.request(first);
+  for (int kv0 = first; kv0 < k1; kv0 += step) {
+    // scores, and the values into LDS: the tile's registers are then free for the next
+    const uint64_t bits = tile.bits;
+    f32x4 sc[2][RT];
 #pragma unroll
-    for (int kt = 0; kt < 2 * H; ++kt)
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 kf[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[ks] = tile.key(t, ks);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int n = NS - 1; n >= 0; --n)
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) acc = mma16(tile.key(kt, ks), qf[n][rt][ks], acc);
-        sc[kt][rt] = acc;
+          for (int ks = 0; ks < KS; ++ks) acc = mma16(kf[ks], qf[n][rt][ks], acc);
+        sc[t][rt] = acc;
       }
-    // the other stage's reads are long done; ask for the next tile under the softmax
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (kv0 + step < k1) tile.request(kv0 + step, stage ^ 1);
-    if (bits != FULL) {
+    }
+    const bool some = bits != FULL;
+    tile.stage(rows, bits, some);
+    if (kv0 + step < k1) tile.request(kv0 + step);
+    if (some) {
 #pragma unroll
-      for (int kt = 0; kt < 2 * H; ++kt)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (!(bits >> (16 * kt + 4 * g + j) & 1))
+          if (!(bits >> (16 * t + 4 * g + j) & 1))
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) sc[kt][rt][j] = -INFINITY;
+            for (int rt = 0; rt < RT; ++rt) sc[t][rt][j] = -INFINITY;
     }
-    bf16x8 pf[NS][RT][H];
+    bf16x8 pf[NS][RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int kt = 0; kt < 2 * H; ++kt)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[kt][rt][j]);
+        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[t][rt][j]);
       mx = max_groups16(mx) * a.scale_log2;
       // the maximum moves only when it must: weights up to 2^8 lose nothing in fp32
       if (__any(mx > m_run[rt] + 8.0f)) {
@@ -277,34 +293,33 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : 2) void k_xattn_rows(XA
         for (int ct = 0; ct < NCT; ++ct) o[rt][ct] *= alpha;
       }
       const float m_use = m_run[rt] == -INFINITY ? 0.0f : m_run[rt];
-      float lsum = 0.0f;
+      float p[8], lsum = 0.0f;
 #pragma unroll
-      for (int kt = 0; kt < 2 * H; ++kt)
+      for (int i = 0; i < 8; ++i)
+        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i / 4][rt][i % 4], a.scale_log2, -m_use));
+      // terms of the weights, which are summed as rounded
+      const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[kt][rt][j], a.scale_log2, -m_use));
-          bf16 t[NS];
-          split_bf16<NS>(p, t);
-          float back = 0.0f;
+      for (int n = 0; n < NS; ++n) {
 #pragma unroll
-          for (int n = NS - 1; n >= 0; --n) {
-            pf[n][rt][kt / 2][4 * (kt & 1) + j] = t[n];
-            back += (float)t[n];
-          }
-          lsum += back;   // summed as rounded
-        }
+        for (int i = 0; i < 8; ++i) pf[n][rt][i] = (bf16)p[i];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2)
+          lsum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[n][rt][i], pf[n][rt][i + 1]}, one, lsum, false);
+        if (n + 1 < NS)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] -= (float)pf[n][rt][i];
+      }
       l_run[rt] += lsum;
     }
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+    for (int ct = 0; ct < NCT; ++ct) {
+      const bf16x8 vf = Rows::operand(rows, lane, ct);
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) {
-        const bf16x8 vf = tile.values(stage, h, ct);
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int n = NS - 1; n >= 0; --n) o[rt][ct] = mma16(vf, pf[n][rt][h], o[rt][ct]);
-      }
+        for (int n = NS - 1; n >= 0; --n) o[rt][ct] = mma16(vf, pf[n][rt], o[rt][ct]);
+    }
   }
 
   // join the waves: maxima and sums, then the outputs of one row tile at a time

@@ -73,8 +73,9 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
       it.r0 = qt * NW * 32;
       int len;
       const int ctx = xattn_context(a, it.set, &len);
-      it.k0 = it.part * a.part_keys;
-      it.k1 = min(len, it.k0 + a.part_keys);
+      const int pk = xattn_part(a, len);
+      it.k0 = it.part * pk;
+      it.k1 = min(len, it.k0 + pk);
       it.kb = (const bf16*)a.k + ctx * a.d.k_b + it.head * a.d.k_h;
       it.vb = (const bf16*)a.v + ctx * a.d.v_b + it.head * a.d.v_h;
       it.mask = MASK ? a.mask + ctx * a.d.mask_b : nullptr;

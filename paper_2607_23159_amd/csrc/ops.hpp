@@ -6,6 +6,18 @@
 
 namespace cs {
 
+// Division by d of numbers below 2^31: with 2^s >= d, the quotient is (umulhi(n, m) +
+// n) >> s for m = ceil(2^32 (2^s - d) / d), rounded up past exact values.
+struct FastDiv {
+  uint32_t d, m, s;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t d_) : d(d_), m(0), s(0) {
+    while ((1ull << s) < d) ++s;
+    m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
+  }
+  CS_DEV int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+};
+
 // ---- per-head norms with rotation (k_qk_norm.hip)
 struct QkNormArgs {
   const void *q, *k;
@@ -23,21 +35,10 @@ struct Kv4RowsArgs {
   const void *k, *v;     // stored rows
   void *ko, *vo;         // loaded rows
   const int* slots;
+  bool stream;           // loaded rows are not read again soon
 };
 template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
 template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);
-
-// Division by d of numbers below 2^31: with 2^s >= d, the quotient is (umulhi(n, m) +
-// n) >> s for m = ceil(2^32 (2^s - d) / d), rounded up past exact values.
-struct FastDiv {
-  uint32_t d, m, s;
-  FastDiv() = default;
-  explicit FastDiv(uint32_t d_) : d(d_), m(0), s(0) {
-    while ((1ull << s) < d) ++s;
-    m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
-  }
-  CS_DEV int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
-};
 
 // ---- attention to contexts (k_xattn*.hip)
 // The queries of a set that share a key head are the rows of one problem: row r is
@@ -52,10 +53,10 @@ struct XAttnArgs {
   float scale_log2;      // log2(e) * scale
   int rows, group;       // lq * group, heads_q / heads_kv
   FastDiv by_group, by_parts, by_heads;   // group, parts, heads_kv
-  // Long contexts: part p of a problem takes keys [p * part_keys, (p + 1) *
-  // part_keys) and leaves its outputs relative to its maximum m and its sums l:
-  // part_o [problem][part][rows][head_dim], part_ml [problem][part][rows] (m, l).
-  int parts, part_keys;
+  // Long contexts: a context's keys are cut into at most `parts` parts of xattn_part
+  // keys.  A part leaves its outputs relative to its maximum m and its sums l: part_o
+  // [problem][part][rows][head_dim], part_ml [problem][part][rows] (m, l).
+  int parts;
   float* part_o;
   float2* part_ml;
 };
@@ -82,6 +83,12 @@ CS_DEV int xattn_context(const XAttnArgs& a, int i, int* len) {
   }
   *len = a.kv_len ? max(0, min(((const_int*)a.kv_len)[j], a.d.lk)) : a.d.lk;
   return j;
+}
+
+// Keys of a part of a context of len keys: whole tiles, a workgroup's worth at least.
+CS_DEV int xattn_part(const XAttnArgs& a, int len) {
+  if (a.parts == 1) return len;
+  return max(128, (a.by_parts.div(len + a.parts - 1) + 63) & ~63);
 }
 
 // LDS by its own address (a generic pointer's conversion checks for null).
