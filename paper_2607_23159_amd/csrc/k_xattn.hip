@@ -22,6 +22,13 @@ static void cut(XAttnArgs& a, bool kv4) {
   a.by_heads = FastDiv(a.d.heads_kv);
 }
 
+// Whether a problem's rows are few enough to meet each key once, in registers: four row
+// tiles of 16, or two where each stands for three (fp32 rows over a 4-bit cache).
+static bool few_rows(const XAttnArgs& a, bool kv4) {
+  if (a.d.dtype == CS_BF16) return a.rows <= 64;
+  return kv4 && a.rows <= 32;
+}
+
 struct Work {
   size_t part_o = 0, part_ml = 0, k = 0, v = 0, bytes = 0;
 };
@@ -38,7 +45,7 @@ static Work layout(const XAttnArgs& a, bool kv4) {
     w.part_o = take(rows * a.d.head_dim * sizeof(float));
     w.part_ml = take(rows * sizeof(float2));
   }
-  if (kv4 && a.rows > XATTN_FEW_ROWS) {
+  if (kv4 && !few_rows(a, kv4)) {
     const size_t n = (size_t)a.d.n_kv * a.d.lk * a.d.heads_kv * a.d.head_dim * (a.d.dtype == CS_BF16 ? 2 : 4);
     w.k = take(n);
     w.v = take(n);
@@ -53,55 +60,56 @@ size_t xattn_workspace(const cs_attn_desc& d, bool kv4) {
   return layout(a, kv4).bytes;
 }
 
-// One row: the parts' outputs, each weighted with 2^(m_p - m).  Sixteen waves
-// take every sixteenth part, lanes the channels.
-template <typename T, int DH> __global__ __launch_bounds__(1024) void k_xattn_join(XAttnArgs a) {
-  constexpr int NW = 16, MAXP = 128;
-  __shared__ float s_w[MAXP], s_o[NW][DH], s_red[2];
+// One row: the parts' outputs, each weighted with 2^(m_p - m).  NW waves take every
+// NW-th of at most MAXP parts, lanes the channels.  Latency is all there is to it: the
+// loads do not wait for the context's length, what lies past its parts is dropped
+// after.
+template <typename T, int DH, int NW, int MAXP> __global__ __launch_bounds__(64 * NW) void k_xattn_join(XAttnArgs a) {
+  __shared__ float s_w[MAXP], s_o[NW][DH], s_sum;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const long pr = blockIdx.x / a.rows;              // problem
-  const int r = (int)(blockIdx.x - pr * a.rows);
-  const int set = (int)(pr / a.d.heads_kv), head = (int)(pr - (long)set * a.d.heads_kv);
+  const int pr = (int)(blockIdx.x / (unsigned)a.rows);   // problem
+  const int r = (int)blockIdx.x - pr * a.rows;
+  const int set = a.by_heads.div(pr), head = pr - set * a.d.heads_kv;
+  const long base = (long)pr * a.parts * a.rows + r;
+  constexpr int NC = (DH + 63) / 64, NP = MAXP / NW, NM = (MAXP + 63) / 64;
+  float o[NP][NC];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int p = min(wave + NW * i, a.parts - 1);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      o[i][c] = lane + 64 * c < DH ? a.part_o[(base + (long)p * a.rows) * DH + lane + 64 * c] : 0.0f;
+  }
+  float2 ml[NM];
+#pragma unroll
+  for (int i = 0; i < NM; ++i) ml[i] = a.part_ml[base + (long)min(lane + 64 * i, a.parts - 1) * a.rows];
   int len;
   xattn_context(a, set, &len);
   const int pk = xattn_part(a, len), n = len > 0 ? (len + pk - 1) / pk : 0;
-  const long base = pr * a.parts * a.rows + r;
-  constexpr int NC = (DH + 63) / 64;
-  float o[MAXP / NW][NC];
-#pragma unroll
-  for (int i = 0; i < MAXP / NW; ++i) {
-    const int p = wave + NW * i;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      o[i][c] = p < n && lane + 64 * c < DH ? a.part_o[(base + (long)p * a.rows) * DH + lane + 64 * c] : 0.0f;
-  }
   if (wave == 0) {
-    float m[2], l[2];
+    float mx = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int p = lane + 64 * i;
-      const float2 ml = p < n ? a.part_ml[base + (long)p * a.rows] : make_float2(-INFINITY, 0.0f);
-      m[i] = ml.x;
-      l[i] = ml.y;
+    for (int i = 0; i < NM; ++i) {
+      if (lane + 64 * i >= n) ml[i] = make_float2(-INFINITY, 0.0f);
+      mx = fmaxf(mx, ml[i].x);
     }
-    float mx = fmaxf(m[0], m[1]);
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor(mx, s, WAVE));
     if (mx == -INFINITY) mx = 0.0f;
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float w = __builtin_amdgcn_exp2f(m[i] - mx);
-      s_w[lane + 64 * i] = w;
-      sum = fmaf(w, l[i], sum);
+    for (int i = 0; i < NM; ++i) {
+      const float w = __builtin_amdgcn_exp2f(ml[i].x - mx);
+      if (lane + 64 * i < MAXP) s_w[lane + 64 * i] = w;
+      sum = fmaf(w, ml[i].y, sum);
     }
     sum = wave_sum(sum);
-    if (lane == 0) s_red[0] = sum;
+    if (lane == 0) s_sum = sum;
   }
   __syncthreads();
   float acc[NC] = {};
 #pragma unroll
-  for (int i = 0; i < MAXP / NW; ++i)
+  for (int i = 0; i < NP; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c)
       if (wave + NW * i < n) acc[c] = fmaf(s_w[wave + NW * i], o[i][c], acc[c]);
@@ -109,24 +117,29 @@ template <typename T, int DH> __global__ __launch_bounds__(1024) void k_xattn_jo
   for (int c = 0; c < NC; ++c)
     if (lane + 64 * c < DH) s_o[wave][lane + 64 * c] = acc[c];
   __syncthreads();
-  if (tid < DH) {
+  for (int c = tid; c < DH; c += 64 * NW) {
     float v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) v += s_o[w][tid];
-    const float l = s_red[0];
+    for (int w = 0; w < NW; ++w) v += s_o[w][c];
     T* dst = (T*)a.o + set * a.d.o_b + xattn_row(a, r, head, a.d.o_r, a.d.o_h);
-    dst[tid] = to_t<T>(l != 0.0f ? v / l : 0.0f);
+    dst[c] = to_t<T>(s_sum != 0.0f ? v / s_sum : 0.0f);
   }
+}
+
+template <typename T, int DH> static void launch_join(const XAttnArgs& a, unsigned blocks, hipStream_t st) {
+  if (a.parts <= 16)
+    hipLaunchKernelGGL((k_xattn_join<T, DH, 4, 16>), dim3(blocks), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_xattn_join<T, DH, 16, 128>), dim3(blocks), dim3(1024), 0, st, a);
 }
 
 template <typename T> static hipError_t join(const XAttnArgs& a, hipStream_t st) {
   const long blocks = (long)a.d.n_q * a.d.heads_kv * a.rows;
   if (blocks > 0x3FFFFFL) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)blocks), block(1024);
   switch (a.d.head_dim) {
-    case 128: hipLaunchKernelGGL((k_xattn_join<T, 128>), grid, block, 0, st, a); break;
-    case 64: hipLaunchKernelGGL((k_xattn_join<T, 64>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_xattn_join<T, 32>), grid, block, 0, st, a); break;
+    case 128: launch_join<T, 128>(a, (unsigned)blocks, st); break;
+    case 64: launch_join<T, 64>(a, (unsigned)blocks, st); break;
+    default: launch_join<T, 32>(a, (unsigned)blocks, st); break;
   }
   return hipGetLastError();
 }
@@ -138,7 +151,7 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
   a.part_ml = (float2*)((char*)work + w.part_ml);
   if (a.parts > 1 && (long)a.d.n_q * a.d.heads_kv * a.rows > 0x3FFFFFL) return hipErrorInvalidConfiguration;
   hipError_t e;
-  if (a.rows <= XATTN_FEW_ROWS && (kv4 || sizeof(T) == 2)) {
+  if (few_rows(a, kv4)) {
     e = xattn_rows<T>(a, kv4, st);
   } else {
     if (kv4) {

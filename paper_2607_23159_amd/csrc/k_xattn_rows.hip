@@ -390,7 +390,8 @@ template <typename T, int DH, bool MASK, bool KV4> static hipError_t launch(cons
   constexpr int NS = sizeof(T) == 2 ? 1 : 3;
   if (a.rows <= 16) return launch_rt<T, DH, 1, NS, MASK, KV4>(a, st);
   if (a.rows <= 32) return launch_rt<T, DH, 2, NS, MASK, KV4>(a, st);
-  if (a.rows <= 64) return launch_rt<T, DH, 4, NS, MASK, KV4>(a, st);
+  if constexpr (NS == 1)
+    if (a.rows <= 64) return launch_rt<T, DH, 4, NS, MASK, KV4>(a, st);
   return hipErrorInvalidValue;
 }
 

@@ -57,6 +57,18 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
   auto row_offset = [&](const TileItem& it, int row, long stride_r, long stride_h) {
     return xattn_row(a, min(it.r0 + wave * 32 + row, a.rows - 1), it.head, stride_r, stride_h);
   };
+  // f(i, offset) of row i * RPI + lane / CPS of this wave, i = 0 .. SI - 1: one step apart
+  // where every query is a row and none lies past the last
+  auto each_row = [&](const TileItem& it, long stride_r, long stride_h, auto f) {
+    if (a.group == 1 && it.r0 + wave * 32 + 32 <= a.rows) {
+      const long at = (long)(it.r0 + wave * 32 + lane / CPS) * (int)stride_r + (long)it.head * (int)stride_h;
+#pragma unroll
+      for (int i = 0; i < SI; ++i) f(i, at + i * (RPI * stride_r));
+    } else {
+#pragma unroll
+      for (int i = 0; i < SI; ++i) f(i, row_offset(it, i * RPI + lane / CPS, stride_r, stride_h));
+    }
+  };
   // The next item of this workgroup with keys to read, from index i on; items without
   // any get their zeros (in parts: nothing, the join does not read them).  Rows past
   // the last are copies of it, here and below: they are stored to the same place.
@@ -118,12 +130,10 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
   frag qf[NKS];   // between load_q and turn_q: the rows as they come from memory
   auto load_q = [&](const TileItem& it) {
     const bf16* src = (const bf16*)a.q + it.set * a.d.q_b + 8 * (lane % CPS);
+    each_row(it, a.d.q_r, a.d.q_h, [&](int i, long at) {
 #pragma unroll
-    for (int i = 0; i < SI; ++i) {
-      const bf16* p = src + row_offset(it, i * RPI + lane / CPS, a.d.q_r, a.d.q_h);
-#pragma unroll
-      for (int s = 0; s < NSEG; ++s) qf[s * SI + i] = MF::load(p + s * (SEG / 2));
-    }
+      for (int s = 0; s < NSEG; ++s) qf[s * SI + i] = MF::load(src + at + s * (SEG / 2));
+    });
   };
   auto turn_q = [&]() {   // to operands: lane row l32, channels 16 ks + 8 half
 #pragma unroll
@@ -235,7 +245,9 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kt][r]);
     mx = max_lane_pair32(mx) * a.scale_log2;
-    if (__any(mx > m_run + 8.0f)) {   // see k_xattn_rows
+    if (kv0 == cur.k0) {   // nothing seen yet: nothing to scale
+      m_run = mx;
+    } else if (__any(mx > m_run + 8.0f)) {   // see k_xattn_rows
       const float m_new = fmaxf(m_run, mx);
       const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
@@ -307,6 +319,8 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
       const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;
       bf16* dst = (bf16*)a.o + cur.set * a.d.o_b + 8 * (lane % CPS);
       constexpr int DPS = NDT / NSEG;   // 32-channel blocks of a segment
+      long at[SI];
+      each_row(cur, a.d.o_r, a.d.o_h, [&](int i, long x) { at[i] = x; });
 #pragma unroll
       for (int s = 0; s < NSEG; ++s) {
         f32x16 os[DPS];
@@ -314,11 +328,9 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
         for (int d = 0; d < DPS; ++d) os[d] = o[s * DPS + d];
         store_o_rows(os, inv, reinterpret_cast<bf16*>(seg + l32 * SRS), half, true);
 #pragma unroll
-        for (int i = 0; i < SI; ++i) {
-          const int row = i * RPI + lane / CPS;
-          *reinterpret_cast<frag*>(dst + row_offset(cur, row, a.d.o_r, a.d.o_h) + s * (SEG / 2)) =
-              *reinterpret_cast<const frag*>(seg + row * SRS + 16 * (lane % CPS));
-        }
+        for (int i = 0; i < SI; ++i)
+          *reinterpret_cast<frag*>(dst + at[i] + s * (SEG / 2)) =
+              *reinterpret_cast<const frag*>(seg + (i * RPI + lane / CPS) * SRS + 16 * (lane % CPS));
       }
     }
     if (!more) return;

@@ -66,7 +66,6 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
 
 // The kernels' launchers: few rows (k_xattn_rows.hip), many rows in bf16
 // (k_xattn_tile.hip), fp32 (k_xattn_f32.hip), and the join of the parts.
-constexpr int XATTN_FEW_ROWS = 64;
 template <typename T> hipError_t xattn_rows(const XAttnArgs& a, bool kv4, hipStream_t st);
 hipError_t xattn_tile(const XAttnArgs& a, hipStream_t st);
 hipError_t xattn_f32(const XAttnArgs& a, hipStream_t st);
