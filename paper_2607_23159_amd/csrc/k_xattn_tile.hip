@@ -347,29 +347,40 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
   }
 }
 
-// Items go round the workgroups that fill the chip's 256 CUs: one of 8 waves each, or
-// two of 4.
+// Items go round the workgroups that fill the chip's 256 CUs: one of 8 or 12 waves each,
+// or two of 4.
 template <int DH, int NW> static hipError_t launch_nw(const XAttnArgs& a, hipStream_t st) {
+  constexpr int OCC = NW == 12 ? 3 : 2;
   const long items = (long)a.d.n_q * a.d.heads_kv * a.parts * cdiv(a.rows, NW * 32);
   if (items > 0x3FFFFFFFL) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)std::min<long>(round_up(items, 8), 256 * (8 / NW))), block(64 * NW);
+  const dim3 grid((unsigned)std::min<long>(round_up(items, 8), 256 * (NW == 4 ? 2 : 1))), block(64 * NW);
   const FastDiv by_qt(cdiv(a.rows, NW * 32));
-  if (a.mask)
-    hipLaunchKernelGGL((k_xattn_tile<DH, NW, 2, true>), grid, block, 0, st, a, by_qt, (int)items);
-  else
-    hipLaunchKernelGGL((k_xattn_tile<DH, NW, 2, false>), grid, block, 0, st, a, by_qt, (int)items);
+  if constexpr (NW < 12) {   // with 12 waves the masks' registers do not fit
+    if (a.mask) {
+      hipLaunchKernelGGL((k_xattn_tile<DH, NW, OCC, true>), grid, block, 0, st, a, by_qt, (int)items);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((k_xattn_tile<DH, NW, OCC, false>), grid, block, 0, st, a, by_qt, (int)items);
   return hipGetLastError();
 }
 
-// 8 waves share a tile of keys between twice the rows, which a full chip runs 7%
+// 8 waves share a tile of keys between twice the rows of 4, which a full chip runs 7%
 // faster (8 sets of 32,760 queries, 512 keys, 12 heads of 128: 0.96 against 1.03 ms; 4 x
 // 1,560: 39.2 against 40.7 us); 4 waves fill it sooner and leave smaller last rounds
-// (1 x 1,560: 14.3 against 17.6 us; 4 x 384, 40 heads: 24.1 against 38.5).  A wave's
-// arithmetic is the same in both, so results are bitwise equal.
+// (1 x 1,560: 14.3 against 17.6 us; 4 x 384, 40 heads: 24.1 against 38.5).  Up to head dim
+// 64 three waves fit a SIMD: 12 take 384 rows at 7% less a row (8 x 32,760 x 512, 12 heads
+// of 64: 602 against 641 us; 4,096 keys 3.68 against 4.02 ms; 2 x 5,000, 300 keys, 4
+// heads: 13.5 against 11.2 us, in one unfilled round).  A wave's arithmetic is the same in
+// all of them, so results are bitwise equal.
 template <int DH> static hipError_t launch_dh(const XAttnArgs& a, hipStream_t st) {
   const long pr = (long)a.d.n_q * a.d.heads_kv * a.parts;
-  const long i8 = pr * cdiv(a.rows, 256), i4 = pr * cdiv(a.rows, 128);
-  const double t8 = (double)cdiv(i8, 256), t4 = i4 <= 256 ? 0.82 : 1.07 * cdiv(i4, 512);
+  const long i4 = pr * cdiv(a.rows, 128);
+  const double t4 = i4 <= 256 ? 0.82 : 1.07 * cdiv(i4, 512), t8 = cdiv(pr * cdiv(a.rows, 256), 256);
+  if constexpr (DH <= 64) {
+    const double t12 = 1.39 * cdiv(pr * cdiv(a.rows, 384), 256);
+    if (!a.mask && t12 < t8 && t12 < t4) return launch_nw<DH, 12>(a, st);
+  }
   return t4 < t8 ? launch_nw<DH, 4>(a, st) : launch_nw<DH, 8>(a, st);
 }
 

@@ -226,12 +226,18 @@ ATTN = [  # dtype, n_q, n_kv, lq, lk, hq, hkv, dim, lengths, mask
     (BF, 1, 1, 385, 130, 3, 1, 128, "full", "none"),
     (BF, 3, 3, 200, 200, 4, 4, 32, "ragged", "empty"),
     (BF, 5, 2, 33, 64, 2, 2, 64, "strange", "holes"),
+    (BF, 6, 4, 3000, 40, 16, 16, 32, "ragged", "none"),
+    (BF, 7, 4, 2500, 70, 12, 12, 64, "ragged", "none"),
+    (BF, 3, 2, 900, 330, 12, 12, 128, "ragged", "holes"),
+    (BF, 2, 2, 200, 1500, 8, 4, 128, "ragged", "none"),
     (FP, 1, 1, 1, 1, 1, 1, 32, "full", "none"),
     (FP, 3, 3, 1, 300, 8, 2, 128, "ragged", "holes"),
     (FP, 2, 2, 297, 77, 4, 4, 64, "ragged", "holes"),
     (FP, 2, 1, 50, 33, 6, 3, 32, "full", "none"),
     (FP, 2, 2, 65, 129, 4, 4, 128, "strange", "empty"),
     (FP, 1, 1, 2, 2500, 4, 1, 64, "full", "none"),
+    (FP, 2, 1, 12, 60, 12, 4, 128, "ragged", "holes"),
+    (FP, 1, 2, 40, 1100, 2, 2, 32, "ragged", "none"),
 ]
 
 
