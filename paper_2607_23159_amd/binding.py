@@ -415,6 +415,13 @@ def _on_current(device) -> None:
         raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
+def _aux(x, numel: int, dtype: str, name: str, device) -> Optional[int]:
+    """Address of an index tensor, a mask or the like on the operator's device."""
+    if x is not None and not isinstance(x, int) and x.device != device:
+        raise ValueError(f"{name}: on {x.device}, the operator is on {device}")
+    return _ptr(x, numel, dtype, name)
+
+
 class _OpDesc:
     """A descriptor with the tensors' signatures it stands for."""
 
@@ -494,7 +501,8 @@ def cs_qk_norm_rope(desc: _OpDesc, q, k, q_out, k_out, q_gain, k_gain, rope=None
     _check(lib().cs_qk_norm_rope(desc.ref, _same(q, s["q"], "q"), _same(k, s["k"], "k"),
                                  _same(q_out, s["q_out"], "q_out"), _same(k_out, s["k_out"], "k_out"),
                                  _same(q_gain, s["q_gain"], "q_gain"), _same(k_gain, s["k_gain"], "k_gain"),
-                                 _same(rope, s["rope"], "rope"), _ptr(pos, desc.c.tokens, "int32", "pos"),
+                                 _same(rope, s["rope"], "rope"),
+                                 _aux(pos, desc.c.tokens, "int32", "pos", desc.device),
                                  _stream(stream)))
 
 
@@ -535,7 +543,7 @@ def cs_kv4_store(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
     """Rows k, v [n_rows][heads][head_dim] into the cache; ``slots``: int32 device tensor or None."""
     _on_current(cache.device)
     d = cache.rows(k, v)
-    _check(lib().cs_kv4_store(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _ptr(slots, d.c.n_rows, "int32", "slots"),
+    _check(lib().cs_kv4_store(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _aux(slots, d.c.n_rows, "int32", "slots", cache.device),
                               _stream(stream)))
 
 
@@ -543,7 +551,7 @@ def cs_kv4_load(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
     """The values that rows of the cache stand for into k and v."""
     _on_current(cache.device)
     d = cache.rows(k, v)
-    _check(lib().cs_kv4_load(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _ptr(slots, d.c.n_rows, "int32", "slots"),
+    _check(lib().cs_kv4_load(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _aux(slots, d.c.n_rows, "int32", "slots", cache.device),
                              _stream(stream)))
 
 
@@ -589,12 +597,19 @@ def cs_kv4_attention_workspace(desc: _OpDesc) -> int:
 
 
 def _attn_rest(desc: _OpDesc, kv_of, kv_len, kv_mask, work):
-    """Addresses of the index tensors (int32), the mask ([n_kv][lk] uint8, contiguous) and the workspace."""
-    c = desc.c
-    nbytes = 0 if work is None else (work.numel() * work.element_size() if not isinstance(work, int) else 1 << 62)
-    return (_ptr(kv_of, c.n_q, "int32", "kv_of"), _ptr(kv_len, c.n_kv, "int32", "kv_len"),
-            _ptr(kv_mask, c.n_kv * c.lk, "uint8", "kv_mask"),
-            work if work is None or isinstance(work, int) else work.data_ptr(), nbytes)
+    """Addresses of the index tensors (int32), the mask ([n_kv][lk] uint8, contiguous) and the
+    workspace (any contiguous tensor), and the workspace's bytes."""
+    c, dev = desc.c, desc.device
+    nbytes = 0
+    if isinstance(work, int):
+        nbytes = 1 << 62        # unchecked
+    elif work is not None:
+        if work.device != dev or not work.is_contiguous():
+            raise ValueError(f"work: a contiguous tensor on {dev} is required")
+        nbytes = work.numel() * work.element_size()
+        work = work.data_ptr()
+    return (_aux(kv_of, c.n_q, "int32", "kv_of", dev), _aux(kv_len, c.n_kv, "int32", "kv_len", dev),
+            _aux(kv_mask, c.n_kv * c.lk, "uint8", "kv_mask", dev), work, nbytes)
 
 
 def cs_cross_attention(desc: _OpDesc, q, k, v, o, kv_of=None, kv_len=None, kv_mask=None, work=None,
@@ -609,6 +624,8 @@ def cs_cross_attention(desc: _OpDesc, q, k, v, o, kv_of=None, kv_len=None, kv_ma
 def cs_kv4_attention(desc: _OpDesc, q, cache: Kv4Cache, o, kv_of=None, kv_len=None, kv_mask=None, work=None,
                      stream=None) -> None:
     _on_current(desc.device)
+    if cache.device != desc.device:
+        raise ValueError(f"the cache is on {cache.device}, the descriptor's tensors on {desc.device}")
     s = desc.sig
     of, ln, mask, w, nbytes = _attn_rest(desc, kv_of, kv_len, kv_mask, work)
     _check(lib().cs_kv4_attention(desc.ref, _same(q, s["q"], "q"), cache.ref, of, ln, mask, _same(o, s["o"], "o"), w,

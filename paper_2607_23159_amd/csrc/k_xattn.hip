@@ -22,11 +22,20 @@ static void cut(XAttnArgs& a, bool kv4) {
   a.by_heads = FastDiv(a.d.heads_kv);
 }
 
-// Whether a problem's rows are few enough to meet each key once, in registers: four row
-// tiles of 16, or two where each stands for three (fp32 rows over a 4-bit cache).
+// Whether a problem goes to k_xattn_rows, which takes its rows 32 at a time and reads
+// the keys once for each 32.
+//   bf16: if that is once (8 contexts of 8,192 rows, 8 key heads: 32 rows 53.0 us, 36
+//     rows in k_xattn_tile 56.2; 64 rows 138 here, 64.1 there).
+//   4 bits, bf16 rows: k_xattn_tile wants the cache unpacked first, which pays once the
+//     rows are many (16 contexts of 32,768 rows, 8 key heads, here / there: 64 rows 339 /
+//     987 us, 128 rows 551 / 1,069, 192 rows 829 / 1,203, 256 rows 1,100 / 1,273, 384 rows
+//     1,647 / 1,622).  Contexts that many queries share would turn earlier.
+//   4 bits, fp32 rows: always.  The queries' and weights' three bf16 terms meet exact
+//     bf16 keys at 220 TFLOP/s, the fp32 products of k_xattn_f32 reach 85 (96 tokens of
+//     4 heads each: 3,751 us, 9,748 there).
 static bool few_rows(const XAttnArgs& a, bool kv4) {
-  if (a.d.dtype == CS_BF16) return a.rows <= 64;
-  return kv4 && a.rows <= 32;
+  if (a.d.dtype != CS_BF16) return kv4;
+  return a.rows <= (kv4 ? 192 : 32);
 }
 
 struct Work {
@@ -46,7 +55,7 @@ static Work layout(const XAttnArgs& a, bool kv4) {
     w.part_ml = take(rows * sizeof(float2));
   }
   if (kv4 && !few_rows(a, kv4)) {
-    const size_t n = (size_t)a.d.n_kv * a.d.lk * a.d.heads_kv * a.d.head_dim * (a.d.dtype == CS_BF16 ? 2 : 4);
+    const size_t n = (size_t)a.d.n_kv * a.d.lk * a.d.heads_kv * a.d.head_dim * sizeof(bf16);
     w.k = take(n);
     w.v = take(n);
   }
@@ -135,7 +144,6 @@ template <typename T, int DH> static void launch_join(const XAttnArgs& a, unsign
 
 template <typename T> static hipError_t join(const XAttnArgs& a, hipStream_t st) {
   const long blocks = (long)a.d.n_q * a.d.heads_kv * a.rows;
-  if (blocks > 0x3FFFFFL) return hipErrorInvalidConfiguration;
   switch (a.d.head_dim) {
     case 128: launch_join<T, 128>(a, (unsigned)blocks, st); break;
     case 64: launch_join<T, 64>(a, (unsigned)blocks, st); break;
@@ -149,31 +157,37 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
   const Work w = layout(a, kv4);
   a.part_o = (float*)((char*)work + w.part_o);
   a.part_ml = (float2*)((char*)work + w.part_ml);
-  if (a.parts > 1 && (long)a.d.n_q * a.d.heads_kv * a.rows > 0x3FFFFFL) return hipErrorInvalidConfiguration;
+  // grids, before anything is enqueued
+  const long pr = (long)a.d.n_q * a.d.heads_kv;
+  const bool few = few_rows(a, kv4), stream = !few && sizeof(T) == 2;
+  if ((a.parts > 1 && pr * a.rows > 0x3FFFFFL) ||
+      pr * a.parts * cdiv(a.rows, few ? 16 : 32) > (stream ? 0x3FFFFFFFL : 0xFFFFFFL))
+    return hipErrorInvalidConfiguration;
   hipError_t e;
-  if (few_rows(a, kv4)) {
+  if (few) {
     e = xattn_rows<T>(a, kv4, st);
   } else {
-    if (kv4) {
-      // many queries meet every key: unpack the cache once
-      Kv4RowsArgs l = {};
-      l.c = a.c;
-      const long hd = (long)a.d.heads_kv * a.d.head_dim;
-      l.r = {a.d.dtype, a.d.n_kv * a.d.lk, hd, a.d.head_dim, hd, a.d.head_dim};
-      l.ko = (char*)work + w.k;
-      l.vo = (char*)work + w.v;
-      e = kv4_load<T>(l, st);
-      if (e != hipSuccess) return e;
-      a.k = l.ko;
-      a.v = l.vo;
-      a.d.k_r = a.d.v_r = hd;
-      a.d.k_h = a.d.v_h = a.d.head_dim;
-      a.d.k_b = a.d.v_b = hd * a.d.lk;
-    }
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
+      if (kv4) {
+        // many queries meet every key: unpack the cache once
+        Kv4RowsArgs l = {};
+        l.c = a.c;
+        const long hd = (long)a.d.heads_kv * a.d.head_dim;
+        l.r = {a.d.dtype, a.d.n_kv * a.d.lk, hd, a.d.head_dim, hd, a.d.head_dim};
+        l.ko = (char*)work + w.k;
+        l.vo = (char*)work + w.v;
+        e = kv4_load<T>(l, st);
+        if (e != hipSuccess) return e;
+        a.k = l.ko;
+        a.v = l.vo;
+        a.d.k_r = a.d.v_r = hd;
+        a.d.k_h = a.d.v_h = a.d.head_dim;
+        a.d.k_b = a.d.v_b = hd * a.d.lk;
+      }
       e = xattn_tile(a, st);
-    else
+    } else {
       e = xattn_f32(a, st);
+    }
   }
   if (e == hipSuccess && a.parts > 1) e = join<T>(a, st);
   return e;

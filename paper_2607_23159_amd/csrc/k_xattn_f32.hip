@@ -167,7 +167,6 @@ template <int DH, bool MASK> __global__ __launch_bounds__(256, 1) void k_xattn_f
 
 template <int DH> static hipError_t launch(const XAttnArgs& a, hipStream_t st) {
   const long blocks = (long)a.d.n_q * a.d.heads_kv * a.parts * cdiv(a.rows, 32);
-  if (blocks > 0xFFFFFFL) return hipErrorInvalidConfiguration;
   if (a.mask)
     hipLaunchKernelGGL((k_xattn_f32<DH, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);
   else

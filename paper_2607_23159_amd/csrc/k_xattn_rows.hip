@@ -1,5 +1,6 @@
 // Attention of few queries (a token or a handful, with the heads that share a key
-// head: at most 64 rows) to a context: keys and values are read once, from memory.
+// head) to a context, 32 rows at a time: keys and values are read once for them, from
+// memory.  Over a 4-bit cache in fp32, of any number of queries.
 //
 // Work split.  A workgroup takes one part of a problem's keys, its four waves the
 // part's tiles in turn, each on its own: no barrier until the waves' outputs are
@@ -186,7 +187,7 @@ template <int DH, bool MASK> struct TileKv4 {
 
 // NS: bf16 terms of a query and of a softmax weight (1: bf16; 3: fp32).
 template <typename T, int DH, int RT, int NS, bool MASK, typename Tile>
-__global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_xattn_rows(XAttnArgs a) {
+__global__ __launch_bounds__(256, NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_xattn_rows(XAttnArgs a, FastDiv by_blocks) {
   typedef ValueRows<DH> Rows;
   constexpr int NW = 4, KS = DH / 32, NCT = DH / 16, OLD = DH + 4, KEYS = Tile::KEYS;
   constexpr uint64_t FULL = (1ull << KEYS) - 1;
@@ -198,8 +199,11 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVE
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int part = blockIdx.x % a.parts, pr = blockIdx.x / a.parts;
-  const int set = pr / a.d.heads_kv, head = pr - set * a.d.heads_kv;
+  // row blocks of one part next to each other, on one XCD: its L2 then reads the part once
+  const int id = by_blocks.d > 1 ? xcd_contiguous(blockIdx.x, gridDim.x) : (int)blockIdx.x;
+  const int at = by_blocks.div(id), r0 = (id - at * (int)by_blocks.d) * 16 * RT;
+  const int pr = a.by_parts.div(at), part = at - pr * a.parts;
+  const int set = a.by_heads.div(pr), head = pr - set * a.d.heads_kv;
   int len;
   const int ctx = xattn_context(a, set, &len);
   const int pk = xattn_part(a, len), k0 = part * pk, k1 = min(len, k0 + pk);
@@ -209,7 +213,7 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVE
   bf16x8 qf[NS][RT][KS];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int r = min(16 * rt + l16, a.rows - 1);
+    const int r = min(r0 + 16 * rt + l16, a.rows - 1);
     const T* src = (const T*)a.q + set * a.d.q_b + xattn_row(a, r, head, a.d.q_r, a.d.q_h);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVE
   float(*s_o)[16 * OLD] = reinterpret_cast<float(*)[16 * OLD]>(smem);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    if (16 * rt >= a.rows) break;
+    if (r0 + 16 * rt >= a.rows) break;
     __syncthreads();   // stages and the previous row tile are read
     float m_all = s_m[0][16 * rt + l16];
 #pragma unroll
@@ -346,17 +350,17 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVE
       *reinterpret_cast<f32x4*>(&s_o[wave][l16 * OLD + 16 * ct + 4 * g]) = o[rt][ct] * f;
     __syncthreads();
     for (int i = tid; i < 16 * DH / 4; i += 64 * NW) {
-      const int q = i / (DH / 4), c = 4 * (i % (DH / 4)), r = 16 * rt + q;
+      const int q = i / (DH / 4), c = 4 * (i % (DH / 4)), tr = 16 * rt + q, r = r0 + tr;
       if (r >= a.rows) break;
-      float m = s_m[0][r], l = 0.0f;
+      float m = s_m[0][tr], l = 0.0f;
 #pragma unroll
-      for (int w = 1; w < NW; ++w) m = fmaxf(m, s_m[w][r]);
+      for (int w = 1; w < NW; ++w) m = fmaxf(m, s_m[w][tr]);
       const float mu = m == -INFINITY ? 0.0f : m;
       f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         v += *reinterpret_cast<const f32x4*>(&s_o[w][q * OLD + c]);
-        l = fmaf(s_l[w][r], __builtin_amdgcn_exp2f(s_m[w][r] - mu), l);
+        l = fmaf(s_l[w][tr], __builtin_amdgcn_exp2f(s_m[w][tr] - mu), l);
       }
       if (a.parts > 1) {
         const long at = ((long)pr * a.parts + part) * a.rows + r;
@@ -375,24 +379,23 @@ __global__ __launch_bounds__(256, RT > 2 || NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVE
   }
 }
 
-// Row tiles of 16: as many as the rows need.
-template <typename T, int DH, int RT, int NS, bool MASK, bool KV4> static hipError_t launch_rt(const XAttnArgs& a, hipStream_t st) {
-  const long blocks = (long)a.d.n_q * a.d.heads_kv * a.parts;
-  if (blocks > 0xFFFFFFL) return hipErrorInvalidConfiguration;
+// Blocks of 16 RT rows.
+template <typename T, int DH, int RT, bool MASK, bool KV4> static hipError_t launch_rt(const XAttnArgs& a, hipStream_t st) {
+  constexpr int NS = sizeof(T) == 2 ? 1 : 3;
+  const FastDiv by_blocks(cdiv(a.rows, 16 * RT));
+  const dim3 grid((unsigned)((long)a.d.n_q * a.d.heads_kv * a.parts * by_blocks.d)), block(256);
   if constexpr (KV4)
-    hipLaunchKernelGGL((k_xattn_rows<T, DH, RT, NS, MASK, TileKv4<DH, MASK>>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_xattn_rows<T, DH, RT, NS, MASK, TileKv4<DH, MASK>>), grid, block, 0, st, a, by_blocks);
   else
-    hipLaunchKernelGGL((k_xattn_rows<T, DH, RT, NS, MASK, TileBf16<DH, MASK>>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_xattn_rows<T, DH, RT, NS, MASK, TileBf16<DH, MASK>>), grid, block, 0, st, a, by_blocks);
   return hipGetLastError();
 }
 
+// One row tile where 16 hold all rows, two else: a third and fourth do not fit the
+// registers of two waves a SIMD (64 rows over 16 4-bit contexts of 32,768 rows: 382 us as one
+// block of four tiles, 326 as two blocks of two).
 template <typename T, int DH, bool MASK, bool KV4> static hipError_t launch(const XAttnArgs& a, hipStream_t st) {
-  constexpr int NS = sizeof(T) == 2 ? 1 : 3;
-  if (a.rows <= 16) return launch_rt<T, DH, 1, NS, MASK, KV4>(a, st);
-  if (a.rows <= 32) return launch_rt<T, DH, 2, NS, MASK, KV4>(a, st);
-  if constexpr (NS == 1)
-    if (a.rows <= 64) return launch_rt<T, DH, 4, NS, MASK, KV4>(a, st);
-  return hipErrorInvalidValue;
+  return a.rows <= 16 ? launch_rt<T, DH, 1, MASK, KV4>(a, st) : launch_rt<T, DH, 2, MASK, KV4>(a, st);
 }
 
 template <typename T, int DH> static hipError_t launch_dh(const XAttnArgs& a, bool kv4, hipStream_t st) {

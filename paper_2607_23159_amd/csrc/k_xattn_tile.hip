@@ -352,7 +352,6 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
 template <int DH, int NW> static hipError_t launch_nw(const XAttnArgs& a, hipStream_t st) {
   constexpr int OCC = NW == 12 ? 3 : 2;
   const long items = (long)a.d.n_q * a.d.heads_kv * a.parts * cdiv(a.rows, NW * 32);
-  if (items > 0x3FFFFFFFL) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)std::min<long>(round_up(items, 8), 256 * (NW == 4 ? 2 : 1))), block(64 * NW);
   const FastDiv by_qt(cdiv(a.rows, NW * 32));
   if constexpr (NW < 12) {   // with 12 waves the masks' registers do not fit

@@ -156,6 +156,7 @@ static cs_status check_attn(const cs_attn_desc* d, bool kv4) {
   // offsets inside a tile of keys are 32-bit byte counts
   CHECK(kv4 || d->lk <= 1 || (d->k_r <= (1 << 23) && d->v_r <= (1 << 23)), CS_E_UNSUPPORTED,
         "strides k_r and v_r must be at most 2^23");
+  CHECK(!kv4 || (long)d->heads_kv * d->head_dim <= (1 << 23), CS_E_UNSUPPORTED, "heads_kv * head_dim must be at most 2^23");
   CHECK((d->lq <= 1 || (d->q_r < (1L << 31) && d->o_r < (1L << 31))) &&
             (d->heads_q <= 1 || (d->q_h < (1L << 31) && d->o_h < (1L << 31))),
         CS_E_UNSUPPORTED, "strides q_r, q_h, o_r and o_h must be below 2^31");

@@ -230,6 +230,10 @@ ATTN = [  # dtype, n_q, n_kv, lq, lk, hq, hkv, dim, lengths, mask
     (BF, 7, 4, 2500, 70, 12, 12, 64, "ragged", "none"),
     (BF, 3, 2, 900, 330, 12, 12, 128, "ragged", "holes"),
     (BF, 2, 2, 200, 1500, 8, 4, 128, "ragged", "none"),
+    (BF, 5, 3, 8, 2600, 16, 4, 128, "ragged", "none"),
+    (BF, 3, 2, 21, 1100, 3, 1, 64, "ragged", "holes"),
+    (BF, 2, 2, 64, 1030, 3, 1, 32, "strange", "none"),
+    (BF, 2, 2, 193, 1030, 2, 2, 32, "ragged", "empty"),
     (FP, 1, 1, 1, 1, 1, 1, 32, "full", "none"),
     (FP, 3, 3, 1, 300, 8, 2, 128, "ragged", "holes"),
     (FP, 2, 2, 297, 77, 4, 4, 64, "ragged", "holes"),
@@ -238,6 +242,8 @@ ATTN = [  # dtype, n_q, n_kv, lq, lk, hq, hkv, dim, lengths, mask
     (FP, 1, 1, 2, 2500, 4, 1, 64, "full", "none"),
     (FP, 2, 1, 12, 60, 12, 4, 128, "ragged", "holes"),
     (FP, 1, 2, 40, 1100, 2, 2, 32, "ragged", "none"),
+    (FP, 5, 3, 8, 2600, 16, 4, 128, "ragged", "none"),
+    (FP, 2, 2, 1100, 150, 4, 4, 64, "ragged", "holes"),
 ]
 
 

@@ -185,3 +185,11 @@ def test_contexts_and_norm_choice_refuse_null_and_unknown():
     assert lib.cs_model_init_norm(C.byref(d), 2, P, synth.weight_count(m), None, C.byref(out)) == B.CS_E_INVAL
     assert "qk_norm" in B.cs_last_error()
     assert lib.cs_model_init_norm(C.byref(d), 1, None, synth.weight_count(m), None, C.byref(out)) == B.CS_E_INVAL
+
+
+def test_calls_too_large_for_a_grid():
+    for kw in (dict(dtype=B.CS_FP32, n_q=1 << 20, lq=1 << 12), dict(n_q=1 << 25, lq=1),
+               dict(n_q=1 << 28, lq=1 << 10)):
+        assert attn(attn_desc(heads_q=2, heads_kv=2, n_kv=1, q_b=8, o_b=8, q_r=8, o_r=8, q_h=8, o_h=8, **kw),
+                    of=P) == B.CS_E_UNSUPPORTED
+        assert "too many" in B.cs_last_error()
