@@ -354,7 +354,11 @@ typedef struct {
  * that are left out are never met: their rows may hold anything, NaN included.  A
  * query with no key left, or whose kv_of is not in 0..n_kv-1, gets zeros.  Scores
  * and sums are fp32; in CS_BF16 mode the softmax weights are rounded to bf16 for
- * the product with v and summed as rounded.  o must not overlap the inputs.
+ * the product with v and summed as rounded.  In CS_FP32 mode a product may be taken
+ * as six products of bf16 terms (off by at most 2^-22 of its magnitude): an element
+ * of 3.39e38 or more, infinities included, in a query or in a key or value that is
+ * not left out then makes NaN of the outputs it enters.  o must not overlap the
+ * inputs.
  * cs_cross_attention_workspace gives the bytes of `work` (0: work may be NULL). */
 cs_status cs_cross_attention_workspace(const cs_attn_desc* desc, size_t* bytes);
 cs_status cs_cross_attention(const cs_attn_desc* desc, const void* q, const void* k, const void* v,

@@ -15,8 +15,12 @@ static void cut(XAttnArgs& a, bool kv4) {
   // Keys of a full context's part: half as many bytes again in 4 bits (16 contexts of up
   // to 32,768 rows: 512 keys 72.7 us, 1,024 66.6, 2,048 82.6; bf16, 8 of up to 8,192: 256
   // keys 35.3, 512 34.2, 1,024 35.8).
-  const int keys = kv4 ? 1024 : 512, most = 128;
-  if (a.rows <= 1024 && a.d.lk > keys) a.parts = std::min(most, cdiv(a.d.lk, keys));
+  // Many rows fill the card by themselves; in fp32, where a workgroup takes long over its
+  // keys, eight times as many keys (one set of 12 heads, 1,560 rows, 32,760 keys: 3,319 us
+  // whole, 1,690 in parts).
+  const bool many = a.rows > 1024;
+  const int keys = !many ? kv4 ? 1024 : 512 : a.d.dtype == CS_FP32 && !kv4 ? 4096 : 1 << 30, most = 128;
+  if (a.d.lk > keys) a.parts = std::min(most, cdiv(a.d.lk, keys));
   a.by_group = FastDiv(a.group);
   a.by_parts = FastDiv(a.parts);
   a.by_heads = FastDiv(a.d.heads_kv);
@@ -37,6 +41,13 @@ static bool few_rows(const XAttnArgs& a, bool kv4) {
   if (a.d.dtype != CS_BF16) return kv4;
   return a.rows <= (kv4 ? 192 : 32);
 }
+
+// Which of the fp32 kernels.  k_xattn_split does a product in bf16 terms, at twice the
+// rate, but its workgroups take 128 rows and all keys in turn where those of k_xattn_f32
+// take 32 rows and split the keys between their waves: it wants 64 workgroups a set (12
+// heads of 128, 512 keys, here / there: 400 rows 59.3 / 28.1 us, 800 rows 60.8 / 52.6, 1,560
+// rows 61.4 / 75.7; 8 such sets: 87.4 / 127, 137 / 248, 221 / 468).
+static bool split_f32(const XAttnArgs& a) { return a.rows > 64 && (long)a.rows * a.d.heads_kv >= 64 * 128; }
 
 struct Work {
   size_t part_o = 0, part_ml = 0, k = 0, v = 0, bytes = 0;
@@ -76,62 +87,66 @@ size_t xattn_workspace(const cs_attn_desc& d, bool kv4) {
 template <typename T, int DH, int NW, int MAXP> __global__ __launch_bounds__(64 * NW) void k_xattn_join(XAttnArgs a) {
   __shared__ float s_w[MAXP], s_o[NW][DH], s_sum;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int pr = (int)(blockIdx.x / (unsigned)a.rows);   // problem
-  const int r = (int)blockIdx.x - pr * a.rows;
-  const int set = a.by_heads.div(pr), head = pr - set * a.d.heads_kv;
-  const long base = (long)pr * a.parts * a.rows + r;
-  constexpr int NC = (DH + 63) / 64, NP = MAXP / NW, NM = (MAXP + 63) / 64;
-  float o[NP][NC];
+  const uint32_t total = (uint32_t)(a.d.n_q * a.d.heads_kv) * a.rows;   // below 2^31
+  for (uint32_t row = blockIdx.x; row < total; row += gridDim.x) {
+    if (row != blockIdx.x) __syncthreads();   // s_sum is read
+    const int pr = (int)(row / (uint32_t)a.rows);   // problem
+    const int r = (int)row - pr * a.rows;
+    const int set = a.by_heads.div(pr), head = pr - set * a.d.heads_kv;
+    const long base = (long)pr * a.parts * a.rows + r;
+    constexpr int NC = (DH + 63) / 64, NP = MAXP / NW, NM = (MAXP + 63) / 64;
+    float o[NP][NC];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int p = min(wave + NW * i, a.parts - 1);
+    for (int i = 0; i < NP; ++i) {
+      const int p = min(wave + NW * i, a.parts - 1);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        o[i][c] = lane + 64 * c < DH ? a.part_o[(base + (long)p * a.rows) * DH + lane + 64 * c] : 0.0f;
+    }
+    float2 ml[NM];
+#pragma unroll
+    for (int i = 0; i < NM; ++i) ml[i] = a.part_ml[base + (long)min(lane + 64 * i, a.parts - 1) * a.rows];
+    int len;
+    xattn_context(a, set, &len);
+    const int pk = xattn_part(a, len), n = len > 0 ? (len + pk - 1) / pk : 0;
+    if (wave == 0) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < NM; ++i) {
+        if (lane + 64 * i >= n) ml[i] = make_float2(-INFINITY, 0.0f);
+        mx = fmaxf(mx, ml[i].x);
+      }
+#pragma unroll
+      for (int s = 32; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor(mx, s, WAVE));
+      if (mx == -INFINITY) mx = 0.0f;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NM; ++i) {
+        const float w = __builtin_amdgcn_exp2f(ml[i].x - mx);
+        if (lane + 64 * i < MAXP) s_w[lane + 64 * i] = w;
+        sum = fmaf(w, ml[i].y, sum);
+      }
+      sum = wave_sum(sum);
+      if (lane == 0) s_sum = sum;
+    }
+    __syncthreads();
+    float acc[NC] = {};
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (wave + NW * i < n) acc[c] = fmaf(s_w[wave + NW * i], o[i][c], acc[c]);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      o[i][c] = lane + 64 * c < DH ? a.part_o[(base + (long)p * a.rows) * DH + lane + 64 * c] : 0.0f;
-  }
-  float2 ml[NM];
+      if (lane + 64 * c < DH) s_o[wave][lane + 64 * c] = acc[c];
+    __syncthreads();
+    for (int c = tid; c < DH; c += 64 * NW) {
+      float v = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NM; ++i) ml[i] = a.part_ml[base + (long)min(lane + 64 * i, a.parts - 1) * a.rows];
-  int len;
-  xattn_context(a, set, &len);
-  const int pk = xattn_part(a, len), n = len > 0 ? (len + pk - 1) / pk : 0;
-  if (wave == 0) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NM; ++i) {
-      if (lane + 64 * i >= n) ml[i] = make_float2(-INFINITY, 0.0f);
-      mx = fmaxf(mx, ml[i].x);
+      for (int w = 0; w < NW; ++w) v += s_o[w][c];
+      T* dst = (T*)a.o + set * a.d.o_b + xattn_row(a, r, head, a.d.o_r, a.d.o_h);
+      dst[c] = to_t<T>(s_sum != 0.0f ? v / s_sum : 0.0f);
     }
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor(mx, s, WAVE));
-    if (mx == -INFINITY) mx = 0.0f;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NM; ++i) {
-      const float w = __builtin_amdgcn_exp2f(ml[i].x - mx);
-      if (lane + 64 * i < MAXP) s_w[lane + 64 * i] = w;
-      sum = fmaf(w, ml[i].y, sum);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) s_sum = sum;
-  }
-  __syncthreads();
-  float acc[NC] = {};
-#pragma unroll
-  for (int i = 0; i < NP; ++i)
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      if (wave + NW * i < n) acc[c] = fmaf(s_w[wave + NW * i], o[i][c], acc[c]);
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-    if (lane + 64 * c < DH) s_o[wave][lane + 64 * c] = acc[c];
-  __syncthreads();
-  for (int c = tid; c < DH; c += 64 * NW) {
-    float v = 0.0f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) v += s_o[w][c];
-    T* dst = (T*)a.o + set * a.d.o_b + xattn_row(a, r, head, a.d.o_r, a.d.o_h);
-    dst[c] = to_t<T>(s_sum != 0.0f ? v / s_sum : 0.0f);
   }
 }
 
@@ -143,7 +158,7 @@ template <typename T, int DH> static void launch_join(const XAttnArgs& a, unsign
 }
 
 template <typename T> static hipError_t join(const XAttnArgs& a, hipStream_t st) {
-  const long blocks = (long)a.d.n_q * a.d.heads_kv * a.rows;
+  const long blocks = std::min((long)a.d.n_q * a.d.heads_kv * a.rows, 0x3FFFFFL);
   switch (a.d.head_dim) {
     case 128: launch_join<T, 128>(a, (unsigned)blocks, st); break;
     case 64: launch_join<T, 64>(a, (unsigned)blocks, st); break;
@@ -160,7 +175,7 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
   // grids, before anything is enqueued
   const long pr = (long)a.d.n_q * a.d.heads_kv;
   const bool few = few_rows(a, kv4), stream = !few && sizeof(T) == 2;
-  if ((a.parts > 1 && pr * a.rows > 0x3FFFFFL) ||
+  if ((a.parts > 1 && pr * a.rows > 0x7FFFFFFFL) ||
       pr * a.parts * cdiv(a.rows, few ? 16 : 32) > (stream ? 0x3FFFFFFFL : 0xFFFFFFL))
     return hipErrorInvalidConfiguration;
   hipError_t e;
@@ -186,7 +201,7 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
       }
       e = xattn_tile(a, st);
     } else {
-      e = xattn_f32(a, st);
+      e = split_f32(a) ? xattn_split(a, st) : xattn_f32(a, st);
     }
   }
   if (e == hipSuccess && a.parts > 1) e = join<T>(a, st);

@@ -1,4 +1,4 @@
-// fp32 attention of many queries (or few) to contexts.
+// fp32 attention to contexts where workgroups are few.
 //
 // The four waves of a workgroup share 32 rows and split the keys in blocks of 32;
 // every fragment comes straight from L2, as in the fp32 self-attention: the fp32

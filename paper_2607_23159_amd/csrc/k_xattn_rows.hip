@@ -12,64 +12,12 @@
 // 16-key score blocks hold there, 4 (l / 16) + j and 16 + 4 (l / 16) + j, and reads
 // the same keys of V^T through two transposing LDS reads (ds_read_b64_tr_b16: lane i
 // of 16 gets column i of the 4 rows that the 16 lanes address).
-#include "ops.hpp"
+#include "xattn_mma.hpp"
 
 namespace cs {
 
-CS_DEV f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-// Maximum / sum over lanes l, l ^ 16, l ^ 32, l ^ 48.
-CS_DEV float max_groups16(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max_lane_pair32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-CS_DEV float sum_groups16(float x) {
-  x += __shfl_xor(x, 16, WAVE);
-  return x + __shfl_xor(x, 32, WAVE);
-}
-
-// x as a sum of NS bf16 terms, the largest first (three hold all 24 bits).
-template <int NS> CS_DEV void split_bf16(float x, bf16* t) {
-#pragma unroll
-  for (int i = 0; i < NS; ++i) {
-    t[i] = (bf16)x;
-    x -= (float)t[i];
-  }
-}
-
-typedef __attribute__((address_space(3))) bf16x8 lds_vec8;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-// Keys of a tile (bit i: key kv0 + i) that are left: below k1 and not masked.
-template <int KEYS, bool MASK>
-CS_DEV uint64_t tile_bits(const uint8_t* mask, int kv0, int k1, int lane) {
-  if constexpr (MASK) {
-    const int key = kv0 + lane;
-    return __ballot(lane < KEYS && key < k1 && mask[min(key, k1 - 1)] != 0);
-  } else {
-    const int n = min(KEYS, k1 - kv0);
-    return n == 64 ? ~0ull : (1ull << n) - 1;
-  }
-}
-
-// Values of a tile in LDS: rows of DH bf16, whose 16-byte chunks are permuted by the
-// row (chunk c of row r at c ^ swz(r)): 16 rows' writes of one chunk, and 8 rows'
-// reads of two, meet every bank once.
-template <int DH> struct ValueRows {
-  static constexpr int NC = DH / 8, BYTES = 2 * DH, PER256 = DH == 128 ? 0 : DH == 64 ? 1 : 2;   // log2 rows in 256 bytes
-  static CS_DEV int swz(int r) { return 2 * ((r >> PER256) & (NC / 2 - 1)) | ((r >> 3) & 1); }
-  static CS_DEV void put(lds_char* rows, int r, int chunk, bf16x8 v) {
-    *(lds_vec8*)(rows + r * BYTES + 16 * (chunk ^ swz(r))) = v;
-  }
-  // V^T operand of 16 channels ct over the 32 rows from `rows` on
-  static CS_DEV bf16x8 operand(const lds_char* rows, int lane, int ct) {
-    const int r = 4 * (lane >> 4) + ((lane & 15) >> 2);
-    const lds_char* p = rows + r * BYTES + 16 * ((2 * ct + ((lane >> 1) & 1)) ^ swz(r)) + 8 * (lane & 1);
-    const bf16x4 x = lds_read_tr(p), y = lds_read_tr(p + 16 * BYTES);   // row + 16 is permuted alike
-    return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-  }
-};
 
 // A tile of 32 keys on its way through the registers of a wave.  Lane l: keys l % 16 and
 // 16 + l % 16, every fourth chunk of a row.  Whole tiles are read at constant offsets
@@ -119,7 +67,7 @@ template <int DH, bool MASK> struct TileBf16 {
 #pragma unroll
     for (int i = 0; i < 2 * KS; ++i) {
       const bool left = !some || (bits >> row(i) & 1);
-      ValueRows<DH>::put(rows, row(i), lane % NC, left ? v[i / KS][i % KS] : bf16x8{});
+      LdsRows<DH>::put(rows, row(i), lane % NC, left ? v[i / KS][i % KS] : bf16x8{});
     }
   }
 };
@@ -180,7 +128,7 @@ template <int DH, bool MASK> struct TileKv4 {
       const float s = kv4_scale(left ? vb[t] : 127);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        ValueRows<DH>::put(rows, row, DH / 32 * (lane >> 4) + ks, kv4_decode8(left ? v[t][ks] : 0, s));
+        LdsRows<DH>::put(rows, row, DH / 32 * (lane >> 4) + ks, kv4_decode8(left ? v[t][ks] : 0, s));
     }
   }
 };
@@ -188,7 +136,7 @@ template <int DH, bool MASK> struct TileKv4 {
 // NS: bf16 terms of a query and of a softmax weight (1: bf16; 3: fp32).
 template <typename T, int DH, int RT, int NS, bool MASK, typename Tile>
 __global__ __launch_bounds__(256, NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_xattn_rows(XAttnArgs a, FastDiv by_blocks) {
-  typedef ValueRows<DH> Rows;
+  typedef LdsRows<DH> Rows;
   constexpr int NW = 4, KS = DH / 32, NCT = DH / 16, OLD = DH + 4, KEYS = Tile::KEYS;
   constexpr uint64_t FULL = (1ull << KEYS) - 1;
   constexpr int WAVE_LDS = KEYS * Rows::BYTES;
@@ -221,13 +169,13 @@ __global__ __launch_bounds__(256, NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_
       if constexpr (NS == 1) {
         qf[0][rt][ks] = *reinterpret_cast<const bf16x8*>(p);
       } else {
+        float x[8];
+        bf16x8 t[NS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          bf16 t[NS];
-          split_bf16<NS>((float)p[i], t);
+        for (int i = 0; i < 8; ++i) x[i] = (float)p[i];
+        split_bf16<NS>(x, t);
 #pragma unroll
-          for (int n = 0; n < NS; ++n) qf[n][rt][ks][i] = t[n];
-        }
+        for (int n = 0; n < NS; ++n) qf[n][rt][ks] = t[n];
       }
     }
   }
@@ -303,16 +251,13 @@ __global__ __launch_bounds__(256, NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_
         p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i / 4][rt][i % 4], a.scale_log2, -m_use));
       // terms of the weights, which are summed as rounded
       const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
+      bf16x8 t[NS];
+      split_bf16<NS>(p, t);
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
+        pf[n][rt] = t[n];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pf[n][rt][i] = (bf16)p[i];
-#pragma unroll
-        for (int i = 0; i < 8; i += 2)
-          lsum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[n][rt][i], pf[n][rt][i + 1]}, one, lsum, false);
-        if (n + 1 < NS)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] -= (float)pf[n][rt][i];
+        for (int i = 0; i < 8; i += 2) lsum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{t[n][i], t[n][i + 1]}, one, lsum, false);
       }
       l_run[rt] += lsum;
     }

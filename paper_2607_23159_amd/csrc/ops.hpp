@@ -65,10 +65,12 @@ size_t xattn_workspace(const cs_attn_desc& d, bool kv4);
 template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStream_t st);
 
 // The kernels' launchers: few rows (k_xattn_rows.hip), many rows in bf16
-// (k_xattn_tile.hip), fp32 (k_xattn_f32.hip), and the join of the parts.
+// (k_xattn_tile.hip), fp32 in few and in many workgroups (k_xattn_f32.hip,
+// k_xattn_split.hip).
 template <typename T> hipError_t xattn_rows(const XAttnArgs& a, bool kv4, hipStream_t st);
 hipError_t xattn_tile(const XAttnArgs& a, hipStream_t st);
 hipError_t xattn_f32(const XAttnArgs& a, hipStream_t st);
+hipError_t xattn_split(const XAttnArgs& a, hipStream_t st);
 
 // Keys of the context of query set i, and the context's index (0 keys if kv_of is out
 // of range).  i is wave-uniform; the index tensors are only read by these kernels, so

@@ -244,6 +244,11 @@ ATTN = [  # dtype, n_q, n_kv, lq, lk, hq, hkv, dim, lengths, mask
     (FP, 1, 2, 40, 1100, 2, 2, 32, "ragged", "none"),
     (FP, 5, 3, 8, 2600, 16, 4, 128, "ragged", "none"),
     (FP, 2, 2, 1100, 150, 4, 4, 64, "ragged", "holes"),
+    (FP, 3, 2, 1030, 77, 8, 8, 128, "ragged", "none"),
+    (FP, 3, 2, 700, 300, 12, 12, 32, "strange", "empty"),
+    (FP, 2, 2, 350, 60, 48, 12, 64, "ragged", "holes"),
+    (FP, 1, 1, 1030, 4200, 8, 8, 32, "full", "holes"),
+    (FP, 2, 2, 100, 1100, 96, 96, 32, "ragged", "none"),
 ]
 
 
@@ -380,7 +385,7 @@ def test_scores_far_apart(dtype, lq, lk, g):
 @pytest.mark.parametrize("kv4", [False, True])
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq,lk,hq,hkv,dim", [(1, 4000, 8, 2, 128), (5, 600, 12, 12, 64), (333, 512, 4, 4, 128),
-                                              (1000, 77, 6, 3, 32)])
+                                              (1000, 77, 6, 3, 32), (1100, 600, 8, 8, 64)])
 def test_attention_does_not_depend_on_the_batch(kv4, dtype, lq, lk, hq, hkv, dim):
     n = 6
     q = rnd(1, n, lq, hq, dim, dtype=dtype).cuda()
@@ -404,6 +409,33 @@ def test_attention_does_not_depend_on_the_batch(kv4, dtype, lq, lk, hq, hkv, dim
     for i in range(n):
         assert torch.equal(call(q[i:i + 1], of[i:i + 1]), whole[i:i + 1]), i
     assert torch.equal(call(q, of), whole)
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lq,lk,g", [(7, 1200, 4), (60, 300, 3), (400, 200, 1), (1100, 70, 8)])
+def test_a_query_of_nans_leaves_the_others(kv4, dtype, lq, lk, g):
+    q = rnd(1, 1, lq, 8, 64, dtype=dtype).cuda()
+    k, v = rnd(2, 1, lk, 8 // g, 64, dtype=dtype).cuda(), rnd(3, 1, lk, 8 // g, 64, dtype=dtype).cuda()
+    cache = _cache(1, 8 // g, lk, 64)
+    B.cs_kv4_store(cache, k.flatten(0, 1), v.flatten(0, 1))
+
+    def call(qq):
+        o = torch.empty_like(qq)
+        if kv4:
+            d = B.kv4_attn_desc(qq, cache, o)
+            B.cs_kv4_attention(d, qq, cache, o, work=_work(B.cs_kv4_attention_workspace(d))[0])
+        else:
+            d = B.attn_desc(qq, k, v, o)
+            B.cs_cross_attention(d, qq, k, v, o, work=_work(B.cs_cross_attention_workspace(d))[0])
+        return o
+
+    whole = call(q)
+    q[0, 3, 5] = math.nan
+    got = call(q)
+    assert got[0, 3, 5].isnan().all()
+    got[0, 3, 5] = whole[0, 3, 5]
+    assert torch.equal(got, whole)
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
