@@ -285,7 +285,8 @@ cs_status cs_rollout_import(cs_rollout* r, const void* buf, size_t bytes);
  *    is the type of the floating tensors.  Strides are counted in elements;
  *    the channels of a head are contiguous.  Rows are moved 16 bytes at a
  *    time: tensor pointers are 16-byte aligned and strides multiples of 16
- *    bytes (CS_E_INVAL otherwise).  Strides are not negative.
+ *    bytes (CS_E_INVAL otherwise).  Strides are not negative; an output's
+ *    are not zero either, where its axis has several entries.
  *  - The work is enqueued on `stream` (hipStream_t or NULL); nothing is
  *    allocated, copied or waited for, so calls can be captured into a HIP
  *    graph.  Descriptors are read before the call returns.  Tensors must
@@ -335,8 +336,9 @@ cs_status cs_qk_norm_rope(const cs_qk_norm_desc* desc, const void* q, const void
  * contexts of up to lk keys and values.  heads_q is a multiple of heads_kv: query
  * head h reads key head h / (heads_q / heads_kv).  head_dim 32, 64 or 128.
  * Strides: set or context (_b), row (_r) and head (_h); mask_b is the stride of
- * the mask from context to context (bytes, any alignment).  scale > 0 multiplies
- * the products q.k. */
+ * the mask from context to context (bytes, any alignment).  scale, in (0, 1e38),
+ * multiplies the products q.k; scores of 10^9 and more in magnitude are not
+ * supported (the softmax subtracts rounded maxima). */
 typedef struct {
   int32_t dtype;                 /* cs_dtype of q, o (and k, v) */
   int32_t n_q, n_kv, lq, lk;

@@ -31,6 +31,13 @@ static cs_status check_stride(long s, long n, int esz, const char* name) {
   return CS_OK;
 }
 
+// The same of an output: its entries lie apart.
+static cs_status check_out_stride(long s, long n, int esz, const char* name) {
+  TRY(check_stride(s, n, esz, name));
+  CHECK(n <= 1 || s > 0, CS_E_INVAL, "output stride %s must be positive", name);
+  return CS_OK;
+}
+
 extern "C" {
 
 cs_status cs_qk_norm_rope(const cs_qk_norm_desc* d, const void* q, const void* k, void* q_out, void* k_out,
@@ -53,15 +60,15 @@ cs_status cs_qk_norm_rope(const cs_qk_norm_desc* d, const void* q, const void* k
     if (d->heads_q > 0) {
       TRY(check_stride(d->q_row, d->tokens, e, "q_row"));
       TRY(check_stride(d->q_head, d->heads_q, e, "q_head"));
-      TRY(check_stride(d->qo_row, d->tokens, e, "qo_row"));
-      TRY(check_stride(d->qo_head, d->heads_q, e, "qo_head"));
+      TRY(check_out_stride(d->qo_row, d->tokens, e, "qo_row"));
+      TRY(check_out_stride(d->qo_head, d->heads_q, e, "qo_head"));
       TRY(check_stride(d->q_gain_head, d->heads_q, 4, "q_gain_head"));
     }
     if (d->heads_k > 0) {
       TRY(check_stride(d->k_row, d->tokens, e, "k_row"));
       TRY(check_stride(d->k_head, d->heads_k, e, "k_head"));
-      TRY(check_stride(d->ko_row, d->tokens, e, "ko_row"));
-      TRY(check_stride(d->ko_head, d->heads_k, e, "ko_head"));
+      TRY(check_out_stride(d->ko_row, d->tokens, e, "ko_row"));
+      TRY(check_out_stride(d->ko_head, d->heads_k, e, "ko_head"));
       TRY(check_stride(d->k_gain_head, d->heads_k, 4, "k_gain_head"));
     }
     if (d->tokens == 0 || (d->heads_q == 0 && d->heads_k == 0)) return CS_OK;
@@ -109,10 +116,11 @@ static cs_status kv4_rows_call(const cs_kv4_cache* c, const cs_kv4_rows* r, cons
   CHECK(slots || (long)r->n_rows <= (long)c->n_kv * c->cap, CS_E_INVAL, "%d rows without slots, the cache has %ld",
         r->n_rows, (long)c->n_kv * c->cap);
   const int e = elem(r->dtype);
-  TRY(check_stride(r->k_row, r->n_rows, e, "k_row"));
-  TRY(check_stride(r->k_head, c->heads, e, "k_head"));
-  TRY(check_stride(r->v_row, r->n_rows, e, "v_row"));
-  TRY(check_stride(r->v_head, c->heads, e, "v_head"));
+  const auto check = store ? check_stride : check_out_stride;
+  TRY(check(r->k_row, r->n_rows, e, "k_row"));
+  TRY(check(r->k_head, c->heads, e, "k_head"));
+  TRY(check(r->v_row, r->n_rows, e, "v_row"));
+  TRY(check(r->v_head, c->heads, e, "v_head"));
   if (r->n_rows == 0) return CS_OK;
   TRY(check_tensor(store ? k : ko, "k"));
   TRY(check_tensor(store ? v : vo, "v"));
@@ -148,11 +156,15 @@ static cs_status check_attn(const cs_attn_desc* d, bool kv4) {
   CHECK(d->heads_q % d->heads_kv == 0, CS_E_INVAL, "heads_q must be a multiple of heads_kv");
   CHECK(d->head_dim == 32 || d->head_dim == 64 || d->head_dim == 128, CS_E_UNSUPPORTED,
         "head_dim must be 32, 64 or 128");
-  CHECK(d->scale > 0.0f && isfinite(d->scale), CS_E_INVAL, "scale must be finite and positive");
+  CHECK(d->scale > 0.0f && d->scale < 1e38f, CS_E_INVAL, "scale must be positive and below 1e38");
   CHECK(d->mask_b >= 0, CS_E_INVAL, "stride mask_b must not be negative");
   // rows of a set: queries x the heads that share a key head
   CHECK((long)d->lq * (d->heads_q / d->heads_kv) < (1L << 30) && d->lk < (1 << 30), CS_E_UNSUPPORTED,
         "lq x heads and lk must be below 2^30");
+  // what grids and workspaces are computed from stays in 64 bits
+  CHECK((double)d->n_q * d->heads_q * std::max(d->lq, 1) < 0x1p40, CS_E_UNSUPPORTED,
+        "too many queries and heads for one call");
+  CHECK(!kv4 || (double)d->n_kv * d->lk < 0x1p31, CS_E_UNSUPPORTED, "n_kv * lk must be below 2^31");
   // offsets inside a tile of keys are 32-bit byte counts
   CHECK(kv4 || d->lk <= 1 || (d->k_r <= (1 << 23) && d->v_r <= (1 << 23)), CS_E_UNSUPPORTED,
         "strides k_r and v_r must be at most 2^23");
@@ -164,9 +176,9 @@ static cs_status check_attn(const cs_attn_desc* d, bool kv4) {
   TRY(check_stride(d->q_b, d->n_q, e, "q_b"));
   TRY(check_stride(d->q_r, d->lq, e, "q_r"));
   TRY(check_stride(d->q_h, d->heads_q, e, "q_h"));
-  TRY(check_stride(d->o_b, d->n_q, e, "o_b"));
-  TRY(check_stride(d->o_r, d->lq, e, "o_r"));
-  TRY(check_stride(d->o_h, d->heads_q, e, "o_h"));
+  TRY(check_out_stride(d->o_b, d->n_q, e, "o_b"));
+  TRY(check_out_stride(d->o_r, d->lq, e, "o_r"));
+  TRY(check_out_stride(d->o_h, d->heads_q, e, "o_h"));
   if (!kv4) {
     TRY(check_stride(d->k_b, d->n_kv, e, "k_b"));
     TRY(check_stride(d->k_r, d->lk, e, "k_r"));

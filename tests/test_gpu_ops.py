@@ -439,6 +439,46 @@ def test_a_query_of_nans_leaves_the_others(kv4, dtype, lq, lk, g):
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lq,lk", [(1, 700), (40, 90), (1100, 130)])
+def test_inputs_that_are_broadcast(dtype, lq, lk):
+    """Strides of zero: one query set for all, keys of one head and one context for all."""
+    q, k, v = rnd(1, 1, lq, 8, 64, dtype=dtype), rnd(2, 1, lk, 1, 64, dtype=dtype), rnd(3, 2, lk, 1, 64, dtype=dtype)
+    lens = torch.tensor([lk, lk // 2 + 1], dtype=torch.int32)
+    full = q.expand(3, -1, -1, -1), k.expand(2, -1, 8, -1), v.expand(-1, -1, 8, -1)
+    of = _of(3, 2, False)
+    ref, bound = R.attention(full[0], full[1].double(), full[2].double(), 0.125, of, lens, None, dtype == BF)
+    q, k, v = q.cuda().expand(3, -1, -1, -1), k.cuda().expand(2, -1, 8, -1), v.cuda().expand(-1, -1, 8, -1)
+    o, check = guarded((3, lq, 8, 64), dtype)
+    d = B.attn_desc(q, k, v, o)
+    B.cs_cross_attention(d, q, k, v, o, of.cuda(), lens.cuda(), work=_work(B.cs_cross_attention_workspace(d))[0])
+    within(o, ref, bound, "o")
+    check()
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lq,lk,g", [(2, 1100, 4), (60, 300, 1), (1100, 70, 1)])
+def test_scores_of_a_billion(kv4, dtype, lq, lk, g):
+    """Scores up to 10^9 leave averages of the values: a weight's exponent is off by at most 64
+    (half a step of 2^30), the same for all keys of a maximum."""
+    q = rnd(1, 1, lq, 8, 64, dtype=dtype).cuda()
+    k, v = rnd(2, 1, lk, 8 // g, 64, dtype=dtype).cuda(), rnd(3, 1, lk, 8 // g, 64, dtype=dtype).cuda()
+    cache = _cache(1, 8 // g, lk, 64)
+    B.cs_kv4_store(cache, k.flatten(0, 1), v.flatten(0, 1))
+    o = torch.empty_like(q)
+    top = (q.double().abs().sum(-1).max() * 1.2 * k.abs().max()).item()   # a stored key is below 7 / 6 of the largest
+    if kv4:
+        d = B.kv4_attn_desc(q, cache, o, scale=1e9 / top)
+        B.cs_kv4_attention(d, q, cache, o, work=_work(B.cs_kv4_attention_workspace(d))[0])
+    else:
+        d = B.attn_desc(q, k, v, o, scale=1e9 / top)
+        B.cs_cross_attention(d, q, k, v, o, work=_work(B.cs_cross_attention_workspace(d))[0])
+    assert o.isfinite().all()
+    assert (o.abs().amax() <= (1.2 if kv4 else 1.01) * v.abs().amax()).item()
+    assert (o.abs().amax(-1) > 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq", [1, 150])
 def test_rows_more_than_two_gib_apart(dtype, lq):
     """Row offsets of a context pass 2^31 bytes."""

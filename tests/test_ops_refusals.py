@@ -193,3 +193,35 @@ def test_calls_too_large_for_a_grid():
         assert attn(attn_desc(heads_q=2, heads_kv=2, n_kv=1, q_b=8, o_b=8, q_r=8, o_r=8, q_h=8, o_h=8, **kw),
                     of=P) == B.CS_E_UNSUPPORTED
         assert "too many" in B.cs_last_error()
+
+
+def test_outputs_whose_entries_coincide():
+    for kw in (dict(qo_row=0), dict(qo_head=0), dict(ko_row=0)):
+        assert norm(norm_desc(**kw)) == B.CS_E_INVAL and "output stride" in B.cs_last_error()
+    for kw in (dict(o_b=0), dict(o_r=0), dict(o_h=0)):
+        assert attn(attn_desc(**kw)) == B.CS_E_INVAL and "output stride" in B.cs_last_error()
+    lib, n = B.lib(), C.c_size_t()
+    for kw in (dict(k_row=0), dict(v_row=0), dict(k_head=0), dict(v_head=0)):
+        r = rows(**kw)
+        assert lib.cs_kv4_load(C.byref(cache()), C.byref(r), P, P, None, None) == B.CS_E_INVAL
+        assert "output stride" in B.cs_last_error()
+    # of one entry, and of inputs, they may be zero
+    for d in (attn_desc(n_q=1, lq=1, q_b=0, q_r=0, o_b=0, o_r=0), attn_desc(q_b=0, k_b=0, v_b=0, k_h=0)):
+        assert lib.cs_cross_attention_workspace(C.byref(d), C.byref(n)) == B.CS_OK
+
+
+def test_sizes_whose_products_pass_64_bits():
+    big = 2 ** 31 - 1
+    lib, n = B.lib(), C.c_size_t(77)
+    for kw, word in ((dict(n_q=big, heads_q=big - 7, heads_kv=big - 7, lq=big // 2), "too many"),
+                     (dict(n_q=big, heads_q=2 ** 20, heads_kv=2 ** 20, lq=1), "too many")):
+        d = attn_desc(q_b=8, q_r=8, q_h=8, o_b=8, o_r=8, o_h=8, n_kv=big, lk=1, **kw)
+        assert lib.cs_cross_attention_workspace(C.byref(d), C.byref(n)) == B.CS_E_UNSUPPORTED and word in B.cs_last_error()
+        assert attn(d) == B.CS_E_UNSUPPORTED
+    d = attn_desc(n_kv=2 ** 20, lk=2 ** 20)
+    assert lib.cs_kv4_attention_workspace(C.byref(d), C.byref(n)) == B.CS_E_UNSUPPORTED and n.value == 77
+
+
+def test_scales_that_overflow():
+    for s in (1e38, 3.4e38):
+        assert attn(attn_desc(scale=s)) == B.CS_E_INVAL and "scale" in B.cs_last_error()
