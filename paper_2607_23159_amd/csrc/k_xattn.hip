@@ -189,6 +189,7 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
         l.c = a.c;
         const long hd = (long)a.d.heads_kv * a.d.head_dim;
         l.r = {a.d.dtype, a.d.n_kv * a.d.lk, hd, a.d.head_dim, hd, a.d.head_dim};
+        l.len = a.kv_len;
         l.ko = (char*)work + w.k;
         l.vo = (char*)work + w.v;
         e = kv4_load<T>(l, st);

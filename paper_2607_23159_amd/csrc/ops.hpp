@@ -36,6 +36,7 @@ struct Kv4RowsArgs {
   void *ko, *vo;         // loaded rows
   const int* slots;
   bool stream;           // loaded rows are not read again soon
+  const int* len;        // rows of each context, or NULL: further ones are skipped
 };
 template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
 template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);

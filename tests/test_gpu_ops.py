@@ -496,6 +496,31 @@ def test_rows_more_than_two_gib_apart(dtype, lq):
         within(o, ref, bound, "o")
 
 
+@pytest.mark.parametrize("dtype,lq", [(BF, 1), (BF, 200), (FP, 3), (FP, 150)])
+def test_cache_rows_past_four_gib(dtype, lq):
+    """Heads of the cache lie 4 GiB apart; only the first rows of the contexts are in use."""
+    n, h, cap, dim, used = 2, 2, 1 << 26, 128, torch.tensor([130, 77], dtype=torch.int32)
+    cache = B.Kv4Cache(*(torch.empty(n, h, cap, w, dtype=torch.uint8, device="cuda") for w in (64, 4, 64, 4)))
+    k, v = rnd(2, n * 130, h, dim, dtype=dtype), rnd(3, n * 130, h, dim, dtype=dtype)
+    slots = torch.cat([torch.arange(130), cap + torch.arange(130)]).int()
+    B.cs_kv4_store(cache, k.cuda(), v.cuda(), slots.cuda())
+    kk, vv = torch.empty_like(k).cuda(), torch.empty_like(v).cuda()
+    B.cs_kv4_load(cache, kk, vv, slots.cuda())
+    kk, vv = kk.cpu(), vv.cpu()
+    for x, y in ((k, kk), (v, vv)):
+        want = R.dequantise(*R.quantise(x.transpose(0, 1)))
+        assert torch.equal(y.transpose(0, 1).double(), want)
+    q = rnd(1, n, lq, h, dim, dtype=dtype)
+    ref, bound = R.attention(q, kk.double().view(n, 130, h, dim), vv.double().view(n, 130, h, dim), 1 / math.sqrt(dim), None,
+                             used, None, dtype == BF)
+    q = q.cuda()
+    o = torch.empty_like(q)
+    d = B.kv4_attn_desc(q, cache, o)
+    work = torch.empty(max(1, B.cs_kv4_attention_workspace(d)), dtype=torch.uint8, device="cuda")
+    B.cs_kv4_attention(d, q, cache, o, kv_len=used.cuda(), work=work)
+    within(o, ref, bound, "o")
+
+
 # --------------------------------------------------------- as they are used together
 def _decode_step(dtype, n=3, hq=8, hkv=2, dim=128, cap=300):
     """The operators of one generated token: norms and rotation of q and k, the new row into the
