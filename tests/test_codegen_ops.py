@@ -23,8 +23,8 @@ def test_tile_attention_waits_once_a_tile(kernels, head_dim, waves, masked):  # 
     occ = 3 if waves == 12 else 2
     for name, code in _named(kernels, f"k_xattn_tileILi{head_dim}ELi{waves}ELi{occ}ELb{masked}E").items():
         barriers = [n for n, i in enumerate(code) if i.startswith("s_barrier")]
-        assert len(barriers) == 1, name
-        tile = code[barriers[0]:]
+        assert len(barriers) == 2, name            # the order of the sets; the tiles
+        tile = code[barriers[-1]:]
         reads = [n for n, i in enumerate(tile) if i.startswith("ds_read_b64_tr_b16")]
         tile = tile[:reads[-1]]
         assert any(map(_is_mfma, tile)) and any(map(_is_direct_load, tile[:reads[0]])), name

@@ -230,6 +230,8 @@ ATTN = [  # dtype, n_q, n_kv, lq, lk, hq, hkv, dim, lengths, mask
     (BF, 7, 4, 2500, 70, 12, 12, 64, "ragged", "none"),
     (BF, 3, 2, 900, 330, 12, 12, 128, "ragged", "holes"),
     (BF, 2, 2, 200, 1500, 8, 4, 128, "ragged", "none"),
+    (BF, 70, 3, 300, 60, 4, 4, 64, "ragged", "none"),
+    (BF, 64, 5, 270, 90, 4, 4, 32, "strange", "holes"),
     (BF, 5, 3, 8, 2600, 16, 4, 128, "ragged", "none"),
     (BF, 3, 2, 21, 1100, 3, 1, 64, "ragged", "holes"),
     (BF, 2, 2, 64, 1030, 3, 1, 32, "strange", "none"),
