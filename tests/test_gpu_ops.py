@@ -612,3 +612,46 @@ def test_two_streams_with_a_workspace_each():
     torch.cuda.synchronize()
     for (s, _), w in zip(pairs, want):
         assert torch.equal(s["o"], w)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_two_graphs_that_share_a_workspace(dtype):
+    """One after the other on one stream: a workspace carries nothing from call to call.  Joined
+    parts of keys, unpacked rows (bf16) and shapes of more than a round of workgroups."""
+    lens = torch.tensor([1200, 0, 700], dtype=torch.int32, device="cuda")
+    calls = []
+    for seed, (lq, kv4) in enumerate([(2, False), (2, True), (300, True), (1100, False)]):
+        q = rnd(seed, 3, lq, 8, 128, dtype=dtype).cuda()
+        k, v = rnd(10 + seed, 3, 1200, 8, 128, dtype=dtype).cuda(), rnd(20 + seed, 3, 1200, 8, 128, dtype=dtype).cuda()
+        o = torch.empty_like(q)
+        if kv4:
+            cache = _cache(3, 8, 1200, 128)
+            B.cs_kv4_store(cache, k.flatten(0, 1), v.flatten(0, 1))
+            d = B.kv4_attn_desc(q, cache, o)
+            need = B.cs_kv4_attention_workspace(d)
+            call = lambda w, st=None, d=d, q=q, c=cache, o=o: B.cs_kv4_attention(d, q, c, o, None, lens, None, w, st)
+        else:
+            d = B.attn_desc(q, k, v, o)
+            need = B.cs_cross_attention_workspace(d)
+            call = lambda w, st=None, d=d, q=q, k=k, v=v, o=o: B.cs_cross_attention(d, q, k, v, o, None, lens, None, w, st)
+        calls.append((call, o, need))
+    work = torch.empty(max(1, max(need for _, _, need in calls)), dtype=torch.uint8, device="cuda")
+    want, graphs, side = [], [], torch.cuda.Stream()
+    for call, o, need in calls:
+        call(torch.empty(max(1, need), dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        want.append(o.clone())
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call(work, side)
+        graphs.append(graph)
+    for i in range(3):
+        for _, o, _ in calls:
+            o.fill_(7.0)
+        work.random_(0, 256)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, o, _), w in zip(calls, want):
+            assert torch.equal(o, w), i
