@@ -33,7 +33,7 @@ CS_DEV void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }     // lgkmcnt 0
 
 // One item of work: 32 NW rows of one part of a problem.
 struct TileItem {
-  int set, head, part, pr, r0, k0, k1;
+  int set, head, part, r0, k0, k1;
   const bf16 *kb, *vb;
   const uint8_t* mask;
 };
@@ -64,7 +64,7 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
   };
   // f(i, offset) of row i * RPI + lane / CPS of this wave, i = 0 .. SI - 1: one step apart
   // where every query is a row and none lies past the last
-  auto each_row = [&](const TileItem& it, long stride_r, long stride_h, auto f) {
+  auto each_row = [&](const TileItem& it, int lane, long stride_r, long stride_h, auto f) {
     if (a.group == 1 && it.r0 + wave * 32 + 32 <= a.rows) {
       const long at = (long)(it.r0 + wave * 32 + lane / CPS) * (int)stride_r + (long)it.head * (int)stride_h;
 #pragma unroll
@@ -96,7 +96,8 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
 
   // The next item of this workgroup with keys to read, from index i on; items without
   // any get their zeros (in parts: nothing, the join does not read them).  Rows past
-  // the last are copies of it, here and below: they are stored to the same place.
+  // the last are copies of it: every load is in bounds, and the last row gets its zeros
+  // several times.
   const int place = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // an XCD takes neighbouring items
   auto find = [&](int& i, TileItem& it) {
     for (;; ++i) {
@@ -104,14 +105,11 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
       const int id = i * (int)gridDim.x + (i & 1 ? (int)gridDim.x - 1 - place : place);
       if (id >= n_items) return false;
       const int n = by_qt.div(id), qt = id - n * by_qt.d;
-      it.pr = a.by_parts.div(n);
-      it.part = n - it.pr * a.parts;
-      it.set = a.by_heads.div(it.pr);
-      it.head = it.pr - it.set * a.d.heads_kv;
-      if (sorted) {
-        it.set = __builtin_amdgcn_readfirstlane(s_order[it.set]);
-        it.pr = it.set * a.d.heads_kv + it.head;
-      }
+      const int pr = a.by_parts.div(n);
+      it.part = n - pr * a.parts;
+      it.set = a.by_heads.div(pr);
+      it.head = pr - it.set * a.d.heads_kv;
+      if (sorted) it.set = __builtin_amdgcn_readfirstlane(s_order[it.set]);
       it.r0 = qt * NW * 32;
       int len;
       const int ctx = xattn_context(a, it.set, &len);
@@ -160,7 +158,7 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
   frag qf[NKS];   // between load_q and turn_q: the rows as they come from memory
   auto load_q = [&](const TileItem& it) {
     const bf16* src = (const bf16*)a.q + it.set * a.d.q_b + 8 * (lane % CPS);
-    each_row(it, a.d.q_r, a.d.q_h, [&](int i, long at) {
+    each_row(it, lane, a.d.q_r, a.d.q_h, [&](int i, long at) {
 #pragma unroll
       for (int s = 0; s < NSEG; ++s) qf[s * SI + i] = MF::load(src + at + s * (SEG / 2));
     });
@@ -343,33 +341,51 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
     // behind this wait then drain under its work
     wait_loads();
     mask_here = mask_next;
+    // Only rows that exist are stored: a copy of the last row in another wave may hold
+    // another maximum than the row itself, and with it other sums and outputs.
+    const int live = a.rows - cur.r0 - wave * 32;   // rows of this wave that exist
     const float l_tot = l_run + __shfl_xor(l_run, 32, WAVE);
+    // the lane's number, formed anew: what follows from it is then not kept in registers
+    // over the products (the masked and the 12-wave variants spill for it)
+    int here = 0;
+    asm volatile("" : "+v"(here));
+    here = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, here));
     if (a.parts > 1) {
-      const long at = ((long)cur.pr * a.parts + cur.part) * a.rows + min(cur.r0 + wave * 32 + l32, a.rows - 1);
-      float* dst = a.part_o + at * DH + 4 * half;
+      const int pr = cur.set * a.d.heads_kv + cur.head;
+      const long at = ((long)pr * a.parts + cur.part) * a.rows + cur.r0 + wave * 32 + (here & 31);
+      float* dst = a.part_o + at * DH + 4 * (here >> 5);
+      if ((here & 31) < live) {
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
+        for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4*>(dst + dt * 32 + 8 * g) =
-              f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
-      if (half == 0) a.part_ml[at] = make_float2(m_run, l_tot);
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4*>(dst + dt * 32 + 8 * g) =
+                f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+        if (here < 32) a.part_ml[at] = make_float2(m_run, l_tot);
+      }
     } else {
       const float inv = l_tot != 0.0f ? 1.0f / l_tot : 0.0f;
-      bf16* dst = (bf16*)a.o + cur.set * a.d.o_b + 8 * (lane % CPS);
+      bf16* dst = (bf16*)a.o + cur.set * a.d.o_b + 8 * (here % CPS);
       constexpr int DPS = NDT / NSEG;   // 32-channel blocks of a segment
       long at[SI];
-      each_row(cur, a.d.o_r, a.d.o_h, [&](int i, long x) { at[i] = x; });
+      each_row(cur, here, a.d.o_r, a.d.o_h, [&](int i, long x) { at[i] = x; });
 #pragma unroll
       for (int s = 0; s < NSEG; ++s) {
         f32x16 os[DPS];
 #pragma unroll
         for (int d = 0; d < DPS; ++d) os[d] = o[s * DPS + d];
         store_o_rows(os, inv, reinterpret_cast<bf16*>(seg + l32 * SRS), half, true);
+        frag y[SI];
 #pragma unroll
-        for (int i = 0; i < SI; ++i)
-          *reinterpret_cast<frag*>(dst + at[i] + s * (SEG / 2)) =
-              *reinterpret_cast<const frag*>(seg + (i * RPI + lane / CPS) * SRS + 16 * (lane % CPS));
+        for (int i = 0; i < SI; ++i) y[i] = *reinterpret_cast<const frag*>(seg + (i * RPI + here / CPS) * SRS + 16 * (here % CPS));
+        if (live >= 32) {
+#pragma unroll
+          for (int i = 0; i < SI; ++i) *reinterpret_cast<frag*>(dst + at[i] + s * (SEG / 2)) = y[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < SI; ++i)
+            if (i * RPI + here / CPS < live) *reinterpret_cast<frag*>(dst + at[i] + s * (SEG / 2)) = y[i];
+        }
       }
     }
     if (!more) return;

@@ -384,6 +384,50 @@ def test_scores_far_apart(dtype, lq, lk, g):
     within(o, ref, bound, "o")
 
 
+def _ramps(n, lq, lk, hq, hkv, dim, dtype):
+    """Scores up to the hundreds: the running maxima move in many tiles, in others for other queries."""
+    q = rnd(1, n, lq, hq, dim, dtype=dtype)
+    k, v = rnd(2, n, lk, hkv, dim, dtype=dtype), rnd(3, n, lk, hkv, dim, dtype=dtype)
+    ramp = torch.linspace(0.02, 30, lk)[None, :, None, None]
+    k = (k * torch.cat([ramp, ramp.flip(1), 30 - (ramp - 15).abs()], 0)[:n]).to(dtype)
+    return q, k, v
+
+
+def _attend(kv4, q, k, v, index=None, lens=None):
+    """Attention of device tensors, k and v through a 4-bit cache if kv4."""
+    o = torch.empty_like(q)
+    if kv4:
+        cache = _cache(k.shape[0], k.shape[2], k.shape[1], k.shape[3])
+        B.cs_kv4_store(cache, k.flatten(0, 1), v.flatten(0, 1))
+        d = B.kv4_attn_desc(q, cache, o)
+        B.cs_kv4_attention(d, q, cache, o, index, lens, work=_work(B.cs_kv4_attention_workspace(d))[0])
+    else:
+        d = B.attn_desc(q, k, v, o)
+        B.cs_cross_attention(d, q, k, v, o, index, lens, work=_work(B.cs_cross_attention_workspace(d))[0])
+    return o
+
+
+@pytest.mark.parametrize("dtype,kv4", [(BF, False), (BF, True), (FP, False), (FP, True)])
+@pytest.mark.parametrize("lq,lk,dim", [(40, 1100, 64), (64, 1100, 128), (300, 1100, 64), (200, 1300, 32), (1130, 330, 64),
+                                       (1060, 100, 128)])
+def test_the_last_row_where_waves_lie_past_it(dtype, kv4, lq, lk, dim):
+    """Rows that are no whole number of workgroups, in parts and over whole contexts: what a workgroup
+    computes past the last row leaves that row as it is, alone and among other sets."""
+    q, k, v = _ramps(3, lq, lk, 2, 2, dim, dtype)
+    kk, vv = k.double(), v.double()
+    if kv4:
+        kk, vv = (R.dequantise(*R.quantise(x)) for x in (k, v))
+    ref, bound = R.attention(q, kk, vv, 1 / math.sqrt(dim), None, None, None, dtype == BF)
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    whole = _attend(kv4, q, k, v)
+    within(whole, ref, bound, "o")
+    for _ in range(3):
+        for i in range(3):
+            alone = _attend(kv4, q[i:i + 1], k, v, torch.tensor([i], dtype=torch.int32, device="cuda"))
+            assert torch.equal(alone[0], whole[i]), i
+        assert torch.equal(_attend(kv4, q, k, v), whole)
+
+
 @pytest.mark.parametrize("kv4", [False, True])
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq,lk,hq,hkv,dim", [(1, 4000, 8, 2, 128), (5, 600, 12, 12, 64), (333, 512, 4, 4, 128),
