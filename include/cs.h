@@ -295,8 +295,11 @@ cs_status cs_rollout_import(cs_rollout* r, const void* buf, size_t bytes);
  *  - A workspace (16-byte aligned, at least the size the _workspace function
  *    gives) carries nothing from one call to the next, but calls that may
  *    overlap (two streams, two graphs) need one each.
- *  - Results do not depend on the batch: a token, or a query with its
- *    context, gives bitwise the same output alone and among others. */
+ *  - Results do not depend on the batch: a token, or a query set with its
+ *    context, gives bitwise the same output alone and among others, and a
+ *    query's output does not depend on the values of its set's other queries.
+ *    Calls of another lq, lk or number of heads may take other kernels or
+ *    cut the keys elsewhere: the same query then agrees to rounding. */
 
 /* Pairs a rotation turns: adjacent channels (2p, 2p + 1), or the first and
  * the second half of the rotated channels (p, p + rot_dim / 2). */

@@ -101,8 +101,9 @@ template <int DH, bool MASK> __global__ __launch_bounds__(256, 1) void k_xattn_f
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[0][r]);
     mx = max_lane_pair32(mx) * a.scale_log2;
-    if (__any(mx > m_run + 8.0f)) {   // see k_xattn_rows
-      const float m_new = fmaxf(m_run, mx);
+    const bool moves = mx > m_run + 8.0f;   // see k_xattn_rows
+    if (__any(moves)) {
+      const float m_new = moves ? mx : m_run;
       const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;

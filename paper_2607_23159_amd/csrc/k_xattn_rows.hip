@@ -241,9 +241,11 @@ __global__ __launch_bounds__(256, NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_
 #pragma unroll
         for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[t][rt][j]);
       mx = max_groups16(mx) * a.scale_log2;
-      // the maximum moves only when it must: weights up to 2^8 lose nothing in fp32
-      if (__any(mx > m_run[rt] + 8.0f)) {
-        const float m_new = fmaxf(m_run[rt], mx);
+      // a row's maximum moves only when it must (weights up to 2^8 lose nothing in fp32), and
+      // by the row's own scores alone: a query's output does not depend on the others
+      const bool moves = mx > m_run[rt] + 8.0f;
+      if (__any(moves)) {
+        const float m_new = moves ? mx : m_run[rt];
         // nothing seen yet: the sums are zero whatever the factor, which must not be NaN
         const float alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
         m_run[rt] = m_new;

@@ -144,8 +144,9 @@ template <int DH, bool MASK> __global__ __launch_bounds__(256, 2) void k_xattn_s
 #pragma unroll
         for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[t][rt][j]);
       mx = max_groups16(mx) * a.scale_log2;
-      if (__any(mx > m_run[rt] + 8.0f)) {   // see k_xattn_rows
-        const float m_new = fmaxf(m_run[rt], mx);
+      const bool moves = mx > m_run[rt] + 8.0f;   // see k_xattn_rows
+      if (__any(moves)) {
+        const float m_new = moves ? mx : m_run[rt];
         const float alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
         m_run[rt] = m_new;
         l_run[rt] *= alpha;

@@ -280,10 +280,11 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kt][r]);
     mx = max_lane_pair32(mx) * a.scale_log2;
+    const bool moves = mx > m_run + 8.0f;   // see k_xattn_rows
     if (kv0 == cur.k0) {   // nothing seen yet: nothing to scale
       m_run = mx;
-    } else if (__any(mx > m_run + 8.0f)) {   // see k_xattn_rows
-      const float m_new = fmaxf(m_run, mx);
+    } else if (__any(moves)) {
+      const float m_new = moves ? mx : m_run;
       const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;
@@ -341,8 +342,7 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
     // behind this wait then drain under its work
     wait_loads();
     mask_here = mask_next;
-    // Only rows that exist are stored: a copy of the last row in another wave may hold
-    // another maximum than the row itself, and with it other sums and outputs.
+    // Only rows that exist are stored: nothing is written by two waves.
     const int live = a.rows - cur.r0 - wave * 32;   // rows of this wave that exist
     const float l_tot = l_run + __shfl_xor(l_run, 32, WAVE);
     // the lane's number, formed anew: what follows from it is then not kept in registers

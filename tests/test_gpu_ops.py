@@ -484,6 +484,21 @@ def test_a_query_of_nans_leaves_the_others(kv4, dtype, lq, lk, g):
     assert torch.equal(got, whole)
 
 
+@pytest.mark.parametrize("dtype,kv4", [(BF, False), (BF, True), (FP, False), (FP, True)])
+@pytest.mark.parametrize("lq,lk,hq,hkv", [(7, 1200, 8, 2), (3, 400, 8, 2), (20, 300, 6, 2), (300, 200, 2, 2), (300, 1100, 2, 2),
+                                          (1100, 330, 2, 2), (1100, 200, 8, 8)])
+def test_a_query_does_not_depend_on_the_other_queries(dtype, kv4, lq, lk, hq, hkv):
+    """Bitwise, where the others' running maxima move at other keys than its own."""
+    q, k, v = _ramps(1, lq, lk, hq, hkv, 64, dtype)
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    whole = _attend(kv4, q, k, v)
+    keep = torch.arange(lq, device="cuda") % 3 == 1
+    for scale in (0.0, 3.0):
+        other = (scale * rnd(7, 1, lq, hq, 64)).to(dtype).cuda()
+        other[:, keep] = q[:, keep]
+        assert torch.equal(_attend(kv4, other, k, v)[:, keep], whole[:, keep]), scale
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq,lk", [(1, 700), (40, 90), (1100, 130)])
 def test_inputs_that_are_broadcast(dtype, lq, lk):
