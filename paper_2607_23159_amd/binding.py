@@ -392,7 +392,9 @@ def cs_rank(s_cached: Sequence[float], s_full: Optional[Sequence[float]]):
 # --------------------------------------------------------------- operators
 # Descriptors are made once from tensors and kept; a call then takes tensors of
 # the same shape, strides, type and device (or raw addresses, unchecked).  Tensors
-# must be on the current device.
+# must be on the current device.  stream: a torch stream or a raw handle; None is
+# torch's current stream, so that calls follow what torch enqueued before them and can
+# be captured by torch.cuda.graph.
 _DTYPES = {"bfloat16": CS_BF16, "float32": CS_FP32}
 
 
@@ -413,6 +415,14 @@ def _on_current(device) -> None:
     import torch
     if device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _op_stream(s, device) -> Optional[int]:
+    if s is not None:
+        return _stream(s)
+    import torch
+    # the call behind torch.cuda.current_stream(device).cuda_stream, without its objects
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _aux(x, numel: int, dtype: str, name: str, device) -> Optional[int]:
@@ -503,7 +513,7 @@ def cs_qk_norm_rope(desc: _OpDesc, q, k, q_out, k_out, q_gain, k_gain, rope=None
                                  _same(q_gain, s["q_gain"], "q_gain"), _same(k_gain, s["k_gain"], "k_gain"),
                                  _same(rope, s["rope"], "rope"),
                                  _aux(pos, desc.c.tokens, "int32", "pos", desc.device),
-                                 _stream(stream)))
+                                 _op_stream(stream, desc.device)))
 
 
 class Kv4Cache(_OpDesc):
@@ -544,7 +554,7 @@ def cs_kv4_store(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
     _on_current(cache.device)
     d = cache.rows(k, v)
     _check(lib().cs_kv4_store(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _aux(slots, d.c.n_rows, "int32", "slots", cache.device),
-                              _stream(stream)))
+                              _op_stream(stream, cache.device)))
 
 
 def cs_kv4_load(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
@@ -552,7 +562,7 @@ def cs_kv4_load(cache: Kv4Cache, k, v, slots=None, stream=None) -> None:
     _on_current(cache.device)
     d = cache.rows(k, v)
     _check(lib().cs_kv4_load(cache.ref, d.ref, k.data_ptr(), v.data_ptr(), _aux(slots, d.c.n_rows, "int32", "slots", cache.device),
-                             _stream(stream)))
+                             _op_stream(stream, cache.device)))
 
 
 def _attn_desc(q, o, n_kv, lk, heads_kv, dim, kv_strides, scale, sig) -> _OpDesc:
@@ -618,7 +628,7 @@ def cs_cross_attention(desc: _OpDesc, q, k, v, o, kv_of=None, kv_len=None, kv_ma
     s = desc.sig
     of, ln, mask, w, nbytes = _attn_rest(desc, kv_of, kv_len, kv_mask, work)
     _check(lib().cs_cross_attention(desc.ref, _same(q, s["q"], "q"), _same(k, s["k"], "k"), _same(v, s["v"], "v"), of, ln,
-                                    mask, _same(o, s["o"], "o"), w, nbytes, _stream(stream)))
+                                    mask, _same(o, s["o"], "o"), w, nbytes, _op_stream(stream, desc.device)))
 
 
 def cs_kv4_attention(desc: _OpDesc, q, cache: Kv4Cache, o, kv_of=None, kv_len=None, kv_mask=None, work=None,
@@ -629,7 +639,7 @@ def cs_kv4_attention(desc: _OpDesc, q, cache: Kv4Cache, o, kv_of=None, kv_len=No
     s = desc.sig
     of, ln, mask, w, nbytes = _attn_rest(desc, kv_of, kv_len, kv_mask, work)
     _check(lib().cs_kv4_attention(desc.ref, _same(q, s["q"], "q"), cache.ref, of, ln, mask, _same(o, s["o"], "o"), w,
-                                  nbytes, _stream(stream)))
+                                  nbytes, _op_stream(stream, desc.device)))
 
 
 def cs_profile_enable(model: int, on: bool) -> None:

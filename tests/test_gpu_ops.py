@@ -674,6 +674,41 @@ def test_two_streams_with_a_workspace_each():
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
+def test_without_a_stream_calls_go_to_the_current_one(dtype):
+    """Behind what torch enqueued on it, and into a graph that is being captured on it."""
+    s, step = _decode_step(dtype)
+    x0 = s["x"].clone()
+    step()
+    torch.cuda.synchronize()
+    want = s["o"].clone()
+    a = rnd(5, 2048, 2048).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s["x"].fill_(9.0)
+        for _ in range(100):            # a while, behind which the input comes
+            a = a @ a * 1e-3
+        s["x"].copy_(x0)
+        step()
+        got = s["o"].clone()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for scale in (2.0, -1.0, 1.0):
+        s["x"].copy_(scale * x0)
+        s["o"].fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = s["o"].clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, s["o"])
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
 def test_two_graphs_that_share_a_workspace(dtype):
     """One after the other on one stream: a workspace carries nothing from call to call.  Joined
     parts of keys, unpacked rows (bf16) and shapes of more than a round of workgroups."""
