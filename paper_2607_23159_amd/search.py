@@ -28,6 +28,7 @@ class GpuModel:
     def __init__(self, cfg, weights: np.ndarray, dtype: Optional[int] = None, stream=None,
                  qk_norm: int = B.CS_QK_NORM_FULL):
         self.cfg = cfg
+        self.contexts = set()     # handles of its prompts, which are freed before it
         self.desc = B.model_desc(cfg, dtype)
         n = B.cs_model_weight_count(self.desc)
         if n != weights.size:
@@ -49,6 +50,9 @@ class GpuModel:
         return GpuPrompts(self, ctx, lens, kv_format)
 
     def close(self):
+        """Frees the model, and its prompts where they are still open."""
+        while self.contexts:
+            B.cs_context_free(self.contexts.pop())
         if self.h:
             B.cs_model_free(self.h)
             self.h = 0
@@ -64,8 +68,9 @@ class GpuPrompts:
     """The projected text of several prompts of a model (cs_context)."""
 
     def __init__(self, model: GpuModel, ctx: torch.Tensor, lens=None, kv_format: int = B.CS_KV_NATIVE):
-        self.model = model        # outlives its contexts
+        self.model = model        # kept alive; closing it closes its prompts
         self.h = B.cs_context_init(model.h, ctx, ctx.shape[0], lens, kv_format)
+        model.contexts.add(self.h)
 
     def velocity(self, x: torch.Tensor, t: float, prompt=None) -> torch.Tensor:
         """Velocities of the latents x, latent i attending to prompt[i] (None: prompt i)."""
@@ -75,7 +80,8 @@ class GpuPrompts:
         return v
 
     def close(self):
-        if self.h and self.model.h:
+        if self.h and self.h in self.model.contexts:
+            self.model.contexts.remove(self.h)
             B.cs_context_free(self.h)
         self.h = 0
 

@@ -168,6 +168,31 @@ def test_refusals_with_live_handles():
 
 
 @pytest.mark.parametrize("fmt", [B.CS_KV_NATIVE, B.CS_KV_4BIT])
+def test_closing_the_model_returns_its_prompts_memory(fmt):
+    m = synth.MODELS["tiny"]
+    flat = synth.make_weights(m)
+    ctx = torch.zeros(4096, m.text_len, m.text_dim, device="cuda")
+
+    def free():
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        return torch.cuda.mem_get_info()[0]
+    free()
+    gm = GpuModel(m, flat)
+    before = free()
+    ps = gm.prompts(ctx, None, fmt)
+    x = torch.from_numpy(synth.make_noise(m, 1).reshape(1, -1)).cuda()
+    ps.velocity(x, 0.5)
+    assert free() < before
+    gm.close()
+    assert free() >= before
+    with pytest.raises(B.CsError) as e:
+        ps.velocity(x, 0.5)
+    assert e.value.status == B.CS_E_INVAL
+    ps.close()
+
+
+@pytest.mark.parametrize("fmt", [B.CS_KV_NATIVE, B.CS_KV_4BIT])
 def test_context_out_of_memory(fmt):
     m, gm, _ = made("tiny", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
     ctx = torch.from_numpy(_prompts(m, 2)).cuda()
