@@ -618,6 +618,8 @@ def _attn_rest(desc: _OpDesc, kv_of, kv_len, kv_mask, work):
             raise ValueError(f"work: a contiguous tensor on {dev} is required")
         nbytes = work.numel() * work.element_size()
         work = work.data_ptr()
+    if kv_mask is not None and not isinstance(kv_mask, int) and kv_mask.dim() > 1 and kv_mask.shape[-1] != c.lk:
+        raise ValueError(f"kv_mask: rows of {kv_mask.shape[-1]} keys, {c.lk} required")
     return (_aux(kv_of, c.n_q, "int32", "kv_of", dev), _aux(kv_len, c.n_kv, "int32", "kv_len", dev),
             _aux(kv_mask, c.n_kv * c.lk, "uint8", "kv_mask", dev), work, nbytes)
 

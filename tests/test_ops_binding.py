@@ -73,3 +73,36 @@ def test_operators_run_on_the_current_stream_or_the_given_one(recorder):
         assert [n for n, _ in recorder.calls] == ["cs_qk_norm_rope", "cs_kv4_store", "cs_kv4_load", "cs_cross_attention",
                                                   "cs_kv4_attention"]
         assert [args[-1] for _, args in recorder.calls] == [want] * 5
+
+
+class FakeMask:
+    is_cuda, device, dtype = True, DEV, torch.uint8
+
+    def __init__(self, *shape):
+        self.shape = torch.Size(shape)
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+
+def test_a_mask_whose_rows_are_longer_than_the_contexts_is_refused(recorder):
+    """Its rows would be read lk apart, across its own."""
+    attn = _desc(B.cs_attn_desc(n_q=2, n_kv=2, lk=40), "q", "k", "v", "o")
+    for call in (lambda m: B.cs_cross_attention(attn, P, P, P, P, kv_mask=m),
+                 lambda m: B.cs_kv4_attention(attn, P, FakeCache(), P, kv_mask=m)):
+        for shape in ((2, 48), (40, 2), (2, 1, 80), (1, 2, 41), (1, 40), (79,)):
+            with pytest.raises(ValueError, match="kv_mask"):
+                call(FakeMask(*shape))
+        recorder.calls.clear()
+        for shape in ((2, 40), (3, 40), (2, 1, 40), (80,)):
+            call(FakeMask(*shape))
+        assert len(recorder.calls) == 4
