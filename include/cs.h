@@ -409,7 +409,9 @@ cs_status cs_kv4_load(const cs_kv4_cache* cache, const cs_kv4_rows* rows, void* 
 
 /* cs_cross_attention over a 4-bit cache: context j is the cache's context j, and
  * desc's n_kv, lk, heads_kv and head_dim are the cache's (its k_ and v_ strides are
- * not read).  Rows that are left out may hold any bytes. */
+ * not read).  Rows that are left out may hold any bytes.  In CS_BF16 mode with more than
+ * 192 queries to a key head (lq * heads_q / heads_kv) the workspace holds the keys and
+ * values of min(n_q, n_kv) contexts in bf16: 4 * lk * heads_kv * head_dim bytes each. */
 cs_status cs_kv4_attention_workspace(const cs_attn_desc* desc, size_t* bytes);
 cs_status cs_kv4_attention(const cs_attn_desc* desc, const void* q, const cs_kv4_cache* cache,
                            const int32_t* kv_of, const int32_t* kv_len, const uint8_t* kv_mask,

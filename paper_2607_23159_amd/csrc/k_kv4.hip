@@ -28,9 +28,14 @@ template <int LH, int U> struct Kv4Items {
       row[u] = (block * U + u) * RW + lane / LH;
       const int slot = row[u] >= a.r.n_rows ? -1 : a.slots ? a.slots[row[u]] : row[u];
       if (slot < 0 || slot >= slots) row[u] = -1;
-      const int ctx = by_cap.div(row[u] < 0 ? 0 : slot);
-      if (a.len && slot - ctx * a.c.cap >= a.len[ctx]) row[u] = -1;
-      at[u] = ((long)ctx * a.c.heads + head) * a.c.cap + (slot - ctx * a.c.cap);
+      const int i = by_cap.div(row[u] < 0 ? 0 : slot), r = slot - i * a.c.cap;
+      int ctx = a.ctx_of ? a.ctx_of[i] : i;
+      if (ctx < 0 || ctx >= a.c.n_kv) {
+        row[u] = -1;
+        ctx = 0;
+      }
+      if (a.len && r >= a.len[ctx]) row[u] = -1;
+      at[u] = ((long)ctx * a.c.heads + head) * a.c.cap + r;
     }
     return true;
   }

@@ -116,8 +116,9 @@ template <int DH, int NW, int OCC, bool MASK> __global__ __launch_bounds__(64 * 
       const int pk = xattn_part(a, len);
       it.k0 = it.part * pk;
       it.k1 = min(len, it.k0 + pk);
-      it.kb = (const bf16*)a.k + ctx * a.d.k_b + it.head * a.d.k_h;
-      it.vb = (const bf16*)a.v + ctx * a.d.v_b + it.head * a.d.v_h;
+      const int kv = a.by_set ? it.set : ctx;
+      it.kb = (const bf16*)a.k + kv * a.d.k_b + it.head * a.d.k_h;
+      it.vb = (const bf16*)a.v + kv * a.d.v_b + it.head * a.d.v_h;
       it.mask = MASK ? a.mask + ctx * a.d.mask_b : nullptr;
       if (it.k0 < it.k1) return true;
       if (a.parts == 1) {

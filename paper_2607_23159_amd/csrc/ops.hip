@@ -124,7 +124,7 @@ static cs_status kv4_rows_call(const cs_kv4_cache* c, const cs_kv4_rows* r, cons
   if (r->n_rows == 0) return CS_OK;
   TRY(check_tensor(store ? k : ko, "k"));
   TRY(check_tensor(store ? v : vo, "v"));
-  const Kv4RowsArgs a = {*c, *r, k, v, ko, vo, slots, true, nullptr};
+  const Kv4RowsArgs a = {*c, *r, k, v, ko, vo, slots, true, nullptr, nullptr};
   hipStream_t st = (hipStream_t)stream;
   hipError_t s;
   if (r->dtype == CS_BF16)
@@ -207,7 +207,7 @@ static cs_status attn_call(const cs_attn_desc* d, const void* q, const void* k, 
     CHECK(work && aligned(work), CS_E_INVAL, "a 16-byte aligned workspace is needed");
     CHECK(work_bytes >= need, CS_E_INVAL, "the workspace holds %zu bytes, %zu needed", work_bytes, need);
   }
-  XAttnArgs a = {q, k, v, o, kv_of, kv_len, kv_mask, {}, *d, (float)(1.4426950408889634 * d->scale)};
+  XAttnArgs a = {q, k, v, o, kv_of, kv_len, false, kv_mask, {}, *d, (float)(1.4426950408889634 * d->scale)};
   if (kv4) a.c = *cache;
   if (d->lk == 1) a.d.k_r = a.d.v_r = d->head_dim;   // never checked
   hipStream_t st = (hipStream_t)stream;

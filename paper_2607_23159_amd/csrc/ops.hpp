@@ -37,6 +37,7 @@ struct Kv4RowsArgs {
   const int* slots;
   bool stream;           // loaded rows are not read again soon
   const int* len;        // rows of each context, or NULL: further ones are skipped
+  const int* ctx_of;     // the context that context i of the slots stands for, or NULL: i
 };
 template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
 template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);
@@ -48,6 +49,7 @@ struct XAttnArgs {
   const void *q, *k, *v;
   void* o;
   const int *kv_of, *kv_len;
+  bool by_set;           // k and v hold a context for each set (kv_len and mask do not)
   const uint8_t* mask;
   cs_kv4_cache c;        // 4-bit keys and values (k, v not read)
   cs_attn_desc d;

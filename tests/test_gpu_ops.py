@@ -457,6 +457,37 @@ def test_attention_does_not_depend_on_the_batch(kv4, dtype, lq, lk, hq, hkv, dim
     assert torch.equal(call(q, of), whole)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lq,lk,dim,masked", [(200, 90, 64, True), (300, 1100, 128, False), (1100, 70, 32, True)])
+def test_fewer_sets_than_contexts(dtype, lq, lk, dim, masked):
+    """Each set's context is unpacked into the workspace, whichever it is and if two sets share it."""
+    n = 9
+    lens = torch.tensor([lk, 3, lk - 1, 0, lk + 5, 17, lk // 2, 1, lk], dtype=torch.int32)
+    mask = _masks("holes", n, lk) if masked else None
+    q = rnd(1, 6, lq, 2, dim, dtype=dtype)
+    parts = [R.quantise(rnd(s, n, 2, lk, dim) + 0.1 * s) for s in (2, 3)]
+    k, v = (R.dequantise(*p).transpose(1, 2) for p in parts)
+    of = torch.tensor([8, 2, 2, n, -1, 3], dtype=torch.int32)
+    ref, bound = R.attention(q, k, v, 1 / math.sqrt(dim), of, lens, mask, dtype == BF)
+    cache = B.Kv4Cache(*(t.cuda() for p in parts for t in p))
+    q = q.cuda()
+    for sets in (slice(0, 6), slice(1, 3), slice(5, 6)):
+        o, check = guarded((sets.stop - sets.start, lq, 2, dim), dtype)
+        d = B.kv4_attn_desc(q[sets], cache, o)
+        w, check_w = _work(B.cs_kv4_attention_workspace(d))
+        B.cs_kv4_attention(d, q[sets], cache, o, of[sets].cuda(), lens.cuda(), _cuda(mask), w)
+        torch.cuda.synchronize()
+        within(o, ref[sets], bound[sets], "o")
+        check()
+        check_w()
+    # without an index the sets read the first contexts
+    o, check = guarded((2, lq, 2, dim), dtype)
+    d = B.kv4_attn_desc(q[:2], cache, o)
+    B.cs_kv4_attention(d, q[:2], cache, o, None, lens.cuda(), _cuda(mask), _work(B.cs_kv4_attention_workspace(d))[0])
+    ref, bound = R.attention(q[:2].cpu(), k, v, 1 / math.sqrt(dim), None, lens, mask, dtype == BF)
+    within(o, ref, bound, "o")
+
+
 @pytest.mark.parametrize("kv4", [False, True])
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq,lk,g", [(7, 1200, 4), (60, 300, 3), (400, 200, 1), (1100, 70, 8)])

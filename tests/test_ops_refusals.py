@@ -225,3 +225,16 @@ def test_sizes_whose_products_pass_64_bits():
 def test_scales_that_overflow():
     for s in (1e38, 3.4e38):
         assert attn(attn_desc(scale=s)) == B.CS_E_INVAL and "scale" in B.cs_last_error()
+
+
+def test_the_workspace_holds_no_more_contexts_than_sets():
+    """Over 4 bits, many bf16 rows read contexts that are unpacked first: as many as the sets that read
+    them, not all of the cache."""
+    n, one = C.c_size_t(0), C.c_size_t(0)
+    big = dict(lq=300, heads_q=8, heads_kv=8, head_dim=128, lk=700)
+    fn = B.lib().cs_kv4_attention_workspace
+    assert fn(C.byref(attn_desc(n_q=1, n_kv=1, **big)), C.byref(one)) == B.CS_OK
+    assert one.value >= 2 * 700 * 8 * 128 * 2
+    for n_q, n_kv in ((1, 64), (3, 2000), (5, 5), (7, 2)):
+        assert fn(C.byref(attn_desc(n_q=n_q, n_kv=n_kv, **big)), C.byref(n)) == B.CS_OK
+        assert n.value <= min(n_q, n_kv) * one.value, (n_q, n_kv)
