@@ -6,26 +6,6 @@
 
 namespace cs {
 
-// A problem's keys are cut into parts by its own sizes, never by the batch, so that
-// results do not depend on it.
-static void cut(XAttnArgs& a, bool kv4) {
-  a.group = a.d.heads_q / a.d.heads_kv;
-  a.rows = a.d.lq * a.group;
-  a.parts = 1;
-  // Keys of a full context's part: half as many bytes again in 4 bits (16 contexts of up
-  // to 32,768 rows: 512 keys 72.7 us, 1,024 66.6, 2,048 82.6; bf16, 8 of up to 8,192: 256
-  // keys 35.3, 512 34.2, 1,024 35.8).
-  // Many rows fill the card by themselves; in fp32, where a workgroup takes long over its
-  // keys, eight times as many keys (one set of 12 heads, 1,560 rows, 32,760 keys: 3,319 us
-  // whole, 1,690 in parts).
-  const bool many = a.rows > 1024;
-  const int keys = !many ? kv4 ? 1024 : 512 : a.d.dtype == CS_FP32 && !kv4 ? 4096 : 1 << 30, most = 128;
-  if (a.d.lk > keys) a.parts = std::min(most, cdiv(a.d.lk, keys));
-  a.by_group = FastDiv(a.group);
-  a.by_parts = FastDiv(a.parts);
-  a.by_heads = FastDiv(a.d.heads_kv);
-}
-
 // Whether a problem goes to k_xattn_rows, which takes its rows 32 at a time and reads
 // the keys once for each 32.
 //   bf16: if that is once (8 contexts of 8,192 rows, 8 key heads: 32 rows 53.0 us, 36
@@ -40,6 +20,32 @@ static void cut(XAttnArgs& a, bool kv4) {
 static bool few_rows(const XAttnArgs& a, bool kv4) {
   if (a.d.dtype != CS_BF16) return kv4;
   return a.rows <= (kv4 ? 192 : 32);
+}
+
+// A problem's keys are cut into parts by its own sizes, never by the batch, so that
+// results do not depend on it.
+static void cut(XAttnArgs& a, bool kv4) {
+  a.group = a.d.heads_q / a.d.heads_kv;
+  a.rows = a.d.lq * a.group;
+  a.parts = 1;
+  // Keys of a full context's part: half as many bytes again in 4 bits (16 contexts of up
+  // to 32,768 rows: 512 keys 72.7 us, 1,024 66.6, 2,048 82.6; bf16, 8 of up to 8,192: 256
+  // keys 35.3, 512 34.2, 1,024 35.8).
+  // In fp32, where a workgroup takes long over its keys, 4,096 keys once the rows are many
+  // (one set of 12 heads, 1,560 rows, 32,760 keys: 3,319 us whole, 1,690 in parts).
+  // Else many rows of enough heads fill the card by themselves.  Fewer workgroups a set than
+  // half the CUs take parts of 2,048 keys, as many as go round once (bf16, one set, whole
+  // / parts: 1,032 rows of one head, 131,072 keys 2,242 / 121 us, of 8 heads
+  // 2,527 / 894; 1,100 rows of 2 heads of 64, 8,192 keys 125 / 41.  Batches that fill the card pay
+  // for the join: 64 sets of 1,100 rows of 2 heads, 8,192 keys 692 / 775).
+  const bool many = a.rows > 1024, f32 = a.d.dtype == CS_FP32 && !kv4;
+  const int keys = !many ? kv4 ? 1024 : 512 : f32 ? 4096 : 2048;
+  long most = 128;
+  if (many && !f32) most = std::min(most, 256 / ((long)a.d.heads_kv * cdiv(a.rows, few_rows(a, kv4) ? 32 : 128)));
+  if (a.d.lk > keys && most > 1) a.parts = (int)std::min<long>(most, cdiv(a.d.lk, keys));
+  a.by_group = FastDiv(a.group);
+  a.by_parts = FastDiv(a.parts);
+  a.by_heads = FastDiv(a.d.heads_kv);
 }
 
 // Which of the fp32 kernels.  k_xattn_split does a product in bf16 terms, at twice the

@@ -488,6 +488,43 @@ def test_fewer_sets_than_contexts(dtype, lq, lk, dim, masked):
     within(o, ref, bound, "o")
 
 
+@pytest.mark.parametrize("dtype,kv4", [(BF, False), (BF, True), (FP, False), (FP, True)])
+@pytest.mark.parametrize("lq,hq,hkv,dim,lk", [(129, 8, 1, 128, 4200), (1061, 2, 2, 64, 2300), (350, 6, 2, 32, 5001)])
+def test_many_rows_of_few_heads_over_long_contexts(dtype, kv4, lq, hq, hkv, dim, lk):
+    n = 3
+    lens = torch.tensor([lk - 7, 300, 0], dtype=torch.int32)
+    mask = _masks("holes", n, lk)
+    q = rnd(1, n, lq, hq, dim, dtype=dtype, scale=1.5)
+    k, v = rnd(2, n, lk, hkv, dim, dtype=dtype), rnd(3, n, lk, hkv, dim, dtype=dtype)
+    kk, vv = k.double(), v.double()
+    if kv4:
+        kk, vv = (R.dequantise(*R.quantise(x)) for x in (k, v))
+    ref, bound = R.attention(q, kk, vv, 1 / math.sqrt(dim), None, lens, mask, dtype == BF)
+    q, k, v, lens, mask = (x.cuda() for x in (q, k, v, lens, mask))
+    cache = _cache(n, hkv, lk, dim)
+    B.cs_kv4_store(cache, k.flatten(0, 1), v.flatten(0, 1))
+
+    def call(qq, index):
+        o, check = guarded(tuple(qq.shape), dtype)
+        if kv4:
+            d = B.kv4_attn_desc(qq, cache, o)
+            w, check_w = _work(B.cs_kv4_attention_workspace(d))
+            B.cs_kv4_attention(d, qq, cache, o, index, lens, mask, w)
+        else:
+            d = B.attn_desc(qq, k, v, o)
+            w, check_w = _work(B.cs_cross_attention_workspace(d))
+            B.cs_cross_attention(d, qq, k, v, o, index, lens, mask, w)
+        torch.cuda.synchronize()
+        check()
+        check_w()
+        return o
+
+    whole = call(q, None)
+    within(whole, ref, bound, "o")
+    for i in range(n):
+        assert torch.equal(call(q[i:i + 1], torch.tensor([i], dtype=torch.int32, device="cuda"))[0], whole[i])
+
+
 @pytest.mark.parametrize("kv4", [False, True])
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq,lk,g", [(7, 1200, 4), (60, 300, 3), (400, 200, 1), (1100, 70, 8)])

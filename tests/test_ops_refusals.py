@@ -238,3 +238,20 @@ def test_the_workspace_holds_no_more_contexts_than_sets():
     for n_q, n_kv in ((1, 64), (3, 2000), (5, 5), (7, 2)):
         assert fn(C.byref(attn_desc(n_q=n_q, n_kv=n_kv, **big)), C.byref(n)) == B.CS_OK
         assert n.value <= min(n_q, n_kv) * one.value, (n_q, n_kv)
+
+
+def test_many_rows_of_few_heads_share_a_long_context_out():
+    """One key head of 1,032 rows over 131,072 keys makes nine blocks of 128 rows for 256 compute units:
+    the keys are cut, as for fewer rows, which shows in the workspace."""
+    n = C.c_size_t(0)
+    few = dict(n_q=1, n_kv=1, lq=129, heads_q=8, heads_kv=1, head_dim=128)
+    row = 128 * 4 + 8          # of a part: outputs, maximum and sum
+    for dtype, fn, kv in ((B.CS_BF16, B.lib().cs_cross_attention_workspace, 0),
+                          (B.CS_BF16, B.lib().cs_kv4_attention_workspace, 4 * 131072 * 128),
+                          (B.CS_FP32, B.lib().cs_kv4_attention_workspace, 0)):
+        assert fn(C.byref(attn_desc(dtype=dtype, lk=131072, **few)), C.byref(n)) == B.CS_OK
+        assert n.value >= kv + 1032 * row * (7 if dtype == B.CS_FP32 else 28)
+    # enough heads, or few keys: none
+    for kw in (dict(heads_q=16, heads_kv=16, lq=1032, lk=131072), dict(heads_q=8, heads_kv=1, lq=129, lk=2048)):
+        d = attn_desc(n_q=1, n_kv=1, head_dim=128, **kw)
+        assert B.lib().cs_cross_attention_workspace(C.byref(d), C.byref(n)) == B.CS_OK and n.value == 0
