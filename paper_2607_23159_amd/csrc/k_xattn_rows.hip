@@ -35,12 +35,12 @@ template <int DH, bool MASK> struct TileBf16 {
   const char *kp, *vp;   // row k0
   int k_b, v_b;          // bytes from row to row
   const uint8_t* mask;
-  int k0, k1, lane, koff;
+  int k1, lane, koff;
   bf16x8 k[2][KS], v[2][KS];
   uint64_t bits;
 
-  CS_DEV TileBf16(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k0_, int k1_, int lane_)
-      : k_b(2 * (int)a.d.k_r), v_b(2 * (int)a.d.v_r), mask(mask_), k0(k0_), k1(k1_), lane(lane_) {
+  CS_DEV TileBf16(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_)
+      : k_b(2 * (int)a.d.k_r), v_b(2 * (int)a.d.v_r), mask(mask_), k1(k1_), lane(lane_) {
     kp = (const char*)((const bf16*)a.k + ctx * a.d.k_b + head * a.d.k_h);
     vp = (const char*)((const bf16*)a.v + ctx * a.d.v_b + head * a.d.v_h);
     koff = (lane & 15) * k_b + 16 * (lane >> 4);
@@ -86,12 +86,12 @@ template <int DH, bool MASK> struct TileKv4 {
   static constexpr int KEYS = 32, KS = DH / 32, WAVES = 4;
   const uint8_t *kc, *ks_, *vc, *vs_;   // row 0
   const uint8_t* mask;
-  int k0, k1, lane;
+  int k1, lane;
   uint32_t k[2][KS], v[2][KS], kb[2], vb[2];
   uint64_t bits;
 
-  CS_DEV TileKv4(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k0_, int k1_, int lane_)
-      : mask(mask_), k0(k0_), k1(k1_), lane(lane_) {
+  CS_DEV TileKv4(const XAttnArgs& a, int ctx, int head, const uint8_t* mask_, int k1_, int lane_)
+      : mask(mask_), k1(k1_), lane(lane_) {
     const long at = ((long)ctx * a.c.heads + head) * a.c.cap;
     kc = a.c.k_codes + at * (DH / 2);
     vc = a.c.v_codes + at * (DH / 2);
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256, NS > 1 ? 1 : RT > 1 ? 2 : Tile::WAVES) void k_
   }
 
   lds_char* const rows = (lds_char*)smem + wave * WAVE_LDS;
-  Tile tile(a, ctx, head, MASK ? a.mask + ctx * a.d.mask_b : nullptr, k0, k1, lane);
+  Tile tile(a, ctx, head, MASK ? a.mask + ctx * a.d.mask_b : nullptr, k1, lane);
   const int first = k0 + wave * KEYS, step = NW * KEYS;
   if (first < k1) tile.request(first);
   for (int kv0 = first; kv0 < k1; kv0 += step) {
