@@ -69,15 +69,24 @@ class GpuPrompts:
 
     def __init__(self, model: GpuModel, ctx: torch.Tensor, lens=None, kv_format: int = B.CS_KV_NATIVE):
         self.model = model        # kept alive; closing it closes its prompts
+        self._wait_for_inputs()
         self.h = B.cs_context_init(model.h, ctx, ctx.shape[0], lens, kv_format)
         model.contexts.add(self.h)
 
     def velocity(self, x: torch.Tensor, t: float, prompt=None) -> torch.Tensor:
         """Velocities of the latents x, latent i attending to prompt[i] (None: prompt i)."""
         v = torch.empty_like(x)
+        self._wait_for_inputs()
         B.cs_velocity_context(self.model.h, self.h, x, x.shape[0], t, v, prompt)
         torch.cuda.synchronize()
         return v
+
+    def _wait_for_inputs(self):
+        """The library works on the model's stream: torch's current one has to be through with the
+        tensors where it is another."""
+        current = torch.cuda.current_stream()
+        if current.cuda_stream != (B._stream(self.model.stream) or 0):
+            current.synchronize()
 
     def close(self):
         if self.h and self.h in self.model.contexts:

@@ -167,6 +167,28 @@ def test_refusals_with_live_handles():
     ps.close()
 
 
+def test_prompts_and_latents_made_on_another_stream():
+    m, gm, _ = made("tiny", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
+    ctx = torch.from_numpy(_prompts(m, 2)).cuda()
+    x = torch.from_numpy(synth.make_noise(m, 2).reshape(2, -1)).cuda()
+    want = gm.prompts(ctx, [3, m.text_len]).velocity(x, 0.5)
+    a = torch.randn(2048, 2048, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def late(t):
+        nonlocal a
+        y = torch.full_like(t, 3.0)
+        for _ in range(100):            # a while, behind which the values come
+            a = a @ a * 1e-3
+        return y.copy_(t)
+    with torch.cuda.stream(side):
+        ps = gm.prompts(late(ctx), [3, m.text_len])
+        got = ps.velocity(late(x), 0.5)
+    assert torch.equal(got, want)
+    ps.close()
+
+
 @pytest.mark.parametrize("fmt", [B.CS_KV_NATIVE, B.CS_KV_4BIT])
 def test_closing_the_model_returns_its_prompts_memory(fmt):
     m = synth.MODELS["tiny"]

@@ -1,5 +1,6 @@
 """Who frees a model's prompts, and in which order (no GPU needed: the library is stood in for)."""
 import gc
+import weakref
 
 import numpy as np
 import pytest
@@ -25,12 +26,29 @@ def freed(monkeypatch):
     monkeypatch.setattr(search.B, "cs_context_init", make("c"))
     monkeypatch.setattr(search.B, "cs_model_free", lambda h: log.append(h))
     monkeypatch.setattr(search.B, "cs_context_free", lambda h: log.append(h))
-    return log
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream(0, []))
+    yield log
+    for gm in _models:                 # a failed test's frames keep theirs: nothing real may be freed
+        gm.contexts, gm.h = set(), 0
+    _models.clear()
 
 
-def _model():
+_models = weakref.WeakSet()
+
+
+class Stream:
+    def __init__(self, handle, log):
+        self.cuda_stream, self.log = handle, log
+
+    def synchronize(self):
+        self.log.append("wait")
+
+
+def _model(stream=None):
     m = synth.MODELS["tiny"]
-    return search.GpuModel(m, np.zeros(synth.weight_count(m), np.float32))
+    gm = search.GpuModel(m, np.zeros(synth.weight_count(m), np.float32), stream=stream)
+    _models.add(gm)
+    return gm
 
 
 def test_a_model_closed_first_frees_its_prompts_before_itself(freed):
@@ -63,3 +81,17 @@ def test_a_model_and_prompts_that_go_together(freed):
     del gm
     gc.collect()
     assert freed == [101, 1]
+
+
+@pytest.mark.parametrize("model_stream,current,waits", [(None, 0, False), (None, 8, True), (8, 8, False), (8, 0, True),
+                                                        (Stream(8, []), 8, False), (Stream(8, []), 16, True)])
+def test_prompts_wait_for_inputs_of_another_stream(freed, monkeypatch, model_stream, current, waits):
+    """The library works on the model's stream: what the current one still has to produce is waited for."""
+    log = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream(current, log))
+    monkeypatch.setattr(search.B, "cs_context_init", lambda *args: log.append("init") or 101)
+    monkeypatch.setattr(search.B, "cs_velocity_context", lambda *args: log.append("velocity"))
+    gm = _model(model_stream)
+    ps = gm.prompts(torch.zeros(1))
+    ps.velocity(torch.zeros(1, 4), 0.5)
+    assert log == (["wait", "init", "wait", "velocity"] if waits else ["init", "velocity"])
