@@ -324,7 +324,8 @@ typedef struct {
 /* RMS norm of every head of q and k over its own channels, then the rotation:
  *   y_c = x_c / sqrt(mean_c(x_c^2) + eps) * gain_c,
  *   (a, b) -> (a cos - b sin, a sin + b cos) for the pairs of the first rot_dim
- * channels, in fp32 and rounded once.  rope: device float
+ * channels, in fp32 and rounded once (the sum of squares too: a head of length 1.8e19 or
+ * more gives zeros, and with eps 0 one shorter than 1e-19 is not resolved).  rope: device float
  * [rope_rows][rot_dim / 2][2] (cos, sin); token t takes row pos[t] (device
  * int32), or row t % rope_rows if pos is NULL.  A token whose position is
  * negative is skipped: its outputs are left as they were (padding).  One whose
@@ -360,9 +361,11 @@ typedef struct {
  * query with no key left, or whose kv_of is not in 0..n_kv-1, gets zeros.  Scores
  * and sums are fp32; in CS_BF16 mode the softmax weights are rounded to bf16 for
  * the product with v and summed as rounded.  In CS_FP32 mode a product may be taken
- * as six products of bf16 terms (off by at most 2^-22 of its magnitude): an element
+ * as six products of bf16 terms (off by at most 2^-22 of its magnitude; it is where
+ * lq * heads_q is at least 8,192 and lq * heads_q / heads_kv above 64).  An element
  * of 3.39e38 or more, infinities included, in a query or in a key or value that is
- * not left out then makes NaN of the outputs it enters.  o must not overlap the
+ * not left out then makes NaN of the outputs it enters, and one below 2^-103 (1e-31) is
+ * held to 2^-134 instead of its 24 bits.  o must not overlap the
  * inputs.
  * cs_cross_attention_workspace gives the bytes of `work` (0: work may be NULL). */
 cs_status cs_cross_attention_workspace(const cs_attn_desc* desc, size_t* bytes);
@@ -409,7 +412,8 @@ cs_status cs_kv4_load(const cs_kv4_cache* cache, const cs_kv4_rows* rows, void* 
 
 /* cs_cross_attention over a 4-bit cache: context j is the cache's context j, and
  * desc's n_kv, lk, heads_kv and head_dim are the cache's (its k_ and v_ strides are
- * not read).  Rows that are left out may hold any bytes.  In CS_BF16 mode with more than
+ * not read).  In CS_FP32 mode queries are taken in bf16 terms, with their limits.  Rows
+ * that are left out may hold any bytes.  In CS_BF16 mode with more than
  * 192 queries to a key head (lq * heads_q / heads_kv) the workspace holds the keys and
  * values of min(n_q, n_kv) contexts in bf16: 4 * lk * heads_kv * head_dim bytes each. */
 cs_status cs_kv4_attention_workspace(const cs_attn_desc* desc, size_t* bytes);

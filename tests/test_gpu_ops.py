@@ -607,6 +607,19 @@ def test_scores_of_a_billion(kv4, dtype, lq, lk, g):
     assert (o.abs().amax(-1) > 0).all()
 
 
+@pytest.mark.parametrize("lq,hq", [(1100, 8), (300, 2), (1, 4)])
+@pytest.mark.parametrize("exponent", [-100, -103, -120])
+def test_fp32_values_near_the_smallest_number(lq, hq, exponent):
+    """Bf16 terms end at 2^-133, the smallest number of their type: values lose bits below 2^-103, by at
+    most half of that number each, whatever the weights, which sum to one."""
+    q, k, v = rnd(1, 1, lq, hq, 64), rnd(2, 1, 100, hq, 64), rnd(3, 1, 100, hq, 64)
+    v *= 2.0 ** exponent / v.abs().clamp_min(1e-3)
+    v *= 1 + 0.9 * rnd(4, 1, 100, hq, 64).abs().clamp_max(1)
+    ref, bound = R.attention(q, k.double(), v.double(), 0.125, None, None, None, False)
+    o = _attend(False, q.cuda(), k.cuda(), v.cuda())
+    within(o, ref, bound - 1e-37 + 2.0 ** -134 + 2.0 ** -149, "o")
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("lq", [1, 150])
 def test_rows_more_than_two_gib_apart(dtype, lq):

@@ -255,3 +255,18 @@ def test_many_rows_of_few_heads_share_a_long_context_out():
     for kw in (dict(heads_q=16, heads_kv=16, lq=1032, lk=131072), dict(heads_q=8, heads_kv=1, lq=129, lk=2048)):
         d = attn_desc(n_q=1, n_kv=1, head_dim=128, **kw)
         assert B.lib().cs_cross_attention_workspace(C.byref(d), C.byref(n)) == B.CS_OK and n.value == 0
+
+
+@pytest.mark.parametrize("what", ["parts", "parts of a cache", "unpacked cache", "both"])
+def test_every_workspace_that_is_needed_is_checked(what):
+    n = C.c_size_t(0)
+    if what == "parts":
+        d, fn = attn_desc(lq=1, lk=1 << 20, k_b=1 << 28, v_b=1 << 28), B.lib().cs_cross_attention_workspace
+        call = attn
+    else:
+        lq, lk = {"parts of a cache": (1, 1 << 20), "unpacked cache": (100, 600), "both": (100, 5000)}[what]
+        d, fn = attn_desc(lq=lq, lk=lk), B.lib().cs_kv4_attention_workspace
+        call = lambda d, **kw: kv4(d, cache(cap=lk), **kw)
+    assert fn(C.byref(d), C.byref(n)) == B.CS_OK and n.value > 0
+    for kw in (dict(), dict(work=P, nbytes=n.value - 1), dict(work=P + 8, nbytes=n.value), dict(nbytes=n.value)):
+        assert call(d, **kw) == B.CS_E_INVAL and "workspace" in B.cs_last_error()
