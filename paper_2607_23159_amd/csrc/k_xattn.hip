@@ -203,7 +203,7 @@ template <typename T> hipError_t xattn(XAttnArgs a, bool kv4, void* work, hipStr
         l.len = a.kv_len;
         l.ko = (char*)work + w.k;
         l.vo = (char*)work + w.v;
-        e = kv4_load<T>(l, st);
+        e = kv4_unpack(l, st);
         if (e != hipSuccess) return e;
         a.k = l.ko;
         a.v = l.vo;

@@ -124,7 +124,7 @@ static cs_status kv4_rows_call(const cs_kv4_cache* c, const cs_kv4_rows* r, cons
   if (r->n_rows == 0) return CS_OK;
   TRY(check_tensor(store ? k : ko, "k"));
   TRY(check_tensor(store ? v : vo, "v"));
-  const Kv4RowsArgs a = {*c, *r, k, v, ko, vo, slots, true, nullptr, nullptr};
+  const Kv4RowsArgs a = {*c, *r, k, v, ko, vo, slots, nullptr, nullptr};
   hipStream_t st = (hipStream_t)stream;
   hipError_t s;
   if (r->dtype == CS_BF16)

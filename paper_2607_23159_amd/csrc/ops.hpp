@@ -35,12 +35,13 @@ struct Kv4RowsArgs {
   const void *k, *v;     // stored rows
   void *ko, *vo;         // loaded rows
   const int* slots;
-  bool stream;           // loaded rows are not read again soon
+  // kv4_unpack only
   const int* len;        // rows of each context, or NULL: further ones are skipped
-  const int* ctx_of;     // the context that context i of the slots stands for, or NULL: i
+  const int* ctx_of;     // the context that context i of the rows stands for, or NULL: i
 };
 template <typename T> hipError_t kv4_store(const Kv4RowsArgs& a, hipStream_t st);
 template <typename T> hipError_t kv4_load(const Kv4RowsArgs& a, hipStream_t st);
+hipError_t kv4_unpack(const Kv4RowsArgs& a, hipStream_t st);   // to bf16, slots not read
 
 // ---- attention to contexts (k_xattn*.hip)
 // The queries of a set that share a key head are the rows of one problem: row r is
