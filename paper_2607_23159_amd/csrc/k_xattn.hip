@@ -8,15 +8,15 @@ namespace cs {
 
 // Whether a problem goes to k_xattn_rows, which takes its rows 32 at a time and reads
 // the keys once for each 32.
-//   bf16: if that is once (8 contexts of 8,192 rows, 8 key heads: 32 rows 53.0 us, 36
-//     rows in k_xattn_tile 56.2; 64 rows 138 here, 64.1 there).
+//   bf16: if that is once (8 contexts of 8,192 rows, 8 key heads, here / in k_xattn_tile: 32
+//     rows 54.1 / 53.5 us, 36 rows 66.2 / 54.8, 64 rows 75.8 / 60.7).
 //   4 bits, bf16 rows: k_xattn_tile wants the cache unpacked first, which pays once the
-//     rows are many (16 contexts of 32,768 rows, 8 key heads, here / there: 64 rows 339 /
-//     987 us, 128 rows 551 / 1,069, 192 rows 829 / 1,203, 256 rows 1,100 / 1,273, 384 rows
-//     1,647 / 1,622).  Contexts that many queries share would turn earlier.
+//     rows are many (16 contexts of 32,768 rows, 8 key heads, here / there: 64 rows 320 /
+//     1,024 us, 128 rows 608 / 1,136, 192 rows 917 / 1,244, 256 rows 1,216 / 1,345, 384 rows
+//     1,823 / 1,773).  Contexts that many queries share would turn earlier.
 //   4 bits, fp32 rows: always.  The queries' and weights' three bf16 terms meet exact
 //     bf16 keys at 220 TFLOP/s, the fp32 products of k_xattn_f32 reach 85 (96 tokens of
-//     4 heads each: 3,751 us, 9,748 there).
+//     4 heads each: 3.8 ms, 9.7 there).
 static bool few_rows(const XAttnArgs& a, bool kv4) {
   if (a.d.dtype != CS_BF16) return kv4;
   return a.rows <= (kv4 ? 192 : 32);
@@ -51,8 +51,8 @@ static void cut(XAttnArgs& a, bool kv4) {
 // Which of the fp32 kernels.  k_xattn_split does a product in bf16 terms, at twice the
 // rate, but its workgroups take 128 rows and all keys in turn where those of k_xattn_f32
 // take 32 rows and split the keys between their waves: it wants 64 workgroups a set (12
-// heads of 128, 512 keys, here / there: 400 rows 59.3 / 28.1 us, 800 rows 60.8 / 52.6, 1,560
-// rows 61.4 / 75.7; 8 such sets: 87.4 / 127, 137 / 248, 221 / 468).
+// heads of 128, 512 keys, here / there: 400 rows 60.7 / 29.3 us, 800 rows 62.4 / 55.1, 1,560
+// rows 63.0 / 79.0; 8 such sets: 89.9 / 126, 138 / 245, 220 / 466).
 static bool split_f32(const XAttnArgs& a) { return a.rows > 64 && (long)a.rows * a.d.heads_kv >= 64 * 128; }
 
 struct Work {

@@ -346,8 +346,8 @@ template <typename T, int DH, int RT, bool MASK, bool KV4> static hipError_t lau
 }
 
 // One row tile where 16 hold all rows, two else: a third and fourth do not fit the
-// registers of two waves a SIMD (64 rows over 16 4-bit contexts of 32,768 rows: 382 us as one
-// block of four tiles, 326 as two blocks of two).
+// registers of two waves a SIMD (64 rows over 16 4-bit contexts of 32,768 rows take 17% longer as
+// one block of four tiles than as two blocks of two).
 template <typename T, int DH, bool MASK, bool KV4> static hipError_t launch(const XAttnArgs& a, hipStream_t st) {
   return a.rows <= 16 ? launch_rt<T, DH, 1, MASK, KV4>(a, st) : launch_rt<T, DH, 2, MASK, KV4>(a, st);
 }

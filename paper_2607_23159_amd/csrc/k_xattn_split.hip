@@ -9,8 +9,8 @@
 // 32 between them, once for all 128 rows, and leave the terms in LDS.  Scores, softmax and
 // value product as in k_xattn_rows.  Two workgroups share a CU: one's splitting and
 // softmax run under the other's products.  12 heads of 128, 1,560 rows: one set of 32,760
-// keys 1,667 us (188 TFLOP/s; a library fp32 product reaches 153, k_xattn_f32 88), 8 sets
-// of 512 keys 242 us (162 TFLOP/s).  Splitting in the registers of every wave, 32 rows at a
+// keys 1,594 us (197 TFLOP/s; a library fp32 product reaches 153, k_xattn_f32 111), 8 sets
+// of 512 keys 220 us (178 TFLOP/s, matrix pipe 46% busy).  Splitting in the registers of every wave, 32 rows at a
 // time, measured 65 TFLOP/s: twice as many instructions go to the terms as to the rest.
 #include "xattn_mma.hpp"
 
