@@ -286,7 +286,8 @@ cs_status cs_rollout_import(cs_rollout* r, const void* buf, size_t bytes);
  *    the channels of a head are contiguous.  Rows are moved 16 bytes at a
  *    time: tensor pointers are 16-byte aligned and strides multiples of 16
  *    bytes (CS_E_INVAL otherwise).  Strides are not negative; an output's
- *    are not zero either, where its axis has several entries.
+ *    are not zero either, where its axis has several entries.  Beyond that
+ *    it is up to the caller that an output's rows and heads do not overlap.
  *  - The work is enqueued on `stream` (hipStream_t or NULL); nothing is
  *    allocated, copied or waited for, so calls can be captured into a HIP
  *    graph.  Descriptors are read before the call returns.  Tensors must

@@ -141,6 +141,22 @@ def test_prompts_in_four_bits(name, dtype, monkeypatch):
     ps.close()
 
 
+@pytest.mark.parametrize("dtype", [synth.DTYPE_FP32, synth.DTYPE_BF16])
+@pytest.mark.parametrize("name", ["tiny", "ragged"])
+def test_prompts_in_four_bits_one_by_one_and_together(name, dtype):
+    """Latents alone on any of the prompts, more latents than prompts, a prompt of no row: bitwise the same."""
+    m, gm, _ = made(name, dtype, B.CS_QK_NORM_FULL)
+    ps = gm.prompts(torch.from_numpy(_prompts(m, 4)).cuda(), [m.text_len, 0, 1, m.text_len // 2 + 1], B.CS_KV_4BIT)
+    of = [3, 0, 1, 2, 3, 0]
+    xs = torch.from_numpy(synth.make_noise(m, len(of), seed0=600).reshape(len(of), -1)).cuda()
+    v = ps.velocity(xs, 0.45, of)
+    assert torch.isfinite(v).all()
+    for i, p in enumerate(of):
+        assert torch.equal(ps.velocity(xs[i:i + 1].contiguous(), 0.45, [p])[0], v[i]), i
+    assert torch.equal(ps.velocity(xs[2:5].contiguous(), 0.45, of[2:5]), v[2:5])
+    ps.close()
+
+
 def test_refusals_with_live_handles():
     m, gm, _ = made("tiny", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
     _, other, _ = made("ragged", synth.DTYPE_FP32, B.CS_QK_NORM_FULL)
