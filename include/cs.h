@@ -50,7 +50,8 @@ typedef enum {
   CS_E_UNSUPPORTED = 5   /* valid but not supported shape/config           */
 } cs_status;
 
-typedef enum { CS_BF16 = 0, CS_FP32 = 1 } cs_dtype;
+/* CS_I8 (8-bit integers with scales): operators that name it only. */
+typedef enum { CS_BF16 = 0, CS_FP32 = 1, CS_I8 = 2 } cs_dtype;
 
 /* Cache modes.  OFF computes every call (recovers the uncached rollout
  * G(c,s)); ADAPTIVE applies the accumulated drift rule with threshold tau;
@@ -421,6 +422,93 @@ cs_status cs_kv4_attention_workspace(const cs_attn_desc* desc, size_t* bytes);
 cs_status cs_kv4_attention(const cs_attn_desc* desc, const void* q, const cs_kv4_cache* cache,
                            const int32_t* kv_of, const int32_t* kv_len, const uint8_t* kv_mask,
                            void* o, void* work, size_t work_bytes, void* stream);
+
+/* Rows of a layer norm: groups of `rows` rows each, one below the other, [groups * rows][dim]
+ * with strides x_row and y_row; dim 1..16384.  Each group has a weight and a bias of its own
+ * (strides w_group, b_group; a modulation per video), or there is one group.  unit_offset: 1 if
+ * the gain is 1 + weight, 0 if it is the weight.  y_dtype CS_I8: see cs_i8_rows. */
+typedef struct {
+  int32_t x_dtype, y_dtype;      /* cs_dtype; x CS_BF16 or CS_FP32 */
+  int32_t groups, rows, dim, unit_offset;
+  float eps;                     /* >= 0 */
+  int64_t x_row, y_row, w_group, b_group;
+} cs_layer_norm_desc;
+
+/* Layer norm of every row, in fp32 and rounded once:
+ *   y_c = (x_c - mean) rstd gain_c + bias_c,  rstd = 1 / sqrt(variance + eps).
+ * The variance is that of the centred values, over dim; a row whose squared deviations add up
+ * to 3.4e38 or more gives its bias.  weight, bias: fp32 [groups][dim], NULL for 1 and 0.  mean,
+ * rstd: fp32 [groups * rows], written for the backward pass, or NULL.  y_scale: the rows' scales
+ * where y_dtype is CS_I8 (else not read).  y may be x (same pointer, type and stride). */
+cs_status cs_layer_norm(const cs_layer_norm_desc* desc, const void* x, const float* weight, const float* bias, void* y,
+                        float* y_scale, float* mean, float* rstd, void* stream);
+
+/* Its backward pass.  x, dx are of x_dtype, dy of y_dtype (CS_BF16 or CS_FP32), strides
+ * as above. */
+typedef struct {
+  int32_t x_dtype, y_dtype;
+  int32_t groups, rows, dim, unit_offset;
+  int64_t x_row, dy_row, dx_row, w_group, dw_group, db_group;
+} cs_layer_norm_grad_desc;
+
+/* With n = (x - mean) rstd and g = dy gain, sums in fp32:
+ *   dx = rstd (g - mean(g) - n mean(g n)),
+ *   dweight = sum of dy n and dbias = sum of dy over the rows of each group, fp32
+ * [groups][dim] (one group: over all rows).  mean, rstd: as cs_layer_norm wrote them.  dx,
+ * dweight and dbias may be NULL; the workspace is needed for the last two only.  A group of no
+ * rows gets zeros there.  dx may be x or dy.  The sums over rows are taken in an order that
+ * depends on rows and dim alone: a group's gradients are bitwise the same alone and among
+ * others. */
+cs_status cs_layer_norm_backward_workspace(const cs_layer_norm_grad_desc* desc, size_t* bytes);
+cs_status cs_layer_norm_backward(const cs_layer_norm_grad_desc* desc, const void* x, const void* dy,
+                                 const float* weight, const float* mean, const float* rstd, void* dx, float* dweight,
+                                 float* dbias, void* work, size_t work_bytes, void* stream);
+
+/* Rows in 8 bits: [rows][dim] values of dtype (CS_BF16 or CS_FP32) with stride x_row, codes
+ * int8 with stride q_row, and a scale a row, fp32 [rows]; dim 1..65536.  A row's scale is its
+ * largest magnitude / 127, rounded to fp32; its codes are the integers nearest to value / scale
+ * (of the exact quotients, halfway ones to the even code), within -127..127; it stands for
+ * code * scale.  A row of zeros, or whose scale underflows to 0, has scale 0 and codes 0; one that holds an
+ * infinity or a NaN has scale NaN and codes 0.  cs_layer_norm writes the same of its results. */
+typedef struct {
+  int32_t dtype, rows, dim;
+  int64_t x_row, q_row;
+} cs_i8_rows;
+cs_status cs_i8_quantise(const cs_i8_rows* rows, const void* x, int8_t* codes, float* scales, void* stream);
+cs_status cs_i8_dequantise(const cs_i8_rows* rows, const int8_t* codes, const float* scales, void* x, void* stream);
+
+/* Weights in 8 bits, [n][k] (outputs by inputs, 1 <= k <= 65536) in the layout of the product's tiles:
+ * cs_i8_weight_bytes bytes of codes and n scales, 16-byte aligned, the caller's.
+ * cs_i8_weight_pack fills both from w, [n][k] with stride w_row: values of CS_BF16 or
+ * CS_FP32, made codes as the rows above, a scale an output, or CS_I8 codes with their scales
+ * given (fp32 [n]; NULL otherwise). */
+typedef struct {
+  int8_t* codes;
+  float* scales;
+  int32_t n, k;
+} cs_i8_weight;
+cs_status cs_i8_weight_bytes(int32_t n, int32_t k, size_t* bytes);
+cs_status cs_i8_weight_pack(const cs_i8_weight* weight, int32_t dtype, const void* w, int64_t w_row,
+                            const float* w_scales, void* stream);
+
+/* Product of `rows` rows of codes a [rows][k], stride a_row, and weights: out [rows][n] of
+ * out_dtype (CS_BF16 or CS_FP32), stride o_row. */
+typedef enum { CS_ACT_NONE = 0, CS_ACT_GELU = 1 } cs_act;
+typedef struct {
+  int32_t out_dtype, rows, n, k;
+  int32_t act;                   /* cs_act; the GELU is the tanh form */
+  int64_t a_row, o_row;
+} cs_matmul_i8_desc;
+
+/* out[m][j] = act(a_scales[m] weight.scales[j] sum_k a[m][k] w[j][k] + bias[j]).  The sum is
+ * an exact 32-bit integer (codes may be -128 too); it is scaled in fp32, by the row's scale first,
+ * and rounded once to the output's type.  bias: fp32 [n] or NULL.  Rows of a are read in whole
+ * 16-byte units: what lies between k and the next multiple of 16 may hold anything.  out must
+ * not overlap the inputs. */
+cs_status cs_matmul_i8_workspace(const cs_matmul_i8_desc* desc, size_t* bytes);
+cs_status cs_matmul_i8(const cs_matmul_i8_desc* desc, const int8_t* a, const float* a_scales,
+                       const cs_i8_weight* weight, const float* bias, void* out, void* work, size_t work_bytes,
+                       void* stream);
 
 /* ---------------------------------------------------------------- ranking */
 

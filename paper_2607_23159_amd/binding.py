@@ -19,11 +19,12 @@ import numpy as np
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcachedsearch.so")
 
 CS_OK, CS_E_INVAL, CS_E_NOMEM, CS_E_DEVICE, CS_E_STATE, CS_E_UNSUPPORTED = range(6)
-CS_BF16, CS_FP32 = 0, 1
+CS_BF16, CS_FP32, CS_I8 = 0, 1, 2
 CS_CACHE_OFF, CS_CACHE_ADAPTIVE, CS_CACHE_STATIC, CS_CACHE_PAB = 0, 1, 2, 3
 CS_QK_NORM_FULL, CS_QK_NORM_HEAD = 0, 1
 CS_KV_NATIVE, CS_KV_4BIT = 0, 1
 CS_ROPE_PAIRS, CS_ROPE_HALVES = 0, 1
+CS_ACT_NONE, CS_ACT_GELU = 0, 1
 (CS_K_SELF_ATTN, CS_K_CROSS_ATTN, CS_K_GEMM, CS_K_NORM, CS_K_DECIDE, CS_K_UPDATE, CS_K_SCORE,
  CS_K_OTHER) = range(8)
 KERNEL_FAMILIES = ["self_attn", "cross_attn", "gemm", "norm", "decide", "update", "score", "other"]
@@ -78,6 +79,29 @@ class cs_kv4_rows(C.Structure):
                 [(n, C.c_int64) for n in ("k_row", "k_head", "v_row", "v_head")])
 
 
+class cs_layer_norm_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("x_dtype", "y_dtype", "groups", "rows", "dim", "unit_offset")] +
+                [("eps", C.c_float)] + [(n, C.c_int64) for n in ("x_row", "y_row", "w_group", "b_group")])
+
+
+class cs_layer_norm_grad_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("x_dtype", "y_dtype", "groups", "rows", "dim", "unit_offset")] +
+                [(n, C.c_int64) for n in ("x_row", "dy_row", "dx_row", "w_group", "dw_group", "db_group")])
+
+
+class cs_i8_rows(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "rows", "dim")] + [(n, C.c_int64) for n in ("x_row", "q_row")])
+
+
+class cs_i8_weight(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("n", C.c_int32), ("k", C.c_int32)]
+
+
+class cs_matmul_i8_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("out_dtype", "rows", "n", "k", "act")] +
+                [(n, C.c_int64) for n in ("a_row", "o_row")])
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -120,6 +144,15 @@ def lib() -> C.CDLL:
         "cs_kv4_attention": (i32, [C.POINTER(cs_attn_desc), vp, C.POINTER(cs_kv4_cache)] + [vp] * 5 + [sz, vp]),
         "cs_kv4_store": (i32, [C.POINTER(cs_kv4_cache), C.POINTER(cs_kv4_rows)] + [vp] * 4),
         "cs_kv4_load": (i32, [C.POINTER(cs_kv4_cache), C.POINTER(cs_kv4_rows)] + [vp] * 4),
+        "cs_layer_norm": (i32, [C.POINTER(cs_layer_norm_desc)] + [vp] * 8),
+        "cs_layer_norm_backward_workspace": (i32, [C.POINTER(cs_layer_norm_grad_desc), C.POINTER(sz)]),
+        "cs_layer_norm_backward": (i32, [C.POINTER(cs_layer_norm_grad_desc)] + [vp] * 9 + [sz, vp]),
+        "cs_i8_quantise": (i32, [C.POINTER(cs_i8_rows)] + [vp] * 4),
+        "cs_i8_dequantise": (i32, [C.POINTER(cs_i8_rows)] + [vp] * 4),
+        "cs_i8_weight_bytes": (i32, [i32, i32, C.POINTER(sz)]),
+        "cs_i8_weight_pack": (i32, [C.POINTER(cs_i8_weight), i32, vp, i64, vp, vp]),
+        "cs_matmul_i8_workspace": (i32, [C.POINTER(cs_matmul_i8_desc), C.POINTER(sz)]),
+        "cs_matmul_i8": (i32, [C.POINTER(cs_matmul_i8_desc), vp, vp, C.POINTER(cs_i8_weight)] + [vp] * 3 + [sz, vp]),
         "cs_profile_enable": (i32, [vp, i32]),
         "cs_profile_reset": (i32, [vp]),
         "cs_profile_read": (i32, [vp, i32, pd, C.POINTER(i64)]),
@@ -606,18 +639,22 @@ def cs_kv4_attention_workspace(desc: _OpDesc) -> int:
     return n.value
 
 
+def _workspace(work, device):
+    """Address and bytes of a workspace (any contiguous tensor, a raw address, or None)."""
+    if work is None:
+        return None, 0
+    if isinstance(work, int):
+        return work, 1 << 62    # unchecked
+    if work.device != device or not work.is_contiguous():
+        raise ValueError(f"work: a contiguous tensor on {device} is required")
+    return work.data_ptr(), work.numel() * work.element_size()
+
+
 def _attn_rest(desc: _OpDesc, kv_of, kv_len, kv_mask, work):
     """Addresses of the index tensors (int32), the mask ([n_kv][lk] uint8, contiguous) and the
-    workspace (any contiguous tensor), and the workspace's bytes."""
+    workspace, and the workspace's bytes."""
     c, dev = desc.c, desc.device
-    nbytes = 0
-    if isinstance(work, int):
-        nbytes = 1 << 62        # unchecked
-    elif work is not None:
-        if work.device != dev or not work.is_contiguous():
-            raise ValueError(f"work: a contiguous tensor on {dev} is required")
-        nbytes = work.numel() * work.element_size()
-        work = work.data_ptr()
+    work, nbytes = _workspace(work, dev)
     if kv_mask is not None and not isinstance(kv_mask, int) and kv_mask.dim() > 1 and kv_mask.shape[-1] != c.lk:
         raise ValueError(f"kv_mask: rows of {kv_mask.shape[-1]} keys, {c.lk} required")
     return (_aux(kv_of, c.n_q, "int32", "kv_of", dev), _aux(kv_len, c.n_kv, "int32", "kv_len", dev),
@@ -642,6 +679,193 @@ def cs_kv4_attention(desc: _OpDesc, q, cache: Kv4Cache, o, kv_of=None, kv_len=No
     of, ln, mask, w, nbytes = _attn_rest(desc, kv_of, kv_len, kv_mask, work)
     _check(lib().cs_kv4_attention(desc.ref, _same(q, s["q"], "q"), cache.ref, of, ln, mask, _same(o, s["o"], "o"), w,
                                   nbytes, _op_stream(stream, desc.device)))
+
+
+def _given(x, sig, name: str) -> Optional[int]:
+    """_same for a tensor that is absent exactly where its descriptor was made without it."""
+    if (x is None) != (sig is None):
+        raise ValueError(f"{name}: the descriptor was made with{'out' if sig is None else ''} it")
+    return _same(x, sig, name)
+
+
+def _vector(x, n: int, name: str, device) -> Optional[int]:
+    """Address of n fp32 values on the operator's device, or None."""
+    return _aux(x, n, "float32", name, device)
+
+
+def _params(dim: int, groups: int, **tensors):
+    """Signatures of fp32 [groups][dim] tensors, and their strides from group to group."""
+    sig = _op_tensors("float32", 2, **tensors)
+    for n, x in tensors.items():
+        if x is not None and tuple(x.shape) != (groups, dim):
+            raise ValueError(f"{n}: shape {tuple(x.shape)}, {(groups, dim)} required")
+    return sig, [0 if x is None else x.stride(0) for x in tensors.values()]
+
+
+def _one_device(sig) -> None:
+    devices = {s[3] for s in sig.values() if s is not None}
+    if len(devices) > 1:
+        raise ValueError(f"tensors on {sorted(map(str, devices))}")
+
+
+def _norm_rows(x, groups: int):
+    """Rows of a group and channels of x [groups * rows][dim]."""
+    if groups < 1 or x.shape[0] % groups:
+        raise ValueError(f"{x.shape[0]} rows are not {groups} groups")
+    return x.shape[0] // groups, x.shape[1]
+
+
+def layer_norm_desc(x, y, weight=None, bias=None, groups: int = 1, unit_offset: bool = False,
+                    eps: float = 1e-6) -> _OpDesc:
+    """Descriptor of cs_layer_norm.  x, y: [groups * rows][dim], y bfloat16, float32 or int8 (with a
+    scale a row); weight, bias: [groups][dim] or None."""
+    sig = _op_tensors(_float_dtype(x), 2, x=x)
+    i8 = str(y.dtype).rsplit(".", 1)[-1] == "int8"
+    sig.update(_op_tensors("int8" if i8 else _float_dtype(y), 2, y=y))
+    rows, dim = _norm_rows(x, groups)
+    if y.shape != x.shape:
+        raise ValueError(f"x {tuple(x.shape)} and y {tuple(y.shape)} differ")
+    p, strides = _params(dim, groups, weight=weight, bias=bias)
+    sig.update(p)
+    _one_device(sig)
+    return _OpDesc(cs_layer_norm_desc(_DTYPES[_float_dtype(x)], CS_I8 if i8 else _DTYPES[_float_dtype(y)], groups, rows,
+                                      dim, int(unit_offset), eps, x.stride(0), y.stride(0), *strides), **sig)
+
+
+def cs_layer_norm(desc: _OpDesc, x, y, weight=None, bias=None, y_scale=None, mean=None, rstd=None, stream=None) -> None:
+    """``y_scale``: float32 [rows in all], required where y is int8; ``mean``, ``rstd``: the same or None."""
+    _on_current(desc.device)
+    s, dev, n = desc.sig, desc.device, desc.c.groups * desc.c.rows
+    _check(lib().cs_layer_norm(desc.ref, _same(x, s["x"], "x"), _given(weight, s["weight"], "weight"),
+                               _given(bias, s["bias"], "bias"), _same(y, s["y"], "y"), _vector(y_scale, n, "y_scale", dev),
+                               _vector(mean, n, "mean", dev), _vector(rstd, n, "rstd", dev), _op_stream(stream, dev)))
+
+
+def layer_norm_grad_desc(x, dy, weight=None, dx=None, dweight=None, dbias=None, groups: int = 1,
+                         unit_offset: bool = False) -> _OpDesc:
+    """Descriptor of cs_layer_norm_backward.  x, dy, dx: [groups * rows][dim], dx of x's type or None;
+    weight, dweight, dbias: float32 [groups][dim] or None."""
+    sig = _op_tensors(_float_dtype(x), 2, x=x, dx=dx)
+    sig.update(_op_tensors(_float_dtype(dy), 2, dy=dy))
+    rows, dim = _norm_rows(x, groups)
+    for n, t in (("dy", dy), ("dx", dx)):
+        if t is not None and t.shape != x.shape:
+            raise ValueError(f"x {tuple(x.shape)} and {n} {tuple(t.shape)} differ")
+    p, strides = _params(dim, groups, weight=weight, dweight=dweight, dbias=dbias)
+    sig.update(p)
+    _one_device(sig)
+    return _OpDesc(cs_layer_norm_grad_desc(_DTYPES[_float_dtype(x)], _DTYPES[_float_dtype(dy)], groups, rows, dim,
+                                           int(unit_offset), x.stride(0), dy.stride(0), 0 if dx is None else dx.stride(0),
+                                           *strides), **sig)
+
+
+def cs_layer_norm_backward_workspace(desc: _OpDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().cs_layer_norm_backward_workspace(desc.ref, C.byref(n)))
+    return n.value
+
+
+def cs_layer_norm_backward(desc: _OpDesc, x, dy, weight, mean, rstd, dx=None, dweight=None, dbias=None, work=None,
+                           stream=None) -> None:
+    """``mean``, ``rstd``: float32 [rows in all], as cs_layer_norm wrote them."""
+    _on_current(desc.device)
+    s, dev, n = desc.sig, desc.device, desc.c.groups * desc.c.rows
+    work, nbytes = _workspace(work, dev)
+    _check(lib().cs_layer_norm_backward(desc.ref, _same(x, s["x"], "x"), _same(dy, s["dy"], "dy"),
+                                        _given(weight, s["weight"], "weight"), _vector(mean, n, "mean", dev),
+                                        _vector(rstd, n, "rstd", dev), _given(dx, s["dx"], "dx"),
+                                        _given(dweight, s["dweight"], "dweight"), _given(dbias, s["dbias"], "dbias"), work,
+                                        nbytes, _op_stream(stream, dev)))
+
+
+def i8_rows_desc(x, codes, scales) -> _OpDesc:
+    """Descriptor of cs_i8_quantise and cs_i8_dequantise.  x, codes: [rows][dim], codes int8;
+    scales: float32 [rows]."""
+    t = _float_dtype(x)
+    sig = _op_tensors(t, 2, x=x)
+    sig.update(_op_tensors("int8", 2, codes=codes))
+    sig.update(_op_tensors("float32", 1, scales=scales))
+    if codes.shape != x.shape or scales.shape[0] != x.shape[0]:
+        raise ValueError(f"x {tuple(x.shape)}, codes {tuple(codes.shape)}, scales {tuple(scales.shape)}")
+    _one_device(sig)
+    return _OpDesc(cs_i8_rows(_DTYPES[t], x.shape[0], x.shape[1], x.stride(0), codes.stride(0)), **sig)
+
+
+def cs_i8_quantise(desc: _OpDesc, x, codes, scales, stream=None) -> None:
+    _on_current(desc.device)
+    s = desc.sig
+    _check(lib().cs_i8_quantise(desc.ref, _same(x, s["x"], "x"), _same(codes, s["codes"], "codes"),
+                                _same(scales, s["scales"], "scales"), _op_stream(stream, desc.device)))
+
+
+def cs_i8_dequantise(desc: _OpDesc, codes, scales, x, stream=None) -> None:
+    """The values that codes stand for into x."""
+    _on_current(desc.device)
+    s = desc.sig
+    _check(lib().cs_i8_dequantise(desc.ref, _same(codes, s["codes"], "codes"), _same(scales, s["scales"], "scales"),
+                                  _same(x, s["x"], "x"), _op_stream(stream, desc.device)))
+
+
+def cs_i8_weight_bytes(n: int, k: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().cs_i8_weight_bytes(n, k, C.byref(out)))
+    return out.value
+
+
+class I8Weight(_OpDesc):
+    """8-bit weights [n][k] in the layout of the products: an int8 tensor of cs_i8_weight_bytes
+    codes and a float32 tensor of n scales, made here, to be filled by cs_i8_weight_pack."""
+
+    def __init__(self, n: int, k: int, device="cuda"):
+        import torch
+        self.tensors = (torch.empty(cs_i8_weight_bytes(n, k), dtype=torch.int8, device=device),
+                        torch.empty(n, dtype=torch.float32, device=device))
+        codes, scales = self.tensors
+        super().__init__(cs_i8_weight(codes.data_ptr(), scales.data_ptr(), n, k), codes=_sig(codes), scales=_sig(scales))
+
+
+def cs_i8_weight_pack(weight: I8Weight, w, scales=None, stream=None) -> None:
+    """w: [n][k] of bfloat16 or float32, or int8 codes with their ``scales`` (float32 [n])."""
+    _on_current(weight.device)
+    i8 = str(w.dtype).rsplit(".", 1)[-1] == "int8"
+    sig = _op_tensors("int8" if i8 else _float_dtype(w), 2, w=w)
+    c = weight.c
+    if tuple(w.shape) != (c.n, c.k) or sig["w"][3] != weight.device:
+        raise ValueError(f"w: shape {tuple(w.shape)} on {w.device}, {(c.n, c.k)} on {weight.device} required")
+    _check(lib().cs_i8_weight_pack(weight.ref, CS_I8 if i8 else _DTYPES[_float_dtype(w)], w.data_ptr(), w.stride(0),
+                                   _vector(scales, c.n, "scales", weight.device), _op_stream(stream, weight.device)))
+
+
+def matmul_i8_desc(codes, scales, weight: I8Weight, out, act: int = CS_ACT_NONE) -> _OpDesc:
+    """Descriptor of cs_matmul_i8.  codes: int8 [rows][k]; scales: float32 [rows]; out: [rows][n]."""
+    t = _float_dtype(out)
+    sig = _op_tensors("int8", 2, codes=codes)
+    sig.update(_op_tensors("float32", 1, scales=scales))
+    sig.update(_op_tensors(t, 2, out=out))
+    c, rows = weight.c, codes.shape[0]
+    if codes.shape[1] != c.k or scales.shape[0] != rows or tuple(out.shape) != (rows, c.n):
+        raise ValueError(f"codes {tuple(codes.shape)}, scales {tuple(scales.shape)}, out {tuple(out.shape)}, weight {(c.n, c.k)}")
+    sig["weight"] = weight.sig["codes"]
+    _one_device(sig)
+    return _OpDesc(cs_matmul_i8_desc(_DTYPES[t], rows, c.n, c.k, act, codes.stride(0), out.stride(0)), **sig)
+
+
+def cs_matmul_i8_workspace(desc: _OpDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().cs_matmul_i8_workspace(desc.ref, C.byref(n)))
+    return n.value
+
+
+def cs_matmul_i8(desc: _OpDesc, codes, scales, weight: I8Weight, out, bias=None, work=None, stream=None) -> None:
+    """``bias``: float32 [n] or None."""
+    _on_current(desc.device)
+    if weight.device != desc.device:
+        raise ValueError(f"the weight is on {weight.device}, the descriptor's tensors on {desc.device}")
+    s, dev = desc.sig, desc.device
+    work, nbytes = _workspace(work, dev)
+    _check(lib().cs_matmul_i8(desc.ref, _same(codes, s["codes"], "codes"), _same(scales, s["scales"], "scales"), weight.ref,
+                              _vector(bias, desc.c.n, "bias", dev), _same(out, s["out"], "out"), work, nbytes,
+                              _op_stream(stream, dev)))
 
 
 def cs_profile_enable(model: int, on: bool) -> None:

@@ -2,9 +2,9 @@
 //
 //   C[M][N] = A[M][K] * W[N][K]^T   (A row-major, W = weights [out][in])
 //
-// Two kernels on direct global->LDS loads: k_gemm_w4 (bf16) and k_gemm_ring
-// (bf16 and fp32); ragged M and N tails are handled by the loads' buffer ranges
-// (zeros) and by masking stores.
+// Two kernels on direct global->LDS loads: k_gemm_w4 (bf16 and 8-bit integers) and
+// k_gemm_ring (those and fp32); ragged M and N tails are handled by the loads' buffer
+// ranges (zeros) and by masking stores.
 //
 // The accumulation order over K depends on the element type only, never on the
 // kernel, the tile shape or M: a row's result is bitwise the same whatever
@@ -12,7 +12,8 @@
 //
 // Every projection of the model has a bias; the accumulators start from it
 // (each column's bias, then the products in a fixed K order), so the epilogue
-// reads no bias.
+// reads no bias.  8-bit products sum to 32-bit integers, exactly; their scales and bias
+// come in after the last product (EpiI8).
 #pragma once
 #include "kernels.hpp"
 
@@ -113,6 +114,33 @@ CS_DEV void gemm_epilogue16_deep(const f32x4 (&acc)[TM][TN], int row_base, int c
 // ---------------------------------------------------------------------------
 constexpr int W_BLOCK_ROWS = 256;   // rows of a block of the tiled weights
 
+// A lane's operands and accumulators of the 16x16 products, and as many of them as use up
+// a 16-byte chunk of each.
+template <typename T> struct Mfma16;
+template <> struct Mfma16<bf16> {
+  typedef bf16x8 chunk;
+  typedef f32x4 acc;
+  static CS_DEV f32x4 mma(const chunk& a, const chunk& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <> struct Mfma16<float> {
+  typedef f32x4 chunk;
+  typedef f32x4 acc;
+  static CS_DEV f32x4 mma(const chunk& a, const chunk& b, f32x4 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+template <> struct Mfma16<int8_t> {
+  typedef i32x4 chunk;
+  typedef i32x4 acc;
+  static CS_DEV i32x4 mma(const chunk& a, const chunk& b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+  }
+};
+
 // Batched launches (blockIdx.y = item): the same A against n weight matrices
 // w_stride elements apart, with an epilogue that moves to item z (Epi::item).
 template <class Epi> struct EpiBatched : std::false_type {};
@@ -173,20 +201,43 @@ CS_DEV void gemm_tile_of(int tiles_m, int tiles_n, int& tm_i, int& tn_i) {
 // ring: each wave gets a region of max(WN (WM + 8), WM (WN + 8)) elements.
 template <class Epi> struct EpiStagesTiles : std::false_type {};
 
-CS_DEV void mfma_16x16x32_agpr(f32x4& acc, const bf16x8& a, const bf16x8& b) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+// Results of a wave's WM x WN block, through LDS (LDS bytes of it) where the epilogue stages tiles.
+template <int WM, int WN, int PD, int LDS, class Epi>
+CS_DEV void w4_store(const f32x4 (&acc)[WM / 16][WN / 16], bf16* smem, int wave, int row_base, int col_base, int n0,
+                     int lane, int M, int N, const Epi& epi) {
+  if constexpr (EpiStagesTiles<Epi>::value && WM >= 32 && WN >= 32) {
+    constexpr int STG = WN * (WM + 8) > WM * (WN + 8) ? WN * (WM + 8) : WM * (WN + 8);
+    static_assert(4 * STG * 2 <= LDS, "staging fits the ring");
+    if (epi.staged_tile(n0)) {   // uniform over the workgroup
+      __syncthreads();           // every wave's last fragment reads are done
+      epi.store_staged_tile(acc, smem + wave * STG, row_base, col_base, lane, M, N);
+      return;
+    }
+  }
+  gemm_epilogue16_deep<PD>(acc, row_base, col_base, lane, M, N, epi);
 }
 
-template <int BM, int BN, int OCC, int GM, int PD, class Epi>
-__global__ __launch_bounds__(256, OCC) void k_gemm_w4(const bf16* __restrict__ A, long lda,
-                                                    const bf16* __restrict__ W, int M, int N,
+// A 16-byte chunk of each operand per lane: 32 k of bf16, 64 of 8-bit integers, in the
+// same cycles.
+CS_DEV void mfma_agpr(f32x4& acc, const bf16x8& a, const bf16x8& b) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+CS_DEV void mfma_agpr(i32x4& acc, const i32x4& a, const i32x4& b) {
+  asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+
+template <typename T, int BM, int BN, int OCC, int GM, int PD, class Epi>
+__global__ __launch_bounds__(256, OCC) void k_gemm_w4(const T* __restrict__ A, long lda,
+                                                    const T* __restrict__ W, int M, int N,
                                                     int K, long w_stride, Epi epi) {
   if constexpr (EpiBatched<Epi>::value) {
     W += blockIdx.y * w_stride;
     epi.item(blockIdx.y);
   }
-  constexpr int BK = 64, NWAVE = 4, WM = BM / 2, WN = BN / 2;
-  constexpr int CH = 8;                       // bf16 per 16-byte chunk
+  typedef typename Mfma16<T>::chunk chunk;
+  constexpr bool I8 = sizeof(T) == 1;
+  constexpr int ES = (int)sizeof(T), BK = 128 / ES, NWAVE = 4, WM = BM / 2, WN = BN / 2;
+  constexpr int CH = 16 / ES;                 // values per 16-byte chunk
   constexpr int CPR = BK / CH;                // chunks per LDS row
   constexpr int RPI = 64 / CPR;               // rows filled by one wave instruction
   constexpr int A_INST = BM / RPI / NWAVE;    // load instructions per wave per slice
@@ -198,9 +249,9 @@ __global__ __launch_bounds__(256, OCC) void k_gemm_w4(const bf16* __restrict__ A
   // products per read: as far apart as fits a half, at most 3
   constexpr int RPM = (NM - 1) / (NF - 1) < 3 ? (NM - 1) / (NF - 1) : 3;
   static_assert(A_INST * RPI * NWAVE == BM && B_INST * RPI * NWAVE == BN, "load split");
-  static_assert(W_BLOCK_ROWS % BN == 0 && RPI * BK * 2 == 1024, "part of a tiled W block");
+  static_assert(W_BLOCK_ROWS % BN == 0 && RPI * BK * ES == 1024, "part of a tiled W block");
   static_assert(RPM * (NF - 1) < NM && NM % A_INST == 0 && NM % B_INST == 0, "interleave");
-  __shared__ __attribute__((aligned(1024))) bf16 smem[3 * A_BUF + 2 * B_BUF];
+  __shared__ __attribute__((aligned(1024))) T smem[3 * A_BUF + 2 * B_BUF];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // uniform
@@ -212,34 +263,39 @@ __global__ __launch_bounds__(256, OCC) void k_gemm_w4(const bf16* __restrict__ A
   gemm_tile_of<GM>(tiles_m, tiles_n, tm_i, tn_i);
   const int m0 = tm_i * BM, n0 = tn_i * BN;
 
-  const bf16* a_base = A + (long)m0 * lda;
+  const T* a_base = A + (long)m0 * lda;
   const int n_in = n0 % W_BLOCK_ROWS;         // first row of the tile in its W block
-  const bf16* b_base = W + (long)(n0 - n_in) * K + n_in * BK;
-  const int a_bytes = min(BM, M - m0) * (int)lda * 2, b_bytes = (W_BLOCK_ROWS * K - n_in * BK) * 2;
+  const T* b_base = W + (long)(n0 - n_in) * K + n_in * BK;
+  int a_bytes = min(BM, M - m0) * (int)lda * ES;
+  if constexpr (I8) a_bytes += epi.a_row - (int)lda;   // rows of A may end before K
+  const int b_bytes = (W_BLOCK_ROWS * K - n_in * BK) * ES;
   int a_off[A_INST], b_off[B_INST];
   {
     const int rin = lane / CPR, phys = lane % CPR;
 #pragma unroll
     for (int i = 0; i < A_INST; ++i) {
       const int row = (wave * A_INST + i) * RPI + rin;
-      a_off[i] = (row * (int)lda + (phys ^ gemm_swz(row)) * CH) * 2;
+      a_off[i] = (row * (int)lda + (phys ^ gemm_swz(row)) * CH) * ES;
     }
 #pragma unroll
     for (int i = 0; i < B_INST; ++i) b_off[i] = (wave * B_INST + i) * 1024 + lane * 16;
   }
-  bf16* const sb0 = smem + 3 * A_BUF;
+  T* const sb0 = smem + 3 * A_BUF;
   // load instruction r of the A (W) rows of slice `slice` into A buffer ab (W buffer bb)
   auto load_a = [&](int r, int slice, int ab) {
-    buffer_load_lds16(a_base, a_bytes, smem + ab * A_BUF + (wave * A_INST + r) * RPI * BK, a_off[r],
-                      slice * BK * 2);
+    T* const dst = smem + ab * A_BUF + (wave * A_INST + r) * RPI * BK;
+    if constexpr (I8)   // the range ends inside a row: the slice moves its start
+      buffer_load_lds16(a_base + slice * BK, a_bytes - slice * BK, dst, a_off[r], 0);
+    else
+      buffer_load_lds16(a_base, a_bytes, dst, a_off[r], slice * BK * ES);
   };
   auto load_b = [&](int r, int slice, int bb) {
     buffer_load_lds16(b_base, b_bytes, sb0 + bb * B_BUF + (wave * B_INST + r) * RPI * BK, b_off[r],
-                      slice * W_BLOCK_ROWS * BK * 2);
+                      slice * W_BLOCK_ROWS * BK * ES);
   };
 
-  f32x4 acc[TM][TN];
-  init_acc16_bias(acc, epi.bias, n0 + wn * WN, lane, N);
+  typename Mfma16<T>::acc acc[TM][TN] = {};
+  if constexpr (!I8) init_acc16_bias(acc, epi.bias, n0 + wn * WN, lane, N);
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -257,22 +313,22 @@ __global__ __launch_bounds__(256, OCC) void k_gemm_w4(const bf16* __restrict__ A
                         b_row0 * BK + ((4 + quad) ^ gemm_swz(b_row0)) * CH};
   // read r (< NF) of k-step ks from A buffer ab / W buffer bb: W fragments
   // first (the first products of the next half use all of them)
-  auto read = [&](int r, int ab, int bb, int ks, bf16x8(&fa)[TM], bf16x8(&fb)[TN]) {
+  auto read = [&](int r, int ab, int bb, int ks, chunk(&fa)[TM], chunk(&fb)[TN]) {
     if (r < TN)
-      fb[r] = *reinterpret_cast<const bf16x8*>(sb0 + bb * B_BUF + b_lds[ks] + r * 16 * BK);
+      fb[r] = *reinterpret_cast<const chunk*>(sb0 + bb * B_BUF + b_lds[ks] + r * 16 * BK);
     else
-      fa[r - TN] = *reinterpret_cast<const bf16x8*>(smem + ab * A_BUF + a_lds[ks] + (r - TN) * 16 * BK);
+      fa[r - TN] = *reinterpret_cast<const chunk*>(smem + ab * A_BUF + a_lds[ks] + (r - TN) * 16 * BK);
   };
 
-  bf16x8 f0a[TM], f0b[TN], f1a[TM], f1b[TN];
+  chunk f0a[TM], f0b[TN], f1a[TM], f1b[TN];
   // One half: the NM products of (pa, pb); after product RPM*r, read r into
   // (na, nb) (RD); NL loads spread evenly, through `ld` (LD).
-  auto half = [&](auto rd, auto ldf, auto nl, const bf16x8(&pa)[TM], const bf16x8(&pb)[TN],
-                  bf16x8(&na)[TM], bf16x8(&nb)[TN], int ab, int bb, int ks) {
+  auto half = [&](auto rd, auto ldf, auto nl, const chunk(&pa)[TM], const chunk(&pb)[TN],
+                  chunk(&na)[TM], chunk(&nb)[TN], int ab, int bb, int ks) {
     constexpr int NL = decltype(nl)::value;
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
-      mfma_16x16x32_agpr(acc[q / TN][q % TN], pb[q % TN], pa[q / TN]);
+      mfma_agpr(acc[q / TN][q % TN], pb[q % TN], pa[q / TN]);
       if constexpr (NL > 0) {
         if (q % (NM / NL) == NM / NL / 2) ldf(q / (NM / NL));
       }
@@ -337,16 +393,14 @@ __global__ __launch_bounds__(256, OCC) void k_gemm_w4(const bf16* __restrict__ A
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));  // read only after the nops
-  if constexpr (EpiStagesTiles<Epi>::value && WM >= 32 && WN >= 32) {
-    constexpr int STG = WN * (WM + 8) > WM * (WN + 8) ? WN * (WM + 8) : WM * (WN + 8);
-    static_assert(NWAVE * STG <= 3 * A_BUF + 2 * B_BUF, "staging fits the ring");
-    if (epi.staged_tile(n0)) {   // uniform over the workgroup
-      __syncthreads();           // every wave's last fragment reads are done
-      epi.store_staged_tile(acc, smem + wave * STG, m0 + wm * WM, n0 + wn * WN, lane, M, N);
-      return;
-    }
+  constexpr int LDS = (3 * A_BUF + 2 * B_BUF) * ES;
+  if constexpr (I8) {
+    f32x4 out[TM][TN];
+    epi.scaled(acc, out, m0 + wm * WM, n0 + wn * WN, lane, M, N);
+    w4_store<WM, WN, PD, LDS>(out, (bf16*)smem, wave, m0 + wm * WM, n0 + wn * WN, n0, lane, M, N, epi.to);
+  } else {
+    w4_store<WM, WN, PD, LDS>(acc, (bf16*)smem, wave, m0 + wm * WM, n0 + wn * WN, n0, lane, M, N, epi);
   }
-  gemm_epilogue16_deep<PD>(acc, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi);
 }
 
 // ---------------------------------------------------------------------------
@@ -386,22 +440,6 @@ __global__ __launch_bounds__(256, OCC) void k_gemm_w4(const bf16* __restrict__ A
 // of whole evaluations and rollouts to 64-bit results (8 shapes, 8 seeds each)
 // is that of sums in natural k order: 4.4e-7 at d = 128, 1.45e-6 at d = 1536.
 // ---------------------------------------------------------------------------
-template <typename T> struct Mfma16;
-template <> struct Mfma16<bf16> {
-  typedef bf16x8 chunk;
-  static CS_DEV f32x4 mma(const chunk& a, const chunk& b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-  }
-};
-template <> struct Mfma16<float> {
-  typedef f32x4 chunk;
-  static CS_DEV f32x4 mma(const chunk& a, const chunk& b, f32x4 c) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-    return c;
-  }
-};
-
 template <typename T, int BM, int BN, int WGM, int WGN, int SL, int STAGES, int OCC, int GM, class Epi>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __restrict__ A, long lda,
                                                                   const T* __restrict__ W, int M,
@@ -411,6 +449,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
     epi.item(blockIdx.y);
   }
   typedef typename Mfma16<T>::chunk chunk;
+  constexpr bool I8 = sizeof(T) == 1;
   constexpr int ES = (int)sizeof(T), CH = 16 / ES, BK = 8 * CH, RPI = 8, NWAVE = WGM * WGN;
   constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, NF = TM + TN;
   constexpr int A_INST = BM / RPI / NWAVE, B_INST = BN / RPI / NWAVE;
@@ -421,7 +460,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
   static_assert(STAGES >= 2 && STAGES <= 4, "wait counts below");
   // the ring, then 1 KB of bias per wave.  One array: the compiler waits for all
   // direct loads before a read of a second one.
-  __shared__ __attribute__((aligned(1024))) T smem[STAGES * STAGE + NWAVE * 1024 / ES];
+  __shared__ __attribute__((aligned(1024))) T smem[STAGES * STAGE + (I8 ? 0 : NWAVE * 1024 / ES)];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // uniform
@@ -455,9 +494,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
       T* sa = smem + st * STAGE + l * SLICE;
       T* sb = sa + BM * BK;
       const int slice = min(step * SL + l, nslice - 1);
+      int range = a_bytes;
+      if constexpr (I8) range += min(0, epi.a_row - (slice + 1) * BK);   // rows of A may end before K
 #pragma unroll
       for (int i = 0; i < A_INST; ++i)
-        buffer_load_lds16(a_base + (long)slice * BK, a_bytes, sa + (wave * A_INST + i) * RPI * BK, a_off[i], 0);
+        buffer_load_lds16(a_base + (long)slice * BK, range, sa + (wave * A_INST + i) * RPI * BK, a_off[i], 0);
 #pragma unroll
       for (int i = 0; i < B_INST; ++i)
         buffer_load_lds16(b_base + (long)slice * W_BLOCK_ROWS * BK, b_bytes,
@@ -470,7 +511,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
   // would be waited for by the compiler, which cannot count the conditional loads
   // behind it and waits for all of them, the whole ring, before the first product.
   T* const s_bias = smem + STAGES * STAGE + wave * (1024 / ES);
-  buffer_load_lds16(epi.bias, N * 4, s_bias, (n0 + wn * WN) * 4 + lane * 16, 0);
+  if constexpr (!I8) buffer_load_lds16(epi.bias, N * 4, s_bias, (n0 + wn * WN) * 4 + lane * 16, 0);
 
 #pragma unroll
   for (int s = 0; s < STAGES; ++s)
@@ -495,12 +536,16 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
   };
   if (nstep >= STAGES) wait_all_barrier<(STAGES - 1) * PER>();   // bias and step 0 landed
   else wait_all_barrier<0>();
-  f32x4 acc[TM][TN];
+  typename Mfma16<T>::acc acc[TM][TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-      acc[i][j] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(s_bias) + 16 * j + 4 * (lane >> 4));
+    for (int i = 0; i < TM; ++i) {
+      if constexpr (I8)
+        acc[i][j] = i32x4{0, 0, 0, 0};
+      else
+        acc[i][j] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(s_bias) + 16 * j + 4 * (lane >> 4));
+    }
   read(0, f[0]);
   auto mul = [&](int step, const chunk(&o)[2 * SL][NF]) {
 #pragma unroll
@@ -534,7 +579,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
   }
   if (k < nstep) step(k, f[0], f[1]);
 
-  gemm_epilogue16_deep<2>(acc, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi);
+  if constexpr (I8) {
+    f32x4 out[TM][TN];
+    epi.scaled(acc, out, m0 + wm * WM, n0 + wn * WN, lane, M, N);
+    gemm_epilogue16_deep<2>(out, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi.to);
+  } else {
+    gemm_epilogue16_deep<2>(acc, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi);
+  }
 }
 
 // ------------------------------------------------------------- epilogues
@@ -798,5 +849,73 @@ struct EpiHead {
     *reinterpret_cast<float2*>(dst + Wd) = make_float2(v[2], v[3]);
   }
 };
+
+// 8-bit products: acc scale_a[row] scale_w[column] + bias[column] (bias NULL: 0), in fp32,
+// goes on to `to`.  a_row: bytes of a row of A that may be read, a multiple of 16; what lies
+// there past K meets zeros of W.
+CS_DEV float i8_value(int acc, float sa, float sw, float bias) { return fmaf((float)acc * sa, sw, bias); }
+
+template <class To> struct EpiI8 {
+  const float *scale_a, *scale_w, *bias;
+  int a_row;
+  To to;
+  // Four columns from col0 on of a vector of n (its rows need not end on a multiple of 4).
+  static CS_DEV f32x4 four(const float* p, int col0, int n) {
+    if (col0 + 4 <= n) return *reinterpret_cast<const f32x4*>(p + col0);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 3; ++r)
+      if (col0 + r < n) v[r] = p[col0 + r];
+    return v;
+  }
+  template <int TM, int TN>
+  CS_DEV void scaled(const i32x4 (&acc)[TM][TN], f32x4 (&out)[TM][TN], int row_base, int col_base, int lane, int M,
+                     int N) const {
+    float sa[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = scale_a[min(row_base + 16 * i + (lane & 15), M - 1)];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int col0 = col_base + 16 * j + 4 * (lane >> 4);
+      const f32x4 sw = four(scale_w, col0, N), b = bias ? four(bias, col0, N) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[i][j][r] = i8_value(acc[i][j][r], sa[i], sw[r], b[r]);
+    }
+  }
+};
+
+// The product by itself: T [M][N] of any N, rows on 16 bytes.
+template <typename T, int ACT> struct EpiMatmul {
+  T* out; long ldo; int n;
+  typedef NoPre Pre;
+  CS_DEV Pre pre(int, int) const { return {}; }
+  CS_DEV void operator()(int row, int col0, const float* v, const Pre&) const {
+    float y[4] = {v[0], v[1], v[2], v[3]};
+    if constexpr (ACT == 1) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = gelu_tanh(y[r]);
+    }
+    T* p = out + (long)row * ldo + col0;
+    if (col0 + 4 <= n) {
+      store4<T>(p, y);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 3; ++r)
+        if (col0 + r < n) p[r] = to_t<T>(y[r]);
+    }
+  }
+  CS_DEV bool staged_tile(int) const { return true; }
+  template <int TM, int TN>
+  CS_DEV void store_staged_tile(const f32x4 (&acc)[TM][TN], bf16* stage, int row_base, int col_base,
+                                int lane, int M, int N) const {
+    if constexpr (ACT == 1)
+      store_rows_staged(acc, stage, row_base, col_base, lane, M, N, out, ldo, GeluF{});
+    else
+      store_rows_staged(acc, stage, row_base, col_base, lane, M, N, out, ldo, IdentityF{});
+  }
+};
+template <int ACT> struct EpiStagesTiles<EpiMatmul<bf16, ACT>> : std::true_type {};
 
 }  // namespace cs

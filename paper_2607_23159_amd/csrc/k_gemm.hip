@@ -60,7 +60,7 @@ template <int BM, int BN, int OCC, int PD, class Epi>
 static void launch_w4(const bf16* A, long lda, const bf16* W, int M, int N, int K, GemmBatch b, const Epi& epi,
                       hipStream_t st) {
   const unsigned tiles = (unsigned)((long)cdiv(M, BM) * cdiv(N, BN));
-  hipLaunchKernelGGL((k_gemm_w4<BM, BN, OCC, GROUP_M, PD, Epi>), dim3(tiles, (unsigned)b.n), dim3(256), 0, st, A, lda,
+  hipLaunchKernelGGL((k_gemm_w4<bf16, BM, BN, OCC, GROUP_M, PD, Epi>), dim3(tiles, (unsigned)b.n), dim3(256), 0, st, A, lda,
                      W, M, N, K, b.w_stride, epi);
 }
 

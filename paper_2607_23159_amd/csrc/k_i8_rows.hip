@@ -1,0 +1,135 @@
+// Rows to 8-bit codes with a scale each, and back (cs_i8_quantise, cs_i8_dequantise), and the
+// layout of 8-bit weights (cs_i8_weight_pack).  Bound by memory.
+#include "gemm_kernel.hpp"
+#include "ops.hpp"
+#include "row_tile.hpp"
+
+namespace cs {
+
+template <typename X, int U, int WPR, int NV>
+__global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void k_i8_quantise(I8RowsArgs a) {
+  __shared__ uint32_t lds[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long row = WPR == 1 ? (long)blockIdx.x * 4 + wave : blockIdx.x;
+  if (row >= a.d.rows) return;
+  const int dim = a.d.dim, t = WPR == 1 ? lane : (int)threadIdx.x;
+  const X* x = (const X*)a.x + row * a.d.x_row;
+  typename Chunk<X, U>::vec raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = U * (64 * WPR * i + t);
+    raw[i] = load_chunk<X, U>(x + c, dim - c);
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < U; ++e) m = max(m, abs_bits(to_f(raw[i][e])));
+  const I8Scale s(row_max<WPR>(m, lds, wave));
+  if (t == 0) a.scales[row] = s.scale;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = U * (64 * WPR * i + t);
+    float y[U];
+#pragma unroll
+    for (int e = 0; e < U; ++e) y[e] = s.code(to_f(raw[i][e]));
+    store_codes<U>(a.codes + row * a.d.q_row + c, dim - c, y);
+  }
+}
+
+template <typename X, int U>
+__global__ __launch_bounds__(256) void k_i8_dequantise(I8RowsArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.d.rows) return;
+  const float scale = a.scales[row];
+  const int8_t* q = a.codes + row * a.d.q_row;
+  X* x = (X*)a.x_out + row * a.d.x_row;
+  for (int c = U * lane; c < a.d.dim; c += 64 * U) {
+    const auto v = load_chunk<int8_t, U>(q + c, a.d.dim - c);
+    float y[U];
+#pragma unroll
+    for (int e = 0; e < U; ++e) y[e] = scale * (float)v[e];
+    store_chunk<X, U>(x + c, a.d.dim - c, y);
+  }
+}
+
+template <typename X> static hipError_t quantise(const I8RowsArgs& a, hipStream_t st) {
+  constexpr int U = sizeof(X) == 2 ? 8 : 4;
+  const int dim = a.d.dim;
+  const unsigned four = (unsigned)(((long)a.d.rows + 3) / 4), one = (unsigned)a.d.rows;
+  if (dim <= 512) hipLaunchKernelGGL((k_i8_quantise<X, U, 1, 8 / U>), dim3(four), dim3(256), 0, st, a);
+  else if (dim <= 2048) hipLaunchKernelGGL((k_i8_quantise<X, U, 1, 32 / U>), dim3(four), dim3(256), 0, st, a);
+  else if (dim <= 8192) hipLaunchKernelGGL((k_i8_quantise<X, U, 4, 32 / U>), dim3(one), dim3(256), 0, st, a);
+  else if (dim <= 16384) hipLaunchKernelGGL((k_i8_quantise<X, U, 4, 64 / U>), dim3(one), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_i8_quantise<X, U, 16, 64 / U>), dim3(one), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t i8_quantise(const I8RowsArgs& a, hipStream_t st) {
+  return a.d.dtype == CS_BF16 ? quantise<bf16>(a, st) : quantise<float>(a, st);
+}
+
+hipError_t i8_dequantise(const I8RowsArgs& a, hipStream_t st) {
+  const unsigned four = (unsigned)(((long)a.d.rows + 3) / 4);
+  if (a.d.dtype == CS_BF16) hipLaunchKernelGGL((k_i8_dequantise<bf16, 8>), dim3(four), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_i8_dequantise<float, 4>), dim3(four), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+// -------------------------------------------------------------- 8-bit weights
+// The layout of gemm_tile_weight with 128 codes to a row of a block; rows past n and columns
+// past k are zero.  A wave per row of the padded matrix.  W int8_t: codes and scales given.
+template <typename W>
+__global__ __launch_bounds__(256) void k_i8_weight(const W* __restrict__ w, long w_row, const float* __restrict__ given,
+                                                   int n, int k, int rows, int8_t* __restrict__ codes,
+                                                   float* __restrict__ scales) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const bool real = row < n;
+  const W* src = w + (real ? row * w_row : 0);
+  const int nk = (k + 127) / 128;
+  int8_t* dst = codes + ((long)(row / W_BLOCK_ROWS) * nk * W_BLOCK_ROWS + row % W_BLOCK_ROWS) * 128;
+  uint32_t m = 0;
+  if constexpr (sizeof(W) > 1) {
+    if (real)
+      for (int c = lane; c < k; c += 64) m = max(m, abs_bits(to_f(src[c])));
+    m = row_max<1>(m, nullptr, 0);
+  }
+  const I8Scale s(m);
+  if (real && lane == 0) {
+    if constexpr (sizeof(W) > 1) scales[row] = s.scale;
+    else scales[row] = given[row];
+  }
+  for (int q = lane; q < nk * 8; q += 64) {
+    const int kt = q >> 3, chunk = q & 7;
+    union { int8_t b[16]; uint4 v; } o;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int c = kt * 128 + chunk * 16 + e;
+      o.b[e] = 0;
+      if (real && c < k) {
+        if constexpr (sizeof(W) > 1) o.b[e] = (int8_t)(int)s.code(to_f(src[c]));
+        else o.b[e] = src[c];
+      }
+    }
+    *reinterpret_cast<uint4*>(dst + (long)kt * W_BLOCK_ROWS * 128 + (chunk ^ gemm_swz(row)) * 16) = o.v;
+  }
+}
+
+long i8_weight_bytes(int n, int k) { return round_up(n, W_BLOCK_ROWS) * round_up(k, 128); }
+
+hipError_t i8_weight_pack(const cs_i8_weight& o, int dtype, const void* w, long w_row, const float* given,
+                          hipStream_t st) {
+  const int rows = (int)round_up(o.n, W_BLOCK_ROWS);
+  const dim3 grid((unsigned)(rows / 4)), block(256);
+  if (dtype == CS_BF16)
+    hipLaunchKernelGGL(k_i8_weight<bf16>, grid, block, 0, st, (const bf16*)w, w_row, given, o.n, o.k, rows, o.codes, o.scales);
+  else if (dtype == CS_FP32)
+    hipLaunchKernelGGL(k_i8_weight<float>, grid, block, 0, st, (const float*)w, w_row, given, o.n, o.k, rows, o.codes, o.scales);
+  else
+    hipLaunchKernelGGL(k_i8_weight<int8_t>, grid, block, 0, st, (const int8_t*)w, w_row, given, o.n, o.k, rows, o.codes, o.scales);
+  return hipGetLastError();
+}
+
+}  // namespace cs

@@ -1,0 +1,289 @@
+// Layer norm by itself, forward and backward (cs_layer_norm, cs_layer_norm_backward), on
+// rows held in registers (row_tile.hpp).  Both are bound by memory.
+#include "ops.hpp"
+#include "row_tile.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace cs {
+
+// Chunks of a lane and waves of a row, by the row's length; LN_MAX_DIM is the last one's.
+template <int WPR, int VPL> struct RowShape { static constexpr int wpr = WPR, vpl = VPL; };
+template <class F> static hipError_t with_shape(int dim, F f) {
+  if (dim <= 512) return f(RowShape<1, 8>{});
+  if (dim <= 2048) return f(RowShape<1, 32>{});
+  if (dim <= 8192) return f(RowShape<4, 32>{});
+  return f(RowShape<4, 64>{});
+}
+
+// ------------------------------------------------------------------ forward
+//   y = (x - mean) rstd gain + bias,  gain = weight or 1 + weight,
+//   mean and variance from the row in registers, the variance of the centred values.
+// Y int8_t: the result, in fp32, goes on to codes and the row's scale.
+template <typename X, typename Y, int U, int WPR, int NV>
+__global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
+  __shared__ float lds[3][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long row = WPR == 1 ? (long)blockIdx.x * 4 + wave : blockIdx.x;
+  const long total = (long)a.d.groups * a.d.rows;
+  if (row >= total) return;   // whole waves, and whole workgroups at WPR 4
+  const int dim = a.d.dim, t = WPR == 1 ? lane : (int)threadIdx.x;
+  const X* x = (const X*)a.x + row * a.d.x_row;
+  typename Chunk<X, U>::vec raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = U * (64 * WPR * i + t);
+    raw[i] = load_chunk<X, U>(x + c, dim - c);
+  }
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < U; ++e) s += to_f(raw[i][e]);
+  const float mean = row_sum<WPR>(s, lds[0], wave) / (float)dim;
+  float q = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int left = dim - U * (64 * WPR * i + t);
+#pragma unroll
+    for (int e = 0; e < U; ++e) {
+      const float z = to_f(raw[i][e]) - mean;
+      q += e < left ? z * z : 0.0f;
+    }
+  }
+  const float rstd = 1.0f / sqrtf(row_sum<WPR>(q, lds[1], wave) / (float)dim + a.d.eps);
+  if (t == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  const int group = (int)((uint32_t)row / (uint32_t)a.d.rows);   // rows in all are below 2^31
+  const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
+  const float* b = a.bias ? a.bias + group * a.d.b_group : nullptr;
+  const float one = a.d.unit_offset ? 1.0f : 0.0f;
+  // the result of chunk i
+  auto result = [&](int i, float* y) {
+    const int c = U * (64 * WPR * i + t);
+    f32x4 wv[U / 4], bv[U / 4];
+#pragma unroll
+    for (int h = 0; h < U / 4; ++h) {
+      wv[h] = bv[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (w) wv[h] = load_chunk<float, 4>(w + c + 4 * h, dim - c - 4 * h);
+      if (b) bv[h] = load_chunk<float, 4>(b + c + 4 * h, dim - c - 4 * h);
+    }
+#pragma unroll
+    for (int e = 0; e < U; ++e) {
+      const float n = (to_f(raw[i][e]) - mean) * rstd;
+      y[e] = fmaf(n, w ? one + wv[e / 4][e % 4] : 1.0f, bv[e / 4][e % 4]);
+    }
+  };
+  if constexpr (std::is_same<Y, int8_t>::value) {
+    float y[NV][U];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int left = dim - U * (64 * WPR * i + t);
+      result(i, y[i]);
+#pragma unroll
+      for (int e = 0; e < U; ++e) m = max(m, e < left ? abs_bits(y[i][e]) : 0u);
+    }
+    const I8Scale s8(row_max<WPR>(m, (uint32_t*)lds[2], wave));
+    if (t == 0) a.y_scale[row] = s8.scale;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = U * (64 * WPR * i + t);
+#pragma unroll
+      for (int e = 0; e < U; ++e) y[i][e] = s8.code(y[i][e]);
+      store_codes<U>((int8_t*)a.y + row * a.d.y_row + c, dim - c, y[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = U * (64 * WPR * i + t);
+      float y[U];
+      result(i, y);
+      store_chunk<Y, U>((Y*)a.y + row * a.d.y_row + c, dim - c, y);
+    }
+  }
+}
+
+template <typename X, typename Y>
+static hipError_t forward(const LayerNormArgs& a, hipStream_t st) {
+  const long total = (long)a.d.groups * a.d.rows;
+  return with_shape(a.d.dim, [&](auto shape) {
+    typedef decltype(shape) S;
+    constexpr int U = sizeof(X) == 2 ? 8 : 4;   // x alone decides: a row's sums do not depend on y's type
+    const unsigned grid = (unsigned)(S::wpr == 1 ? (total + 3) / 4 : total);
+    hipLaunchKernelGGL((k_layer_norm_op<X, Y, U, S::wpr, S::vpl / U>), dim3(grid), dim3(256), 0, st, a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t layer_norm(const LayerNormArgs& a, hipStream_t st) {
+  if (a.d.x_dtype == CS_BF16)
+    return a.d.y_dtype == CS_BF16   ? forward<bf16, bf16>(a, st)
+           : a.d.y_dtype == CS_FP32 ? forward<bf16, float>(a, st)
+                                    : forward<bf16, int8_t>(a, st);
+  return a.d.y_dtype == CS_BF16   ? forward<float, bf16>(a, st)
+         : a.d.y_dtype == CS_FP32 ? forward<float, float>(a, st)
+                                  : forward<float, int8_t>(a, st);
+}
+
+// ----------------------------------------------------------------- backward
+// With n = (x - mean) rstd and g = dy gain:
+//   dx = rstd (g - mean(g) - n mean(g n)),  dw = sum over rows of dy n,  db = sum of dy.
+// A workgroup takes LN_PART-th of a group's rows (ln_part_rows) and keeps its lanes' parts of
+// dw and db in registers; its sums go to the workspace, [group][part][2][dim], and a second
+// launch adds a group's parts up in order.
+int ln_part_rows(int rows) {
+  // about 512 parts of a long group, 16 rows at least: the sums that leave stay a
+  // fraction of the rows that come in
+  return (int)std::max<long>(16, (cdiv(rows, 512) + 3) / 4 * 4);
+}
+static int ln_parts(int rows) { return cdiv(rows, ln_part_rows(rows)); }
+
+size_t layer_norm_backward_workspace(const cs_layer_norm_grad_desc& d) {
+  return (size_t)d.groups * ln_parts(d.rows) * 2 * round_up(d.dim, 4) * sizeof(float);
+}
+
+template <typename X, typename Y, int U, int WPR, int NV>
+__global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, int parts, int part_rows) {
+  __shared__ float lds[2][2][4];
+  __shared__ float sums[WPR == 1 ? 4 * 64 * U : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = blockIdx.x / parts, part = blockIdx.x - group * parts;
+  const int dim = a.d.dim, t = WPR == 1 ? lane : (int)threadIdx.x;
+  const int first = part * part_rows, last = min(first + part_rows, a.d.rows);
+  const float one = a.d.unit_offset ? 1.0f : 0.0f;
+  const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
+  float dw[NV][U] = {}, db[NV][U] = {};
+  int odd = 0;
+  for (int r = first + (WPR == 1 ? wave : 0); r < last; r += WPR == 1 ? 4 : 1, odd ^= 1) {
+    const long row = (long)group * a.d.rows + r;
+    const X* x = (const X*)a.x + row * a.d.x_row;
+    const Y* dy = (const Y*)a.dy + row * a.d.dy_row;
+    typename Chunk<X, U>::vec xv[NV];
+    typename Chunk<Y, U>::vec dv[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = U * (64 * WPR * i + t);
+      xv[i] = load_chunk<X, U>(x + c, dim - c);
+      dv[i] = load_chunk<Y, U>(dy + c, dim - c);
+    }
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.0f, s2 = 0.0f;
+    auto gain = [&](int i, float* o) {
+      const int c = U * (64 * WPR * i + t);
+#pragma unroll
+      for (int h = 0; h < U / 4; ++h) {
+        const f32x4 v = w ? load_chunk<float, 4>(w + c + 4 * h, dim - c - 4 * h) : f32x4{};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[4 * h + e] = w ? one + v[e] : 1.0f;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float gw[U];
+      gain(i, gw);
+#pragma unroll
+      for (int e = 0; e < U; ++e) {
+        const float d = to_f(dv[i][e]), n = (to_f(xv[i][e]) - mean) * rstd, g = d * gw[e];
+        dw[i][e] = fmaf(d, n, dw[i][e]);
+        db[i][e] += d;
+        s1 += g;             // channels past the end have dy 0
+        s2 = fmaf(g, n, s2);
+      }
+    }
+    const float m1 = row_sum<WPR>(s1, lds[odd][0], wave) / (float)dim;
+    const float m2 = row_sum<WPR>(s2, lds[odd][1], wave) / (float)dim;
+    if (a.dx) {
+      X* dx = (X*)a.dx + row * a.d.dx_row;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = U * (64 * WPR * i + t);
+        float gw[U], o[U];
+        gain(i, gw);
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+          const float n = (to_f(xv[i][e]) - mean) * rstd;
+          o[e] = rstd * (fmaf(to_f(dv[i][e]), gw[e], -m1) - n * m2);
+        }
+        store_chunk<X, U>(dx + c, dim - c, o);
+      }
+    }
+  }
+  if (!a.part) return;
+  const long ld = (dim + 3) & ~3;
+  float* out = a.part + ((long)group * parts + part) * 2 * ld;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = U * (64 * WPR * i + t);
+      float v[U];
+#pragma unroll
+      for (int e = 0; e < U; ++e) v[e] = k ? db[i][e] : dw[i][e];
+      if constexpr (WPR == 1) {
+        // the four waves' rows, added in order by the first
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < U; ++e) sums[(wave * U + e) * 64 + lane] = v[e];
+        __syncthreads();
+        if (wave != 0) continue;
+#pragma unroll
+        for (int e = 0; e < U; ++e)
+          v[e] = ((sums[e * 64 + lane] + sums[(U + e) * 64 + lane]) + sums[(2 * U + e) * 64 + lane]) +
+                 sums[(3 * U + e) * 64 + lane];
+      }
+#pragma unroll
+      for (int h = 0; h < U / 4; ++h)
+        if (c + 4 * h < dim)   // whole chunks: the workspace's rows are padded to 4
+          *reinterpret_cast<f32x4*>(out + k * ld + c + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+    }
+}
+
+// The parts' sums, a channel a lane and a quarter of the parts a wave.
+__global__ __launch_bounds__(256) void k_layer_norm_grad_sum(LayerNormGradArgs a, int parts) {
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int cols = (a.d.dim + 63) / 64, group = blockIdx.x / cols, k = blockIdx.y;
+  const int c = (blockIdx.x - group * cols) * 64 + lane;
+  const long ld = (a.d.dim + 3) & ~3;
+  const float* p = a.part + ((long)group * parts * 2 + k) * ld + c;
+  const int per = (parts + 3) / 4, first = wave * per, last = min(first + per, parts);
+  float s = 0.0f;
+  if (c < a.d.dim)
+    for (int i = first; i < last; ++i) s += p[(long)i * 2 * ld];
+  sums[wave][lane] = s;
+  __syncthreads();
+  float* out = k ? a.dbias : a.dweight;
+  if (wave == 0 && c < a.d.dim && out)
+    out[group * (k ? a.d.db_group : a.d.dw_group) + c] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+}
+
+template <typename X, typename Y>
+static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
+  const int parts = ln_parts(a.d.rows), part_rows = ln_part_rows(a.d.rows);
+  if (a.d.rows > 0) {
+    const hipError_t s = with_shape(a.d.dim, [&](auto shape) {
+      typedef decltype(shape) S;
+      constexpr int U = std::is_same<X, bf16>::value && std::is_same<Y, bf16>::value ? 8 : 4;
+      hipLaunchKernelGGL((k_layer_norm_grad<X, Y, U, S::wpr, S::vpl / U>), dim3((unsigned)a.d.groups * parts), dim3(256),
+                         0, st, a, parts, part_rows);
+      return hipGetLastError();
+    });
+    if (s != hipSuccess) return s;
+  }
+  if (!a.dweight && !a.dbias) return hipSuccess;
+  hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)((long)cdiv(a.d.dim, 64) * a.d.groups), 2), dim3(256), 0, st, a,
+                     parts);
+  return hipGetLastError();
+}
+
+hipError_t layer_norm_backward(const LayerNormGradArgs& a, hipStream_t st) {
+  if (a.d.x_dtype == CS_BF16)
+    return a.d.y_dtype == CS_BF16 ? backward<bf16, bf16>(a, st) : backward<bf16, float>(a, st);
+  return a.d.y_dtype == CS_BF16 ? backward<float, bf16>(a, st) : backward<float, float>(a, st);
+}
+
+}  // namespace cs

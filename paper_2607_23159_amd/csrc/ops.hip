@@ -8,7 +8,7 @@
 
 using namespace cs;
 
-static int elem(int dtype) { return dtype == CS_BF16 ? 2 : 4; }
+static int elem(int dtype) { return dtype == CS_BF16 ? 2 : dtype == CS_I8 ? 1 : 4; }
 static bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 static cs_status check_dtype(int dtype) {
@@ -35,6 +35,16 @@ static cs_status check_stride(long s, long n, int esz, const char* name) {
 static cs_status check_out_stride(long s, long n, int esz, const char* name) {
   TRY(check_stride(s, n, esz, name));
   CHECK(n <= 1 || s > 0, CS_E_INVAL, "output stride %s must be positive", name);
+  return CS_OK;
+}
+
+// A tensor that may be absent.
+static cs_status check_optional(const void* p, const char* name) { return p ? check_tensor(p, name) : CS_OK; }
+
+static cs_status check_work(const void* work, size_t bytes, size_t need) {
+  if (need == 0) return CS_OK;
+  CHECK(work && aligned(work), CS_E_INVAL, "a 16-byte aligned workspace is needed");
+  CHECK(bytes >= need, CS_E_INVAL, "the workspace holds %zu bytes, %zu needed", bytes, need);
   return CS_OK;
 }
 
@@ -202,11 +212,7 @@ static cs_status attn_call(const cs_attn_desc* d, const void* q, const void* k, 
     TRY(check_tensor(k, "k"));
     TRY(check_tensor(v, "v"));
   }
-  const size_t need = xattn_workspace(*d, kv4);
-  if (need > 0) {
-    CHECK(work && aligned(work), CS_E_INVAL, "a 16-byte aligned workspace is needed");
-    CHECK(work_bytes >= need, CS_E_INVAL, "the workspace holds %zu bytes, %zu needed", work_bytes, need);
-  }
+  TRY(check_work(work, work_bytes, xattn_workspace(*d, kv4)));
   XAttnArgs a = {q, k, v, o, kv_of, kv_len, false, kv_mask, {}, *d, (float)(1.4426950408889634 * d->scale)};
   if (kv4) a.c = *cache;
   if (d->lk == 1) a.d.k_r = a.d.v_r = d->head_dim;   // never checked
@@ -254,6 +260,203 @@ cs_status cs_kv4_attention(const cs_attn_desc* desc, const void* q, const cs_kv4
               desc->head_dim == cache->head_dim,
           CS_E_INVAL, "n_kv, lk, heads_kv and head_dim must be the cache's");
     return attn_call(desc, q, nullptr, nullptr, cache, kv_of, kv_len, kv_mask, o, work, work_bytes, stream);
+  })
+}
+
+// ------------------------------------------------------------- layer norm
+// What the two descriptors have in common.
+static cs_status check_norm_rows(int x_dtype, int groups, int rows, int dim, int unit_offset, long w_group) {
+  CHECK(x_dtype == CS_BF16 || x_dtype == CS_FP32, CS_E_INVAL, "x_dtype must be CS_BF16 or CS_FP32");
+  CHECK(groups >= 0 && rows >= 0, CS_E_INVAL, "groups and rows must not be negative");
+  CHECK((long)groups * rows < (1L << 31), CS_E_UNSUPPORTED, "groups * rows must be below 2^31");
+  CHECK(dim >= 1, CS_E_INVAL, "dim must be positive");
+  CHECK(dim <= LN_MAX_DIM, CS_E_UNSUPPORTED, "dim must be at most %d", LN_MAX_DIM);
+  CHECK(unit_offset == 0 || unit_offset == 1, CS_E_INVAL, "unit_offset must be 0 or 1");
+  return check_stride(w_group, groups, 4, "w_group");
+}
+
+cs_status cs_layer_norm(const cs_layer_norm_desc* d, const void* x, const float* weight, const float* bias, void* y,
+                        float* y_scale, float* mean, float* rstd, void* stream) {
+  GUARD({
+    CHECK(d, CS_E_INVAL, "desc is NULL");
+    TRY(check_norm_rows(d->x_dtype, d->groups, d->rows, d->dim, d->unit_offset, d->w_group));
+    CHECK(d->y_dtype == CS_BF16 || d->y_dtype == CS_FP32 || d->y_dtype == CS_I8, CS_E_INVAL,
+          "y_dtype must be CS_BF16, CS_FP32 or CS_I8");
+    CHECK(d->eps >= 0.0f && isfinite(d->eps), CS_E_INVAL, "eps must be finite and not negative");
+    const long total = (long)d->groups * d->rows;
+    TRY(check_stride(d->b_group, d->groups, 4, "b_group"));
+    TRY(check_stride(d->x_row, total, elem(d->x_dtype), "x_row"));
+    TRY(check_out_stride(d->y_row, total, elem(d->y_dtype), "y_row"));
+    if (total == 0) return CS_OK;
+    TRY(check_tensor(x, "x"));
+    TRY(check_tensor(y, "y"));
+    TRY(check_optional(weight, "weight"));
+    TRY(check_optional(bias, "bias"));
+    if (d->y_dtype == CS_I8) TRY(check_tensor(y_scale, "y_scale"));
+    TRY(check_optional(mean, "mean"));
+    TRY(check_optional(rstd, "rstd"));
+    HIPC(layer_norm({x, weight, bias, y, y_scale, mean, rstd, *d}, (hipStream_t)stream));
+    return CS_OK;
+  })
+}
+
+static cs_status check_norm_grad(const cs_layer_norm_grad_desc* d) {
+  CHECK(d, CS_E_INVAL, "desc is NULL");
+  TRY(check_norm_rows(d->x_dtype, d->groups, d->rows, d->dim, d->unit_offset, d->w_group));
+  CHECK(d->y_dtype == CS_BF16 || d->y_dtype == CS_FP32, CS_E_INVAL, "y_dtype must be CS_BF16 or CS_FP32");
+  // grids: parts of 16 rows at least, and 64 channels of a group
+  CHECK((long)d->groups * (cdiv(d->dim, 64) + 1) < (1L << 31), CS_E_UNSUPPORTED, "too many groups for one call");
+  const long total = (long)d->groups * d->rows;
+  TRY(check_stride(d->x_row, total, elem(d->x_dtype), "x_row"));
+  TRY(check_stride(d->dy_row, total, elem(d->y_dtype), "dy_row"));
+  return CS_OK;
+}
+
+cs_status cs_layer_norm_backward_workspace(const cs_layer_norm_grad_desc* desc, size_t* bytes) {
+  GUARD({
+    TRY(check_norm_grad(desc));
+    CHECK(bytes, CS_E_INVAL, "bytes is NULL");
+    *bytes = layer_norm_backward_workspace(*desc);
+    return CS_OK;
+  })
+}
+
+cs_status cs_layer_norm_backward(const cs_layer_norm_grad_desc* d, const void* x, const void* dy, const float* weight,
+                                 const float* mean, const float* rstd, void* dx, float* dweight, float* dbias,
+                                 void* work, size_t work_bytes, void* stream) {
+  GUARD({
+    TRY(check_norm_grad(d));
+    const long total = (long)d->groups * d->rows;
+    if (dx) TRY(check_out_stride(d->dx_row, total, elem(d->x_dtype), "dx_row"));
+    if (dweight) TRY(check_out_stride(d->dw_group, d->groups, 4, "dw_group"));
+    if (dbias) TRY(check_out_stride(d->db_group, d->groups, 4, "db_group"));
+    if (d->groups == 0 || (!dx && !dweight && !dbias)) return CS_OK;
+    if (total > 0) {
+      TRY(check_tensor(x, "x"));
+      TRY(check_tensor(dy, "dy"));
+      TRY(check_tensor(mean, "mean"));
+      TRY(check_tensor(rstd, "rstd"));
+    }
+    TRY(check_optional(weight, "weight"));
+    TRY(check_optional(dx, "dx"));
+    TRY(check_optional(dweight, "dweight"));
+    TRY(check_optional(dbias, "dbias"));
+    float* part = nullptr;
+    if (dweight || dbias) {
+      TRY(check_work(work, work_bytes, layer_norm_backward_workspace(*d)));
+      part = (float*)work;
+    }
+    HIPC(layer_norm_backward({x, dy, weight, mean, rstd, dx, dweight, dbias, part, *d}, (hipStream_t)stream));
+    return CS_OK;
+  })
+}
+
+// ------------------------------------------------------------------ 8 bits
+static cs_status i8_rows_call(const cs_i8_rows* r, const void* x, void* x_out, const int8_t* codes, const float* scales,
+                              bool store, void* stream) {
+  CHECK(r, CS_E_INVAL, "rows is NULL");
+  TRY(check_dtype(r->dtype));
+  CHECK(r->rows >= 0, CS_E_INVAL, "rows must not be negative");
+  CHECK(r->dim >= 1, CS_E_INVAL, "dim must be positive");
+  CHECK(r->dim <= I8_MAX_DIM, CS_E_UNSUPPORTED, "dim must be at most %d", I8_MAX_DIM);
+  TRY((store ? check_stride : check_out_stride)(r->x_row, r->rows, elem(r->dtype), "x_row"));
+  TRY((store ? check_out_stride : check_stride)(r->q_row, r->rows, 1, "q_row"));
+  if (r->rows == 0) return CS_OK;
+  TRY(check_tensor(store ? x : x_out, "x"));
+  TRY(check_tensor(codes, "codes"));
+  TRY(check_tensor(scales, "scales"));
+  const I8RowsArgs a = {x, x_out, (int8_t*)codes, (float*)scales, *r};
+  HIPC(store ? i8_quantise(a, (hipStream_t)stream) : i8_dequantise(a, (hipStream_t)stream));
+  return CS_OK;
+}
+
+cs_status cs_i8_quantise(const cs_i8_rows* rows, const void* x, int8_t* codes, float* scales, void* stream) {
+  GUARD({ return i8_rows_call(rows, x, nullptr, codes, scales, true, stream); })
+}
+
+cs_status cs_i8_dequantise(const cs_i8_rows* rows, const int8_t* codes, const float* scales, void* x, void* stream) {
+  GUARD({ return i8_rows_call(rows, nullptr, x, codes, scales, false, stream); })
+}
+
+static cs_status check_weight_size(int n, int k) {
+  CHECK(n >= 1 && k >= 1, CS_E_INVAL, "n and k must be positive");
+  CHECK(n <= (1 << 24), CS_E_UNSUPPORTED, "n must be at most 2^24");
+  CHECK(k <= I8_MAX_DIM, CS_E_UNSUPPORTED, "k must be at most %d", I8_MAX_DIM);
+  return CS_OK;
+}
+
+static cs_status check_weight(const cs_i8_weight* w) {
+  CHECK(w, CS_E_INVAL, "weight is NULL");
+  TRY(check_weight_size(w->n, w->k));
+  TRY(check_tensor(w->codes, "weight codes"));
+  TRY(check_tensor(w->scales, "weight scales"));
+  return CS_OK;
+}
+
+cs_status cs_i8_weight_bytes(int32_t n, int32_t k, size_t* bytes) {
+  GUARD({
+    TRY(check_weight_size(n, k));
+    CHECK(bytes, CS_E_INVAL, "bytes is NULL");
+    *bytes = (size_t)i8_weight_bytes(n, k);
+    return CS_OK;
+  })
+}
+
+cs_status cs_i8_weight_pack(const cs_i8_weight* weight, int32_t dtype, const void* w, int64_t w_row,
+                            const float* w_scales, void* stream) {
+  GUARD({
+    TRY(check_weight(weight));
+    CHECK(dtype == CS_BF16 || dtype == CS_FP32 || dtype == CS_I8, CS_E_INVAL,
+          "dtype must be CS_BF16, CS_FP32 or CS_I8");
+    TRY(check_stride(w_row, weight->n, elem(dtype), "w_row"));
+    TRY(check_tensor(w, "w"));
+    CHECK(dtype == CS_I8 || !w_scales, CS_E_INVAL, "w_scales belong to CS_I8 codes only");
+    if (dtype == CS_I8) TRY(check_tensor(w_scales, "w_scales"));
+    HIPC(i8_weight_pack(*weight, dtype, w, w_row, w_scales, (hipStream_t)stream));
+    return CS_OK;
+  })
+}
+
+static cs_status check_matmul(const cs_matmul_i8_desc* d) {
+  CHECK(d, CS_E_INVAL, "desc is NULL");
+  CHECK(d->out_dtype == CS_BF16 || d->out_dtype == CS_FP32, CS_E_INVAL, "out_dtype must be CS_BF16 or CS_FP32");
+  CHECK(d->rows >= 0, CS_E_INVAL, "rows must not be negative");
+  CHECK(d->rows <= (1 << 30), CS_E_UNSUPPORTED, "rows must be at most 2^30");
+  TRY(check_weight_size(d->n, d->k));
+  CHECK(d->act == CS_ACT_NONE || d->act == CS_ACT_GELU, CS_E_INVAL, "unknown act %d", d->act);
+  // tiles of 32 x 32 at least
+  CHECK((long)cdiv(d->rows, 32) * cdiv(d->n, 32) < (1L << 31), CS_E_UNSUPPORTED, "too many rows and outputs for one call");
+  TRY(check_stride(d->a_row, d->rows, 1, "a_row"));
+  // offsets inside a tile of rows are 32-bit byte counts
+  CHECK(d->rows <= 1 || d->a_row <= (1 << 22), CS_E_UNSUPPORTED, "stride a_row must be at most 2^22");
+  return check_out_stride(d->o_row, d->rows, elem(d->out_dtype), "o_row");
+}
+
+cs_status cs_matmul_i8_workspace(const cs_matmul_i8_desc* desc, size_t* bytes) {
+  GUARD({
+    TRY(check_matmul(desc));
+    CHECK(bytes, CS_E_INVAL, "bytes is NULL");
+    *bytes = matmul_i8_workspace(*desc);
+    return CS_OK;
+  })
+}
+
+cs_status cs_matmul_i8(const cs_matmul_i8_desc* d, const int8_t* a, const float* a_scales, const cs_i8_weight* weight,
+                       const float* bias, void* out, void* work, size_t work_bytes, void* stream) {
+  GUARD({
+    TRY(check_matmul(d));
+    TRY(check_weight(weight));
+    CHECK(weight->n == d->n && weight->k == d->k, CS_E_INVAL, "n and k must be the weight's");
+    if (d->rows == 0) return CS_OK;
+    TRY(check_tensor(a, "a"));
+    TRY(check_tensor(a_scales, "a_scales"));
+    TRY(check_optional(bias, "bias"));
+    TRY(check_tensor(out, "out"));
+    TRY(check_work(work, work_bytes, matmul_i8_workspace(*d)));
+    MatmulI8Args m = {a, a_scales, bias, *weight, out, *d};
+    if (d->rows == 1) m.d.a_row = round_up(d->k, 16), m.d.o_row = round_up(d->n, 8);   // never checked
+    HIPC(matmul_i8(m, work, (hipStream_t)stream));
+    return CS_OK;
   })
 }
 

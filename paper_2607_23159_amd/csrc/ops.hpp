@@ -28,6 +28,55 @@ struct QkNormArgs {
 };
 template <typename T> hipError_t qk_norm_rope(const QkNormArgs& a, hipStream_t st);
 
+// ---- layer norm (k_layer_norm.hip)
+constexpr int LN_MAX_DIM = 16384;
+struct LayerNormArgs {
+  const void* x;
+  const float *weight, *bias;    // NULL: 1 and 0
+  void* y;
+  float *y_scale, *mean, *rstd;  // y_scale: CS_I8 only; mean, rstd may be NULL
+  cs_layer_norm_desc d;
+};
+hipError_t layer_norm(const LayerNormArgs& a, hipStream_t st);
+
+struct LayerNormGradArgs {
+  const void *x, *dy;
+  const float *weight, *mean, *rstd;
+  void* dx;                      // may be NULL
+  float *dweight, *dbias;        // may be NULL
+  float* part;                   // layer_norm_backward_workspace bytes, or NULL without dweight and dbias
+  cs_layer_norm_grad_desc d;
+};
+size_t layer_norm_backward_workspace(const cs_layer_norm_grad_desc& d);
+hipError_t layer_norm_backward(const LayerNormGradArgs& a, hipStream_t st);
+
+// ---- 8-bit rows and weights (k_i8_rows.hip)
+constexpr int I8_MAX_DIM = 65536;
+struct I8RowsArgs {
+  const void* x;                 // quantised rows
+  void* x_out;                   // read-back rows
+  int8_t* codes;
+  float* scales;
+  cs_i8_rows d;
+};
+hipError_t i8_quantise(const I8RowsArgs& a, hipStream_t st);
+hipError_t i8_dequantise(const I8RowsArgs& a, hipStream_t st);
+long i8_weight_bytes(int n, int k);
+// dtype of w: bf16, fp32, or CS_I8 with its scales given.
+hipError_t i8_weight_pack(const cs_i8_weight& o, int dtype, const void* w, long w_row, const float* given,
+                          hipStream_t st);
+
+// ---- product of 8-bit rows and weights (k_matmul_i8.hip)
+struct MatmulI8Args {
+  const int8_t* a;
+  const float *a_scale, *bias;   // bias may be NULL
+  cs_i8_weight w;
+  void* out;
+  cs_matmul_i8_desc d;
+};
+size_t matmul_i8_workspace(const cs_matmul_i8_desc& d);
+hipError_t matmul_i8(const MatmulI8Args& a, void* work, hipStream_t st);
+
 // ---- rows of the 4-bit cache (k_kv4.hip)
 struct Kv4RowsArgs {
   cs_kv4_cache c;
@@ -105,7 +154,6 @@ typedef __attribute__((address_space(3))) char lds_char;
 // has to be there.  (No register is written, and the operands are read at issue.)
 // base and bytes are wave-uniform.
 CS_DEV void load_lds16(const void* base, int bytes, lds_char* lds, int voff) {
-  typedef int i32x4 __attribute__((ext_vector_type(4)));
   const uint64_t b = (uint64_t)base;
   const i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32)) & 0xFFFF,
                       __builtin_amdgcn_readfirstlane(bytes), 0x00020000};
