@@ -2,11 +2,84 @@
 // (cs_matmul_i8).  Sums are 32-bit integers and exact, so every kernel and tile shape gives
 // bitwise the same results.
 #include "gemm_kernel.hpp"
+#include "gemm_tile.hpp"
 #include "ops.hpp"
 
 namespace cs {
 
 constexpr int GROUP_M = 4;
+
+// Up to 16 rows of up to FEW_COLS outputs are k_matmul_few's.  1 x 1536 x 8960: 6.0 us against
+// 11.0 with the best tile, 16 rows 8.3 against 11.2; 16 x 1536 x 1536 4.0 against 4.3.  Past them one
+// row is as fast either way (1 x 13,824 x 5120: 16.1 us both, weights from HBM), and for more the
+// rows, which every workgroup reads past LDS, cost more than the tiles' latency (16 x 13,824 x 5120
+// 21.3 against 16.5).
+constexpr int FEW_ROWS = 16, FEW_COLS = 4096;
+
+// Few rows: the weights are all there is to read, once, so they go straight from memory to the
+// operand registers.  A workgroup has 16 columns; its 8 waves take the K slices in turn, 4 each in
+// flight, and add their sums up in LDS.  Rows past M repeat the last one, and bytes past the end of a
+// row its last ones, which meet zeros of W.  Bound by latency: 1 x 1536 x 8960, 13.8 MB of weights from
+// HBM, takes 6.0 us, of which 2.5 are those of an empty launch.  4 or 16 waves are within 10% of it, 32 columns a
+// workgroup 40% slower.
+template <class To>
+__global__ __launch_bounds__(512) void k_matmul_few(const int8_t* __restrict__ a, long a_row,
+                                                    const int8_t* __restrict__ w, int M, int N, int nk,
+                                                    EpiI8<To> epi) {
+  constexpr int U = 4, NW = 8, SLICE = W_BLOCK_ROWS * 128;   // SLICE: bytes from one slice to the next
+  __shared__ i32x4 sums[NW][64];
+  const int lane = threadIdx.x & 63, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int8_t* wp = w + ((long)(n0 / W_BLOCK_ROWS) * nk * W_BLOCK_ROWS + n0 % W_BLOCK_ROWS + (lane & 15)) * 128;
+  const int swz = gemm_swz(lane & 15), last = epi.a_row - 16;
+  const int8_t* ap = a + min(lane & 15, M - 1) * a_row;
+  i32x4 acc = {0, 0, 0, 0};
+  for (int k0 = wave; k0 < nk; k0 += U * NW) {
+    i32x4 wv[U][2], av[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kt = k0 + u * NW;
+      if (kt >= nk) break;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        wv[u][s] = *reinterpret_cast<const i32x4*>(wp + (long)kt * SLICE + ((4 * s + quad) ^ swz) * 16);
+        av[u][s] = *reinterpret_cast<const i32x4*>(ap + min(kt * 128 + s * 64 + quad * 16, last));
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * NW >= nk) break;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) acc = Mfma16<int8_t>::mma(wv[u][s], av[u][s], acc);
+    }
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int i = 1; i < NW; ++i) acc += sums[i][lane];
+  const int row = lane & 15, col0 = n0 + 4 * quad;
+  if (row >= M || col0 >= N) return;
+  const float sa = epi.scale_a[row];
+  const f32x4 sw = epi.four(epi.scale_w, col0, N), b = epi.bias ? epi.four(epi.bias, col0, N) : f32x4{0.f, 0.f, 0.f, 0.f};
+  float y[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) y[r] = i8_value(acc[r], sa, sw[r], b[r]);
+  epi.to(row, col0, y, epi.to.pre(row, col0));
+}
+
+template <class To> static void launch_few(const MatmulI8Args& a, int kp, const EpiI8<To>& epi, hipStream_t st) {
+  hipLaunchKernelGGL(k_matmul_few<To>, dim3((unsigned)cdiv(a.d.n, 16)), dim3(512), 0, st, a.a, a.d.a_row, a.w.codes,
+                     a.d.rows, a.d.n, kp / 128, epi);
+}
+
+template <int BM, int BN, int OCC, int PD, class Epi>
+static void launch_w4(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st) {
+  const unsigned tiles = (unsigned)((long)cdiv(a.d.rows, BM) * cdiv(a.d.n, BN));
+  hipLaunchKernelGGL((k_gemm_w4<int8_t, BM, BN, OCC, GROUP_M, PD, Epi>), dim3(tiles), dim3(256), 0, st, a.a, a.d.a_row,
+                     a.w.codes, a.d.rows, a.d.n, kp, 0L, epi);
+}
 
 template <int BM, int BN, int WGM, int WGN, int SL, int STAGES, int OCC, class Epi>
 static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st) {
@@ -18,7 +91,23 @@ static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream
 template <class To> static hipError_t product(const MatmulI8Args& a, const To& to, hipStream_t st) {
   const EpiI8<To> epi = {a.a_scale, a.w.scales, a.bias, (int)round_up(a.d.k, 16), to};
   const int kp = (int)round_up(a.d.k, 128);
-  launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, epi, st);
+  if (a.d.rows <= FEW_ROWS && a.d.n <= FEW_COLS) {
+    launch_few(a, kp, epi, st);
+    return hipGetLastError();
+  }
+  switch (choose_tile_i8(a.d.rows, a.d.n, a.d.k, false)) {
+    case W4_256x256: launch_w4<256, 256, 1, 2>(a, kp, epi, st); break;
+    case W4_224x256: launch_w4<224, 256, 1, 2>(a, kp, epi, st); break;
+    case W4_192x256: launch_w4<192, 256, 1, 2>(a, kp, epi, st); break;
+    case W4_160x256: launch_w4<160, 256, 1, 2>(a, kp, epi, st); break;
+    case W4_128x128: launch_w4<128, 128, 2, 2>(a, kp, epi, st); break;
+    case W4_64x64: launch_w4<64, 64, 3, 2>(a, kp, epi, st); break;
+    case RING_128x128: launch_ring<128, 128, 2, 4, 1, 4, 2>(a, kp, epi, st); break;
+    case RING_64x128: launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, epi, st); break;
+    case RING_64x64: launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, epi, st); break;
+    case RING_32x64: launch_ring<32, 64, 1, 4, 2, 3, 2>(a, kp, epi, st); break;
+    default: launch_ring<32, 32, 2, 2, 2, 4, 2>(a, kp, epi, st);
+  }
   return hipGetLastError();
 }
 
