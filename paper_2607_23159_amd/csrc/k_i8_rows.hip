@@ -6,7 +6,7 @@
 
 namespace cs {
 
-template <typename X, int U, int WPR, int NV>
+template <typename X, int U, int WPR, int NV, bool TAIL>
 __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void k_i8_quantise(I8RowsArgs a) {
   __shared__ uint32_t lds[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -18,63 +18,65 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void k_i8_quantise(I8RowsAr
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = U * (64 * WPR * i + t);
-    raw[i] = load_chunk<X, U>(x + c, dim - c);
+    raw[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
   }
-  uint32_t m = 0;
+  std::conditional_t<sizeof(X) == 2, u16x2, uint32_t> m = {};
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int e = 0; e < U; ++e) m = max(m, abs_bits(to_f(raw[i][e])));
-  const I8Scale s(row_max<WPR>(m, lds, wave));
+  for (int i = 0; i < NV; ++i) max_bits(m, raw[i]);
+  const I8Scale s(row_max<WPR>(fp32_bits(m), lds, wave));
   if (t == 0) a.scales[row] = s.scale;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = U * (64 * WPR * i + t);
-    float y[U];
-#pragma unroll
-    for (int e = 0; e < U; ++e) y[e] = s.code(to_f(raw[i][e]));
-    store_codes<U>(a.codes + row * a.d.q_row + c, dim - c, y);
-  }
+  store_codes<U, NV, WPR, TAIL, sizeof(X) == 2>(s, a.codes + row * a.d.q_row, dim, t,
+                                                [&](int i, int e) { return to_f(raw[i][e]); });
 }
 
-template <typename X, int U>
+// WPR: waves of a row (1 or 4).
+template <typename X, int U, int WPR, bool TAIL>
 __global__ __launch_bounds__(256) void k_i8_dequantise(I8RowsArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const long row = WPR == 1 ? (long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.d.rows) return;
   const float scale = a.scales[row];
   const int8_t* q = a.codes + row * a.d.q_row;
   X* x = (X*)a.x_out + row * a.d.x_row;
-  for (int c = U * lane; c < a.d.dim; c += 64 * U) {
-    const auto v = load_chunk<int8_t, U>(q + c, a.d.dim - c);
+  for (int c = U * t; c < a.d.dim; c += 64 * WPR * U) {
+    const auto v = load_chunk<int8_t, U, TAIL>(q + c, a.d.dim - c);
     float y[U];
 #pragma unroll
     for (int e = 0; e < U; ++e) y[e] = scale * (float)v[e];
-    store_chunk<X, U>(x + c, a.d.dim - c, y);
+    store_chunk<X, U, TAIL>(x + c, a.d.dim - c, y);
   }
 }
 
 template <typename X> static hipError_t quantise(const I8RowsArgs& a, hipStream_t st) {
   constexpr int U = sizeof(X) == 2 ? 8 : 4;
-  const int dim = a.d.dim;
-  const unsigned four = (unsigned)(((long)a.d.rows + 3) / 4), one = (unsigned)a.d.rows;
-  if (dim <= 512) hipLaunchKernelGGL((k_i8_quantise<X, U, 1, 8 / U>), dim3(four), dim3(256), 0, st, a);
-  else if (dim <= 2048) hipLaunchKernelGGL((k_i8_quantise<X, U, 1, 32 / U>), dim3(four), dim3(256), 0, st, a);
-  else if (dim <= 8192) hipLaunchKernelGGL((k_i8_quantise<X, U, 4, 32 / U>), dim3(one), dim3(256), 0, st, a);
-  else if (dim <= 16384) hipLaunchKernelGGL((k_i8_quantise<X, U, 4, 64 / U>), dim3(one), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_i8_quantise<X, U, 16, 64 / U>), dim3(one), dim3(1024), 0, st, a);
-  return hipGetLastError();
+  if (a.d.dim > 16384) {   // a workgroup of 16 waves to a row
+    hipLaunchKernelGGL((k_i8_quantise<X, U, 16, 64 / U, true>), dim3((unsigned)a.d.rows), dim3(1024), 0, st, a);
+    return hipGetLastError();
+  }
+  return with_row_shape<U>(a.d.dim, [&](auto shape) {
+    typedef decltype(shape) S;
+    const unsigned grid = (unsigned)(S::WPR == 1 ? ((long)a.d.rows + 3) / 4 : a.d.rows);
+    hipLaunchKernelGGL((k_i8_quantise<X, U, S::WPR, S::NV, S::TAIL>), dim3(grid), dim3(256), 0, st, a);
+    return hipGetLastError();
+  });
 }
 
 hipError_t i8_quantise(const I8RowsArgs& a, hipStream_t st) {
   return a.d.dtype == CS_BF16 ? quantise<bf16>(a, st) : quantise<float>(a, st);
 }
 
-hipError_t i8_dequantise(const I8RowsArgs& a, hipStream_t st) {
-  const unsigned four = (unsigned)(((long)a.d.rows + 3) / 4);
-  if (a.d.dtype == CS_BF16) hipLaunchKernelGGL((k_i8_dequantise<bf16, 8>), dim3(four), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_i8_dequantise<float, 4>), dim3(four), dim3(256), 0, st, a);
+template <typename X> static hipError_t dequantise(const I8RowsArgs& a, hipStream_t st) {
+  constexpr int U = sizeof(X) == 2 ? 8 : 4;
+  const bool tail = a.d.dim % U != 0, wide = a.d.dim > 2048;
+  const auto kernel = wide ? (tail ? k_i8_dequantise<X, U, 4, true> : k_i8_dequantise<X, U, 4, false>)
+                           : (tail ? k_i8_dequantise<X, U, 1, true> : k_i8_dequantise<X, U, 1, false>);
+  const unsigned grid = (unsigned)(wide ? a.d.rows : ((long)a.d.rows + 3) / 4);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a);
   return hipGetLastError();
+}
+
+hipError_t i8_dequantise(const I8RowsArgs& a, hipStream_t st) {
+  return a.d.dtype == CS_BF16 ? dequantise<bf16>(a, st) : dequantise<float>(a, st);
 }
 
 // -------------------------------------------------------------- 8-bit weights

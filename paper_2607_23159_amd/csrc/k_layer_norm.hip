@@ -8,48 +8,40 @@
 
 namespace cs {
 
-// Chunks of a lane and waves of a row, by the row's length; LN_MAX_DIM is the last one's.
-template <int WPR, int VPL> struct RowShape { static constexpr int wpr = WPR, vpl = VPL; };
-template <class F> static hipError_t with_shape(int dim, F f) {
-  if (dim <= 512) return f(RowShape<1, 8>{});
-  if (dim <= 2048) return f(RowShape<1, 32>{});
-  if (dim <= 8192) return f(RowShape<4, 32>{});
-  return f(RowShape<4, 64>{});
-}
-
 // ------------------------------------------------------------------ forward
 //   y = (x - mean) rstd gain + bias,  gain = weight or 1 + weight,
 //   mean and variance from the row in registers, the variance of the centred values.
 // Y int8_t: the result, in fp32, goes on to codes and the row's scale.
-template <typename X, typename Y, int U, int WPR, int NV>
+// One row to a wave or workgroup: a loop over rows with the gains in registers and the next row on
+// its way keeps fewer rows in flight (65,520 x 1536, fp32 to bf16: 120 us against 110, 5.5 TB/s).
+template <typename X, typename Y, int U, int WPR, int NV, bool TAIL>
 __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
-  __shared__ float lds[3][4];
+  __shared__ float lds[2][4];
+  __shared__ uint32_t lds_max[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const long row = WPR == 1 ? (long)blockIdx.x * 4 + wave : blockIdx.x;
-  const long total = (long)a.d.groups * a.d.rows;
-  if (row >= total) return;   // whole waves, and whole workgroups at WPR 4
+  if (row >= (long)a.d.groups * a.d.rows) return;   // whole waves, and whole workgroups at WPR 4
   const int dim = a.d.dim, t = WPR == 1 ? lane : (int)threadIdx.x;
   const X* x = (const X*)a.x + row * a.d.x_row;
   typename Chunk<X, U>::vec raw[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = U * (64 * WPR * i + t);
-    raw[i] = load_chunk<X, U>(x + c, dim - c);
+    raw[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
   }
-  float s = 0.0f;
+  float s = 0.0f, q = 0.0f;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < U; ++e) s += to_f(raw[i][e]);
   const float mean = row_sum<WPR>(s, lds[0], wave) / (float)dim;
-  float q = 0.0f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int left = dim - U * (64 * WPR * i + t);
 #pragma unroll
     for (int e = 0; e < U; ++e) {
       const float z = to_f(raw[i][e]) - mean;
-      q += e < left ? z * z : 0.0f;
+      q += (TAIL ? e < left : left > 0) ? z * z : 0.0f;
     }
   }
   const float rstd = 1.0f / sqrtf(row_sum<WPR>(q, lds[1], wave) / (float)dim + a.d.eps);
@@ -68,8 +60,8 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
 #pragma unroll
     for (int h = 0; h < U / 4; ++h) {
       wv[h] = bv[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (w) wv[h] = load_chunk<float, 4>(w + c + 4 * h, dim - c - 4 * h);
-      if (b) bv[h] = load_chunk<float, 4>(b + c + 4 * h, dim - c - 4 * h);
+      if (w) wv[h] = load_chunk<float, 4, TAIL>(w + c + 4 * h, dim - c - 4 * h);
+      if (b) bv[h] = load_chunk<float, 4, TAIL>(b + c + 4 * h, dim - c - 4 * h);
     }
 #pragma unroll
     for (int e = 0; e < U; ++e) {
@@ -85,24 +77,19 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
       const int left = dim - U * (64 * WPR * i + t);
       result(i, y[i]);
 #pragma unroll
-      for (int e = 0; e < U; ++e) m = max(m, e < left ? abs_bits(y[i][e]) : 0u);
+      for (int e = 0; e < U; ++e) m = max(m, (TAIL ? e < left : left > 0) ? abs_bits(y[i][e]) : 0u);
     }
-    const I8Scale s8(row_max<WPR>(m, (uint32_t*)lds[2], wave));
+    const I8Scale s8(row_max<WPR>(m, lds_max, wave));
     if (t == 0) a.y_scale[row] = s8.scale;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = U * (64 * WPR * i + t);
-#pragma unroll
-      for (int e = 0; e < U; ++e) y[i][e] = s8.code(y[i][e]);
-      store_codes<U>((int8_t*)a.y + row * a.d.y_row + c, dim - c, y[i]);
-    }
+    store_codes<U, NV, WPR, TAIL, false>(s8, (int8_t*)a.y + row * a.d.y_row, dim, t,
+                                         [&](int i, int e) { return y[i][e]; });
   } else {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = U * (64 * WPR * i + t);
       float y[U];
       result(i, y);
-      store_chunk<Y, U>((Y*)a.y + row * a.d.y_row + c, dim - c, y);
+      store_chunk<Y, U, TAIL>((Y*)a.y + row * a.d.y_row + c, dim - c, y);
     }
   }
 }
@@ -110,11 +97,11 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
 template <typename X, typename Y>
 static hipError_t forward(const LayerNormArgs& a, hipStream_t st) {
   const long total = (long)a.d.groups * a.d.rows;
-  return with_shape(a.d.dim, [&](auto shape) {
+  constexpr int U = sizeof(X) == 2 ? 8 : 4;   // x alone decides: a row's sums do not depend on y's type
+  return with_row_shape<U>(a.d.dim, [&](auto shape) {
     typedef decltype(shape) S;
-    constexpr int U = sizeof(X) == 2 ? 8 : 4;   // x alone decides: a row's sums do not depend on y's type
-    const unsigned grid = (unsigned)(S::wpr == 1 ? (total + 3) / 4 : total);
-    hipLaunchKernelGGL((k_layer_norm_op<X, Y, U, S::wpr, S::vpl / U>), dim3(grid), dim3(256), 0, st, a);
+    const unsigned grid = (unsigned)(S::WPR == 1 ? (total + 3) / 4 : total);
+    hipLaunchKernelGGL((k_layer_norm_op<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3(grid), dim3(256), 0, st, a);
     return hipGetLastError();
   });
 }
@@ -146,136 +133,157 @@ size_t layer_norm_backward_workspace(const cs_layer_norm_grad_desc& d) {
   return (size_t)d.groups * ln_parts(d.rows) * 2 * round_up(d.dim, 4) * sizeof(float);
 }
 
-template <typename X, typename Y, int U, int WPR, int NV>
+template <typename X, typename Y, int U, int WPR, int NV, bool TAIL>
 __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, int parts, int part_rows) {
-  __shared__ float lds[2][2][4];
-  __shared__ float sums[WPR == 1 ? 4 * 64 * U : 1];
+  constexpr int STEP = WPR == 1 ? 4 : 1;               // rows of the workgroup's waves
+  __shared__ float2 lds[2][4];
+  __shared__ float sums[WPR == 1 ? 4 : 1][WPR == 1 ? 64 * NV * U : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int group = blockIdx.x / parts, part = blockIdx.x - group * parts;
   const int dim = a.d.dim, t = WPR == 1 ? lane : (int)threadIdx.x;
-  const int first = part * part_rows, last = min(first + part_rows, a.d.rows);
-  const float one = a.d.unit_offset ? 1.0f : 0.0f;
-  const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
-  float dw[NV][U] = {}, db[NV][U] = {};
-  int odd = 0;
-  for (int r = first + (WPR == 1 ? wave : 0); r < last; r += WPR == 1 ? 4 : 1, odd ^= 1) {
+  const int first = part * part_rows + (WPR == 1 ? wave : 0), last = min((part + 1) * part_rows, a.d.rows);
+  const float inv = 1.0f / (float)dim;
+  // gains: past the row's end anything, since dy is zero there
+  float gain[NV][U];
+  {
+    const float one = a.d.unit_offset ? 1.0f : 0.0f;
+    const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int h = 0; h < U / 4; ++h) {
+        const int c = U * (64 * WPR * i + t) + 4 * h;
+        const f32x4 v = w ? load_chunk<float, 4, TAIL>(w + c, dim - c) : f32x4{};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) gain[i][4 * h + e] = w ? one + v[e] : 1.0f;
+      }
+  }
+  struct Row {
+    typename Chunk<X, U>::vec x[NV];
+    typename Chunk<Y, U>::vec dy[NV];
+    float mean, rstd;
+  };
+  auto load = [&](int r, Row& o) {
     const long row = (long)group * a.d.rows + r;
     const X* x = (const X*)a.x + row * a.d.x_row;
     const Y* dy = (const Y*)a.dy + row * a.d.dy_row;
-    typename Chunk<X, U>::vec xv[NV];
-    typename Chunk<Y, U>::vec dv[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = U * (64 * WPR * i + t);
-      xv[i] = load_chunk<X, U>(x + c, dim - c);
-      dv[i] = load_chunk<Y, U>(dy + c, dim - c);
+      o.x[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
+      o.dy[i] = load_chunk<Y, U, TAIL>(dy + c, dim - c);
     }
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    o.mean = a.mean[row];
+    o.rstd = a.rstd[row];
+  };
+  float dw[NV][U] = {}, db[NV][U] = {};
+  Row next;
+  if (first < last) load(first, next);
+  int odd = 0;
+  for (int r = first; r < last; r += STEP, odd ^= 1) {
+    const Row cur = next;
+    if (r + STEP < last) load(r + STEP, next);   // on its way while this row is reduced
     float s1 = 0.0f, s2 = 0.0f;
-    auto gain = [&](int i, float* o) {
-      const int c = U * (64 * WPR * i + t);
 #pragma unroll
-      for (int h = 0; h < U / 4; ++h) {
-        const f32x4 v = w ? load_chunk<float, 4>(w + c + 4 * h, dim - c - 4 * h) : f32x4{};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[4 * h + e] = w ? one + v[e] : 1.0f;
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float gw[U];
-      gain(i, gw);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < U; ++e) {
-        const float d = to_f(dv[i][e]), n = (to_f(xv[i][e]) - mean) * rstd, g = d * gw[e];
+        const float d = to_f(cur.dy[i][e]), n = (to_f(cur.x[i][e]) - cur.mean) * cur.rstd, g = d * gain[i][e];
         dw[i][e] = fmaf(d, n, dw[i][e]);
         db[i][e] += d;
-        s1 += g;             // channels past the end have dy 0
+        s1 += g;
         s2 = fmaf(g, n, s2);
       }
-    }
-    const float m1 = row_sum<WPR>(s1, lds[odd][0], wave) / (float)dim;
-    const float m2 = row_sum<WPR>(s2, lds[odd][1], wave) / (float)dim;
-    if (a.dx) {
-      X* dx = (X*)a.dx + row * a.d.dx_row;
+    const float2 m = row_sums<WPR>(s1, s2, lds[odd], wave);
+    if (!a.dx) continue;
+    const float m1 = m.x * inv, m2 = m.y * inv;
+    X* dx = (X*)a.dx + ((long)group * a.d.rows + r) * a.d.dx_row;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = U * (64 * WPR * i + t);
-        float gw[U], o[U];
-        gain(i, gw);
+    for (int i = 0; i < NV; ++i) {
+      const int c = U * (64 * WPR * i + t);
+      float o[U];
 #pragma unroll
-        for (int e = 0; e < U; ++e) {
-          const float n = (to_f(xv[i][e]) - mean) * rstd;
-          o[e] = rstd * (fmaf(to_f(dv[i][e]), gw[e], -m1) - n * m2);
-        }
-        store_chunk<X, U>(dx + c, dim - c, o);
+      for (int e = 0; e < U; ++e) {
+        const float n = (to_f(cur.x[i][e]) - cur.mean) * cur.rstd;
+        o[e] = cur.rstd * (fmaf(to_f(cur.dy[i][e]), gain[i][e], -m1) - n * m2);
       }
+      store_chunk<X, U, TAIL>(dx + c, dim - c, o);
     }
   }
   if (!a.part) return;
   const long ld = (dim + 3) & ~3;
   float* out = a.part + ((long)group * parts + part) * 2 * ld;
+  auto store = [&](float* p, int c, const float* v) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+    for (int h = 0; h < U / 4; ++h)
+      if (c + 4 * h < dim)   // whole chunks: the workspace's rows are padded to 4
+        *reinterpret_cast<f32x4*>(p + c + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+  };
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = U * (64 * WPR * i + t);
-      float v[U];
+  for (int k = 0; k < 2; ++k) {
+    if constexpr (WPR == 1) {
+      // the four waves' rows, added in order; element e of chunk i of a lane lies at 64 (U i + e) + lane
+      __syncthreads();
 #pragma unroll
-      for (int e = 0; e < U; ++e) v[e] = k ? db[i][e] : dw[i][e];
-      if constexpr (WPR == 1) {
-        // the four waves' rows, added in order by the first
-        __syncthreads();
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < U; ++e) sums[(wave * U + e) * 64 + lane] = v[e];
-        __syncthreads();
-        if (wave != 0) continue;
+        for (int e = 0; e < U; ++e) sums[wave][64 * (U * i + e) + lane] = k ? db[i][e] : dw[i][e];
+      __syncthreads();
+      for (int i = wave; i < NV; i += 4) {
+        float v[U];
 #pragma unroll
-        for (int e = 0; e < U; ++e)
-          v[e] = ((sums[e * 64 + lane] + sums[(U + e) * 64 + lane]) + sums[(2 * U + e) * 64 + lane]) +
-                 sums[(3 * U + e) * 64 + lane];
+        for (int e = 0; e < U; ++e) {
+          const int q = 64 * (U * i + e) + lane;
+          v[e] = ((sums[0][q] + sums[1][q]) + sums[2][q]) + sums[3][q];
+        }
+        store(out + k * ld, U * (64 * i + lane), v);
       }
+    } else {
 #pragma unroll
-      for (int h = 0; h < U / 4; ++h)
-        if (c + 4 * h < dim)   // whole chunks: the workspace's rows are padded to 4
-          *reinterpret_cast<f32x4*>(out + k * ld + c + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      for (int i = 0; i < NV; ++i) store(out + k * ld, U * (64 * WPR * i + t), k ? db[i] : dw[i]);
     }
+  }
 }
 
-// The parts' sums, a channel a lane and a quarter of the parts a wave.
-__global__ __launch_bounds__(256) void k_layer_norm_grad_sum(LayerNormGradArgs a, int parts) {
-  __shared__ float sums[4][64];
+// The parts' sums, a channel a lane and a sixteenth of the parts a wave.  With four waves, a load
+// behind the other, 512 parts of 5120 channels took 33 us.
+__global__ __launch_bounds__(1024) void k_layer_norm_grad_sum(LayerNormGradArgs a, int parts) {
+  __shared__ float sums[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int cols = (a.d.dim + 63) / 64, group = blockIdx.x / cols, k = blockIdx.y;
   const int c = (blockIdx.x - group * cols) * 64 + lane;
   const long ld = (a.d.dim + 3) & ~3;
   const float* p = a.part + ((long)group * parts * 2 + k) * ld + c;
-  const int per = (parts + 3) / 4, first = wave * per, last = min(first + per, parts);
+  const int per = (parts + 15) / 16, first = wave * per, last = min(first + per, parts);
   float s = 0.0f;
-  if (c < a.d.dim)
+  if (c < a.d.dim) {
+#pragma unroll 8
     for (int i = first; i < last; ++i) s += p[(long)i * 2 * ld];
+  }
   sums[wave][lane] = s;
   __syncthreads();
   float* out = k ? a.dbias : a.dweight;
-  if (wave == 0 && c < a.d.dim && out)
-    out[group * (k ? a.d.db_group : a.d.dw_group) + c] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+  if (wave != 0 || c >= a.d.dim || !out) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += sums[i][lane];
+  out[group * (k ? a.d.db_group : a.d.dw_group) + c] = s;
 }
 
 template <typename X, typename Y>
 static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
   const int parts = ln_parts(a.d.rows), part_rows = ln_part_rows(a.d.rows);
   if (a.d.rows > 0) {
-    const hipError_t s = with_shape(a.d.dim, [&](auto shape) {
+    constexpr int U = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
+    const hipError_t s = with_row_shape<U>(a.d.dim, [&](auto shape) {
       typedef decltype(shape) S;
-      constexpr int U = std::is_same<X, bf16>::value && std::is_same<Y, bf16>::value ? 8 : 4;
-      hipLaunchKernelGGL((k_layer_norm_grad<X, Y, U, S::wpr, S::vpl / U>), dim3((unsigned)a.d.groups * parts), dim3(256),
+      hipLaunchKernelGGL((k_layer_norm_grad<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)a.d.groups * parts), dim3(256),
                          0, st, a, parts, part_rows);
       return hipGetLastError();
     });
     if (s != hipSuccess) return s;
   }
   if (!a.dweight && !a.dbias) return hipSuccess;
-  hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)((long)cdiv(a.d.dim, 64) * a.d.groups), 2), dim3(256), 0, st, a,
+  hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)((long)cdiv(a.d.dim, 64) * a.d.groups), 2), dim3(1024), 0, st, a,
                      parts);
   return hipGetLastError();
 }
