@@ -156,6 +156,18 @@ typedef enum { CS_QK_NORM_FULL = 0, CS_QK_NORM_HEAD = 1 } cs_qk_norm;
 cs_status cs_model_init_norm(const cs_model_desc* desc, int32_t qk_norm, const float* weights,
                              size_t n_weights, void* stream, cs_model** out);
 
+/* Projections of the blocks (q, k and v, self-attention output, cross-attention q and output,
+ * feed-forward up and down): in the compute type, or in 8 bits (cs_matmul_i8): weights rounded
+ * to codes with a scale an output channel (cs_i8_weight_pack, from the float32 values), their inputs
+ * to codes with a scale a row (cs_layer_norm, cs_i8_quantise).  Half the weights' memory, and
+ * the roundings of 8 bits.  The rest, text keys and values among it, stays in the compute type. */
+typedef enum { CS_PROJ_NATIVE = 0, CS_PROJ_8BIT = 1 } cs_proj_format;
+/* cs_model_init_norm with the choice of the projections (cs_proj_format).  CS_PROJ_8BIT: dtype
+ * CS_BF16, hidden at most 16384 and ffn at most 65536 (else CS_E_UNSUPPORTED).  Everything else, rollouts
+ * included, is as with cs_model_init. */
+cs_status cs_model_init_proj(const cs_model_desc* desc, int32_t qk_norm, int32_t proj, const float* weights,
+                             size_t n_weights, void* stream, cs_model** out);
+
 /* One transformer evaluation v_theta(x, t, c) (Sec. Preliminaries) for n
  * latents sharing the timestep t and one text context.  x: device
  * [n][D] float32; ctx: device [text_len][text_dim] float32; v: device

@@ -23,6 +23,7 @@ CS_BF16, CS_FP32, CS_I8 = 0, 1, 2
 CS_CACHE_OFF, CS_CACHE_ADAPTIVE, CS_CACHE_STATIC, CS_CACHE_PAB = 0, 1, 2, 3
 CS_QK_NORM_FULL, CS_QK_NORM_HEAD = 0, 1
 CS_KV_NATIVE, CS_KV_4BIT = 0, 1
+CS_PROJ_NATIVE, CS_PROJ_8BIT = 0, 1
 CS_ROPE_PAIRS, CS_ROPE_HALVES = 0, 1
 CS_ACT_NONE, CS_ACT_GELU = 0, 1
 (CS_K_SELF_ATTN, CS_K_CROSS_ATTN, CS_K_GEMM, CS_K_NORM, CS_K_DECIDE, CS_K_UPDATE, CS_K_SCORE,
@@ -118,6 +119,7 @@ def lib() -> C.CDLL:
         "cs_model_weight_count": (i32, [C.POINTER(cs_model_desc), C.POINTER(sz)]),
         "cs_model_init": (i32, [C.POINTER(cs_model_desc), pf, sz, vp, C.POINTER(vp)]),
         "cs_model_init_norm": (i32, [C.POINTER(cs_model_desc), i32, pf, sz, vp, C.POINTER(vp)]),
+        "cs_model_init_proj": (i32, [C.POINTER(cs_model_desc), i32, i32, pf, sz, vp, C.POINTER(vp)]),
         "cs_model_free": (None, [vp]),
         "cs_context_init": (i32, [vp, pf, pi32, i32, i32, C.POINTER(vp)]),
         "cs_context_free": (None, [vp]),
@@ -249,9 +251,13 @@ def cs_model_init(desc: cs_model_desc, weights, n_weights: int, stream=None) -> 
 
 
 def cs_model_init_norm(desc: cs_model_desc, qk_norm: int, weights, n_weights: int, stream=None) -> int:
+    return cs_model_init_proj(desc, qk_norm, CS_PROJ_NATIVE, weights, n_weights, stream)
+
+
+def cs_model_init_proj(desc: cs_model_desc, qk_norm: int, proj: int, weights, n_weights: int, stream=None) -> int:
     out = C.c_void_p()
-    _check(lib().cs_model_init_norm(C.byref(desc), int(qk_norm), _ptr(weights, n_weights, name="weights"), n_weights,
-                                    _stream(stream), C.byref(out)))
+    _check(lib().cs_model_init_proj(C.byref(desc), int(qk_norm), int(proj), _ptr(weights, n_weights, name="weights"),
+                                    n_weights, _stream(stream), C.byref(out)))
     _model_D[out.value] = desc.in_ch * desc.lat_f * desc.lat_h * desc.lat_w
     _model_text[out.value] = (desc.text_len, desc.text_dim)
     return out.value

@@ -821,6 +821,12 @@ template <int GATED, typename T> struct EpiResidualStore {
   }
 };
 
+// Residual updates read and write the fp32 residual stream in their epilogue,
+// which then weighs several times a bf16 store.
+template <class Epi> struct EpiIsResidual : std::false_type {};
+template <int G> struct EpiIsResidual<EpiResidual<G>> : std::true_type {};
+template <int G, typename T> struct EpiIsResidual<EpiResidualStore<G, T>> : std::true_type {};
+
 // Patch embedding: z = acc + bias (fp32 residual stream).
 struct EpiPatch {
   float* z; long ldz; const float* bias;

@@ -48,12 +48,6 @@ hipError_t gemm_tile_weight(const float* src, int N, int K, T* dst, hipStream_t 
   return hipGetLastError();
 }
 
-// Residual updates read and write the fp32 residual stream in their epilogue,
-// which then weighs several times a bf16 store.
-template <class Epi> struct EpiIsResidual : std::false_type {};
-template <int G> struct EpiIsResidual<EpiResidual<G>> : std::true_type {};
-template <int G, typename T> struct EpiIsResidual<EpiResidualStore<G, T>> : std::true_type {};
-
 struct GemmBatch { int n; long w_stride; };
 
 template <int BM, int BN, int OCC, int PD, class Epi>

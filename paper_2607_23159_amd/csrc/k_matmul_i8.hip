@@ -91,16 +91,18 @@ static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream
 template <class To> static hipError_t product(const MatmulI8Args& a, const To& to, hipStream_t st) {
   const EpiI8<To> epi = {a.a_scale, a.w.scales, a.bias, (int)round_up(a.d.k, 16), to};
   const int kp = (int)round_up(a.d.k, 128);
+  constexpr bool RES = EpiIsResidual<To>::value;
+  constexpr int PD = RES ? 8 : 2, PD2 = RES ? 4 : 2;   // as in bf16
   if (a.d.rows <= FEW_ROWS && a.d.n <= FEW_COLS) {
     launch_few(a, kp, epi, st);
     return hipGetLastError();
   }
-  switch (choose_tile_i8(a.d.rows, a.d.n, a.d.k, false)) {
-    case W4_256x256: launch_w4<256, 256, 1, 2>(a, kp, epi, st); break;
-    case W4_224x256: launch_w4<224, 256, 1, 2>(a, kp, epi, st); break;
-    case W4_192x256: launch_w4<192, 256, 1, 2>(a, kp, epi, st); break;
-    case W4_160x256: launch_w4<160, 256, 1, 2>(a, kp, epi, st); break;
-    case W4_128x128: launch_w4<128, 128, 2, 2>(a, kp, epi, st); break;
+  switch (choose_tile_i8(a.d.rows, a.d.n, a.d.k, RES)) {
+    case W4_256x256: launch_w4<256, 256, 1, PD>(a, kp, epi, st); break;
+    case W4_224x256: launch_w4<224, 256, 1, PD>(a, kp, epi, st); break;
+    case W4_192x256: launch_w4<192, 256, 1, PD>(a, kp, epi, st); break;
+    case W4_160x256: launch_w4<160, 256, 1, PD>(a, kp, epi, st); break;
+    case W4_128x128: launch_w4<128, 128, 2, PD2>(a, kp, epi, st); break;
     case W4_64x64: launch_w4<64, 64, 3, 2>(a, kp, epi, st); break;
     case RING_128x128: launch_ring<128, 128, 2, 4, 1, 4, 2>(a, kp, epi, st); break;
     case RING_64x128: launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, epi, st); break;
@@ -119,6 +121,41 @@ hipError_t matmul_i8(const MatmulI8Args& a, void*, hipStream_t st) {
                                   : product(a, EpiMatmul<bf16, 0>{(bf16*)a.out, a.d.o_row, a.d.n}, st);
   return a.d.act == CS_ACT_GELU ? product(a, EpiMatmul<float, 1>{(float*)a.out, a.d.o_row, a.d.n}, st)
                                 : product(a, EpiMatmul<float, 0>{(float*)a.out, a.d.o_row, a.d.n}, st);
+}
+
+// ------------------------------------------------- the transformer's projections
+static MatmulI8Args projection(const I8Rows& a, const I8Weight& w, int M, int N, int K, const float* bias) {
+  MatmulI8Args m = {};
+  m.a = a.codes;
+  m.a_scale = a.scales;
+  m.bias = bias;
+  m.w = {const_cast<int8_t*>(w.codes), const_cast<float*>(w.scales), N, K};
+  m.d.rows = M;
+  m.d.n = N;
+  m.d.k = K;
+  m.d.a_row = K;   // K is a multiple of 64
+  return m;
+}
+
+hipError_t gemm_store_i8(const I8Rows& a, const I8Weight& w, int M, int N, int K, const float* bias, int act,
+                         bf16* out, hipStream_t st) {
+  const MatmulI8Args m = projection(a, w, M, N, K, bias);
+  return act == 1 ? product(m, EpiMatmul<bf16, 1>{out, N, N}, st) : product(m, EpiMatmul<bf16, 0>{out, N, N}, st);
+}
+
+hipError_t gemm_qkv_i8(const I8Rows& a, const I8Weight& w, int M, int d, const float* bias, int L, bf16* qk, bf16* vt,
+                       long vt_ld, hipStream_t st) {
+  return product(projection(a, w, M, 3 * d, d, bias), EpiQKV<bf16>{qk, vt, nullptr, d, L, vt_ld, (long)d * vt_ld}, st);
+}
+
+hipError_t gemm_residual_i8(const I8Rows& a, const I8Weight& w, int M, int N, int K, const float* bias,
+                            const float* gate, float* z, bf16* y, hipStream_t st) {
+  const MatmulI8Args m = projection(a, w, M, N, K, bias);
+  if (y)
+    return gate ? product(m, EpiResidualStore<1, bf16>{z, N, nullptr, gate, y}, st)
+                : product(m, EpiResidualStore<0, bf16>{z, N, nullptr, nullptr, y}, st);
+  return gate ? product(m, EpiResidual<1>{z, N, nullptr, gate}, st)
+              : product(m, EpiResidual<0>{z, N, nullptr, nullptr}, st);
 }
 
 }  // namespace cs

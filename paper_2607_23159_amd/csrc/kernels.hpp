@@ -44,6 +44,17 @@ hipError_t gemm_head(const T* A, const T* W, int M, int d, int P, const float* b
                      const int* slot_id, int L, int gh, int gw, int F, int H, int Wd, long D,
                      hipStream_t st);
 
+// ---- projections in 8 bits (k_matmul_i8.hip): rows of codes with a scale each, and weights as
+// cs_i8_weight_pack lays them out.  Outputs and epilogues as those of the bf16 ones above.
+struct I8Rows { const int8_t* codes; const float* scales; };
+struct I8Weight { const int8_t* codes; const float* scales; };
+hipError_t gemm_store_i8(const I8Rows& a, const I8Weight& w, int M, int N, int K, const float* bias, int act,
+                         bf16* out, hipStream_t st);
+hipError_t gemm_qkv_i8(const I8Rows& a, const I8Weight& w, int M, int d, const float* bias, int L, bf16* qk, bf16* vt,
+                       long vt_ld, hipStream_t st);
+hipError_t gemm_residual_i8(const I8Rows& a, const I8Weight& w, int M, int N, int K, const float* bias,
+                            const float* gate, float* z, bf16* y, hipStream_t st);
+
 // ---- attention (k_attn.hip)
 template <typename T> struct AttnArgs {
   const T* q; long q_ld; long q_ss;     // stream s: rows at q + s*q_ss, row stride q_ld

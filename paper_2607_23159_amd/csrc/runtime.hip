@@ -175,6 +175,7 @@ struct Block {
   const void *qkv_w, *o_w, *caq_w, *cak_w, *cav_w, *cao_w, *ffn1_w, *ffn2_w;
   const float *qkv_b, *q_gain, *k_gain, *o_b, *ca_ln_g, *ca_ln_b, *caq_b, *cak_b, *cav_b,
       *caq_gain, *cak_gain, *cao_b, *ffn1_b, *ffn2_b;
+  I8Weight qkv8, o8, caq8, cao8, ffn1_8, ffn2_8;   // CS_PROJ_8BIT: in the place of qkv_w ... ffn2_w
 };
 
 // Lays arrays out in one allocation, 256-byte aligned: with a null base it
@@ -194,6 +195,8 @@ struct Workspace {
   void *patches = nullptr, *u = nullptr, *qk = nullptr, *vt = nullptr, *o = nullptr,
        *q2 = nullptr, *h = nullptr;
   float* z = nullptr;
+  int8_t* u8 = nullptr;       // CS_PROJ_8BIT: a projection's rows in 8 bits, and their scales
+  float* s8 = nullptr;
   int32_t* ids = nullptr;     // identity slot ids [cap] (velocity calls)
   int32_t* zeros = nullptr;   // branch 0 for every slot [cap] (velocity calls)
   void release() {
@@ -223,6 +226,7 @@ struct cs_model {
   long d = 0, L = 0, P = 0, D = 0, Lp = 0, Ltp = 0;
   int gf = 0, gh = 0, gw = 0;
   int qk_norm = CS_QK_NORM_FULL;
+  bool proj8 = false;        // CS_PROJ_8BIT
   void* arena = nullptr;
   const void *patch_w, *text1_w, *text2_w, *time1_w, *time2_w, *mod_w, *head_w;
   const float *patch_b, *text1_b, *text2_b, *time1_b, *time2_b, *mod_b, *head_mod, *head_b;
@@ -329,6 +333,10 @@ static void ws_layout(const cs_model* m, Workspace& w, int cap, Layout& l) {
   l.take(w.o, rows * m->d * e);
   l.take(w.q2, rows * m->d * e);
   l.take(w.h, rows * (long)m->desc.ffn * e);
+  if (m->proj8) {
+    l.take(w.u8, rows * std::max<long>(m->d, m->desc.ffn));
+    l.take(w.s8, rows * sizeof(float));
+  }
   l.take(w.ids, cap * sizeof(int32_t));
   l.take(w.zeros, cap * sizeof(int32_t));
   w.cap = cap;
@@ -544,6 +552,24 @@ struct PabIO {
   int self_mode, cross_mode;
 };
 
+// The inputs of a block's projections in 8 bits, into the workspace: a norm of the residual
+// stream (gain weight, or 1 + weight), or rows of the compute type.
+static hipError_t norm_rows_8bit(const cs_model* m, const Workspace& w, long rows, const float* weight,
+                                 const float* bias, bool unit_offset) {
+  LayerNormArgs a = {};
+  a.x = w.z;
+  a.weight = weight;
+  a.bias = bias;
+  a.y = w.u8;
+  a.y_scale = w.s8;
+  a.d = {CS_FP32, CS_I8, 1, (int32_t)rows, (int32_t)m->d, unit_offset, 1e-6f, m->d, m->d, 0, 0};
+  return layer_norm(a, m->stream);
+}
+
+static hipError_t rows_8bit(const cs_model* m, const Workspace& w, const void* x, long rows, int dim) {
+  return i8_quantise({x, nullptr, w.u8, w.s8, {CS_BF16, (int32_t)rows, dim, dim, dim}}, m->stream);
+}
+
 // One transformer evaluation for n_slots streams.  Stream s reads latent
 // x + (slot_id[s] / cand_div) * D, attends to text branch kv_branch[s] of c, or to its
 // prompt of cx where that is given, and writes its velocity to vout + slot_id[s] * D.
@@ -564,6 +590,36 @@ static cs_status dit_forward(cs_model* m, Workspace& w, const CtxKV* c, const cs
   T* Q2 = (T*)w.q2;
   T* Hh = (T*)w.h;
   float* Z = w.z;
+  // The block's steps around a projection, in the model's format: a norm to its input; rows
+  // to its input; u W^T to out; z += gate (u W^T).  `u` is the input in the compute type.
+  constexpr bool CAN8 = sizeof(T) == 2;
+  const bool p8 = CAN8 && m->proj8;
+  const I8Rows in8 = {w.u8, w.s8};
+  auto norm = [&](const float* shift_or_gain, const float* scale_or_bias, int mode) {
+    if (p8)
+      return mode == 0 ? norm_rows_8bit(m, w, rows, scale_or_bias, shift_or_gain, true)
+                       : norm_rows_8bit(m, w, rows, shift_or_gain, scale_or_bias, false);
+    return layer_norm_mod<T>(Z, rows, (int)d, shift_or_gain, scale_or_bias, mode, U, st);
+  };
+  auto store = [&](const void* wt, const I8Weight& w8, int n, const float* bias, int act, T* out) {
+    if constexpr (CAN8)
+      if (p8) return gemm_store_i8(in8, w8, (int)rows, n, (int)d, bias, act, out, st);
+    return gemm_store<T>(U, d, (const T*)wt, (int)rows, n, (int)d, bias, act, out, n, st);
+  };
+  auto residual = [&](const T* u, int k, const void* wt, const I8Weight& w8, const float* bias, const float* gate,
+                      T* y) {
+    if constexpr (CAN8)
+      if (p8) {
+        const hipError_t s = rows_8bit(m, w, u, rows, k);
+        return s != hipSuccess ? s : gemm_residual_i8(in8, w8, (int)rows, (int)d, k, bias, gate, Z, y, st);
+      }
+    return gemm_residual<T>(u, k, (const T*)wt, (int)rows, (int)d, k, bias, gate, Z, y, st);
+  };
+  auto qkv = [&](const Block& bk) {
+    if constexpr (CAN8)
+      if (p8) return gemm_qkv_i8(in8, bk.qkv8, (int)rows, (int)d, bk.qkv_b, (int)L, QK, VT, m->Lp, st);
+    return gemm_qkv<T>(U, (const T*)bk.qkv_w, (int)rows, (int)d, bk.qkv_b, (int)L, QK, VT, m->Lp, st);
+  };
 
   TRY(time_cond<T>(m, t));
   {
@@ -586,9 +642,9 @@ static cs_status dit_forward(cs_model* m, Workspace& w, const CtxKV* c, const cs
       HIPC(residual_add<T>(Z, y_self, md + 2 * d, rows, (int)d, st));
     } else {
     { ProfScope ps(pf, CS_K_NORM, st);
-      HIPC(layer_norm_mod<T>(Z, rows, (int)d, md + 0 * d, md + 1 * d, 0, U, st)); }
+      HIPC(norm(md + 0 * d, md + 1 * d, 0)); }
     { ProfScope ps(pf, CS_K_GEMM, st);
-      HIPC(gemm_qkv<T>(U, (const T*)bk.qkv_w, (int)rows, (int)d, bk.qkv_b, (int)L, QK, VT, m->Lp, st)); }
+      HIPC(qkv(bk)); }
     { ProfScope ps(pf, CS_K_NORM, st);
       HIPC(norm_rows<T>(m, QK, rows, 2 * d, 2, bk.q_gain, bk.k_gain, m->rope)); }
     {
@@ -603,8 +659,7 @@ static cs_status dit_forward(cs_model* m, Workspace& w, const CtxKV* c, const cs
       HIPC(flash_attention<T>(a, g.head_dim, st));
     }
     { ProfScope ps(pf, CS_K_GEMM, st);
-      HIPC(gemm_residual<T>(O, d, (const T*)bk.o_w, (int)rows, (int)d, (int)d, bk.o_b, md + 2 * d, Z,
-                            self_mode == PAB_STORE ? y_self : nullptr, st)); }
+      HIPC(residual(O, (int)d, bk.o_w, bk.o8, bk.o_b, md + 2 * d, self_mode == PAB_STORE ? y_self : nullptr)); }
     }
     // cross-attention
     if (cross_mode == PAB_REUSE) {
@@ -612,9 +667,9 @@ static cs_status dit_forward(cs_model* m, Workspace& w, const CtxKV* c, const cs
       HIPC(residual_add<T>(Z, y_cross, nullptr, rows, (int)d, st));
     } else {
     { ProfScope ps(pf, CS_K_NORM, st);
-      HIPC(layer_norm_mod<T>(Z, rows, (int)d, bk.ca_ln_g, bk.ca_ln_b, 1, U, st)); }
+      HIPC(norm(bk.ca_ln_g, bk.ca_ln_b, 1)); }
     { ProfScope ps(pf, CS_K_GEMM, st);
-      HIPC(gemm_store<T>(U, d, (const T*)bk.caq_w, (int)rows, (int)d, (int)d, bk.caq_b, 0, Q2, d, st)); }
+      HIPC(store(bk.caq_w, bk.caq8, (int)d, bk.caq_b, 0, Q2)); }
     { ProfScope ps(pf, CS_K_NORM, st);
       HIPC(norm_rows<T>(m, Q2, rows, d, 1, bk.caq_gain, nullptr, nullptr)); }
     if (cx) {
@@ -632,16 +687,14 @@ static cs_status dit_forward(cs_model* m, Workspace& w, const CtxKV* c, const cs
       HIPC(flash_attention<T>(a, g.head_dim, st));
     }
     { ProfScope ps(pf, CS_K_GEMM, st);
-      HIPC(gemm_residual<T>(O, d, (const T*)bk.cao_w, (int)rows, (int)d, (int)d, bk.cao_b, nullptr, Z,
-                            cross_mode == PAB_STORE ? y_cross : nullptr, st)); }
+      HIPC(residual(O, (int)d, bk.cao_w, bk.cao8, bk.cao_b, nullptr, cross_mode == PAB_STORE ? y_cross : nullptr)); }
     }
     // feed-forward
     { ProfScope ps(pf, CS_K_NORM, st);
-      HIPC(layer_norm_mod<T>(Z, rows, (int)d, md + 3 * d, md + 4 * d, 0, U, st)); }
+      HIPC(norm(md + 3 * d, md + 4 * d, 0)); }
     { ProfScope ps(pf, CS_K_GEMM, st);
-      HIPC(gemm_store<T>(U, d, (const T*)bk.ffn1_w, (int)rows, F, (int)d, bk.ffn1_b, 1, Hh, F, st));
-      HIPC(gemm_residual<T>(Hh, F, (const T*)bk.ffn2_w, (int)rows, (int)d, F, bk.ffn2_b, md + 5 * d, Z,
-                            nullptr, st)); }
+      HIPC(store(bk.ffn1_w, bk.ffn1_8, F, bk.ffn1_b, 1, Hh));
+      HIPC(residual(Hh, F, bk.ffn2_w, bk.ffn2_8, bk.ffn2_b, md + 5 * d, nullptr)); }
   }
   { ProfScope ps(pf, CS_K_NORM, st);
     HIPC(layer_norm_mod<T>(Z, rows, (int)d, m->hmod, m->hmod + d, 0, U, st)); }
@@ -708,10 +761,14 @@ cs_status cs_model_weight_count(const cs_model_desc* desc, size_t* count) {
   })
 }
 
-static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const float* weights, size_t n_weights,
-                                 void* stream, cs_model** out) {
+static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, int proj, const float* weights,
+                                 size_t n_weights, void* stream, cs_model** out) {
   TRY(validate_desc(desc));
   CHECK(qk_norm == CS_QK_NORM_FULL || qk_norm == CS_QK_NORM_HEAD, CS_E_INVAL, "unknown qk_norm %d", qk_norm);
+  CHECK(proj == CS_PROJ_NATIVE || proj == CS_PROJ_8BIT, CS_E_INVAL, "unknown proj %d", proj);
+  CHECK(proj == CS_PROJ_NATIVE || desc->dtype == CS_BF16, CS_E_UNSUPPORTED, "projections in 8 bits need dtype CS_BF16");
+  CHECK(proj == CS_PROJ_NATIVE || (desc->hidden <= LN_MAX_DIM && desc->ffn <= I8_MAX_DIM), CS_E_UNSUPPORTED,
+        "projections in 8 bits need hidden up to %d and ffn up to %d", LN_MAX_DIM, I8_MAX_DIM);
   CHECK(out, CS_E_INVAL, "out is NULL");
   *out = nullptr;
   CHECK(weights, CS_E_INVAL, "weights is NULL");
@@ -723,6 +780,7 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
   std::unique_ptr<cs_model> m(new cs_model());
   m->desc = *desc;
   m->qk_norm = qk_norm;
+  m->proj8 = proj == CS_PROJ_8BIT;
   m->stream = (hipStream_t)stream;
   m->esz = desc->dtype == CS_BF16 ? 2 : 4;
   m->d = desc->hidden;
@@ -744,6 +802,18 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
     return t.matrix && t.name != "time1_w" && t.name != "time2_w" &&
            t.name != "mod_w";
   };
+  // a block's projections but the text keys' and values': in 8 bits where asked for, their
+  // scales behind their codes
+  auto ends = [](const std::string& s, const char* e) {
+    const std::string t(e);
+    return s.size() > t.size() && s.compare(s.size() - t.size(), t.size(), t) == 0;
+  };
+  auto eight = [&](const TSpec& t) {
+    if (!m->proj8) return false;
+    for (const char* e : {".qkv_w", ".o_w", ".caq_w", ".cao_w", ".ffn1_w", ".ffn2_w"})
+      if (ends(t.name, e)) return true;
+    return false;
+  };
   std::vector<size_t> off(spec.size());
   size_t bytes = 0;
   const size_t tables_bytes = (size_t)desc->n_blocks * 6 * m->d * sizeof(float);
@@ -753,6 +823,10 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
     const bool is_table = spec[i].name.size() > 4 && spec[i].name.compare(spec[i].name.size() - 4, 4, ".mod") == 0;
     if (is_table) { off[i] = (size_t)-1; continue; }
     off[i] = bytes;
+    if (eight(spec[i])) {
+      bytes += i8_weight_bytes((int)spec[i].rows, (int)spec[i].cols) + round_up(spec[i].rows * 4, 256);
+      continue;
+    }
     const long elems = tiled(spec[i]) ? gemm_tiled_weight_elems((int)spec[i].rows, (int)spec[i].cols)
                                       : spec[i].rows * spec[i].cols;
     bytes += round_up((size_t)elems * (spec[i].matrix ? m->esz : 4), 256);
@@ -763,6 +837,7 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
   size_t src = 0;
   int table_j = 0;
   std::vector<const void*> ptr(spec.size());
+  std::vector<I8Weight> w8(spec.size(), I8Weight{nullptr, nullptr});
   for (size_t i = 0; i < spec.size(); ++i) {
     const long n = spec[i].rows * spec[i].cols;
     if (off[i] == (size_t)-1) {
@@ -770,6 +845,12 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
       HIPC(hipMemcpyAsync(dst, weights + src, n * sizeof(float), hipMemcpyDeviceToDevice, st));
       ptr[i] = dst;
       ++table_j;
+    } else if (eight(spec[i])) {
+      const int rows = (int)spec[i].rows, cols = (int)spec[i].cols;
+      int8_t* codes = (int8_t*)(base + off[i]);
+      const cs_i8_weight o = {codes, (float*)(codes + i8_weight_bytes(rows, cols)), rows, cols};
+      HIPC(i8_weight_pack(o, CS_FP32, weights + src, cols, nullptr, st));
+      w8[i] = {o.codes, o.scales};
     } else if (spec[i].matrix) {
       if (tiled(spec[i]) && m->esz == 2)
         HIPC(gemm_tile_weight<bf16>(weights + src, (int)spec[i].rows, (int)spec[i].cols, (bf16*)(base + off[i]), st));
@@ -789,6 +870,7 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
   m->mod_tables = (const float*)(base + tables_off);
   size_t k = 0;
   auto P_ = [&]() { return ptr[k++]; };
+  auto M_ = [&](I8Weight& o) { o = w8[k]; return ptr[k++]; };
   auto F_ = [&]() { return (const float*)ptr[k++]; };
   m->patch_w = P_(); m->patch_b = F_();
   m->text1_w = P_(); m->text1_b = F_();
@@ -800,13 +882,13 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
   for (int j = 0; j < desc->n_blocks; ++j) {
     Block& b = m->blocks[j];
     (void)P_();  // modulation table (gathered above)
-    b.qkv_w = P_(); b.qkv_b = F_(); b.q_gain = F_(); b.k_gain = F_();
-    b.o_w = P_(); b.o_b = F_();
+    b.qkv_w = M_(b.qkv8); b.qkv_b = F_(); b.q_gain = F_(); b.k_gain = F_();
+    b.o_w = M_(b.o8); b.o_b = F_();
     b.ca_ln_g = F_(); b.ca_ln_b = F_();
-    b.caq_w = P_(); b.caq_b = F_(); b.cak_w = P_(); b.cak_b = F_();
+    b.caq_w = M_(b.caq8); b.caq_b = F_(); b.cak_w = P_(); b.cak_b = F_();
     b.cav_w = P_(); b.cav_b = F_(); b.caq_gain = F_(); b.cak_gain = F_();
-    b.cao_w = P_(); b.cao_b = F_();
-    b.ffn1_w = P_(); b.ffn1_b = F_(); b.ffn2_w = P_(); b.ffn2_b = F_();
+    b.cao_w = M_(b.cao8); b.cao_b = F_();
+    b.ffn1_w = M_(b.ffn1_8); b.ffn1_b = F_(); b.ffn2_w = M_(b.ffn2_8); b.ffn2_b = F_();
   }
   m->head_mod = F_(); m->head_w = P_(); m->head_b = F_();
 
@@ -848,12 +930,17 @@ static cs_status model_init_impl(const cs_model_desc* desc, int qk_norm, const f
 
 cs_status cs_model_init(const cs_model_desc* desc, const float* weights, size_t n_weights,
                         void* stream, cs_model** out) {
-  GUARD({ return model_init_impl(desc, CS_QK_NORM_FULL, weights, n_weights, stream, out); })
+  GUARD({ return model_init_impl(desc, CS_QK_NORM_FULL, CS_PROJ_NATIVE, weights, n_weights, stream, out); })
 }
 
 cs_status cs_model_init_norm(const cs_model_desc* desc, int32_t qk_norm, const float* weights, size_t n_weights,
                              void* stream, cs_model** out) {
-  GUARD({ return model_init_impl(desc, qk_norm, weights, n_weights, stream, out); })
+  GUARD({ return model_init_impl(desc, qk_norm, CS_PROJ_NATIVE, weights, n_weights, stream, out); })
+}
+
+cs_status cs_model_init_proj(const cs_model_desc* desc, int32_t qk_norm, int32_t proj, const float* weights,
+                             size_t n_weights, void* stream, cs_model** out) {
+  GUARD({ return model_init_impl(desc, qk_norm, proj, weights, n_weights, stream, out); })
 }
 
 void cs_model_free(cs_model* model) {

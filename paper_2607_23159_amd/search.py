@@ -26,7 +26,7 @@ class GpuModel:
     """A model handle whose weights were uploaded from a flat float32 array."""
 
     def __init__(self, cfg, weights: np.ndarray, dtype: Optional[int] = None, stream=None,
-                 qk_norm: int = B.CS_QK_NORM_FULL):
+                 qk_norm: int = B.CS_QK_NORM_FULL, proj: int = B.CS_PROJ_NATIVE):
         self.cfg = cfg
         self.contexts = set()     # handles of its prompts, which are freed before it
         self.desc = B.model_desc(cfg, dtype)
@@ -35,7 +35,7 @@ class GpuModel:
             raise ValueError(f"weight array has {weights.size} values, model needs {n}")
         w = _dev(weights)
         self.stream = stream
-        self.h = B.cs_model_init_norm(self.desc, qk_norm, w, n, stream)
+        self.h = B.cs_model_init_proj(self.desc, qk_norm, proj, w, n, stream)
         del w
         torch.cuda.synchronize()
 

@@ -249,3 +249,19 @@ def test_operators_run_on_the_current_stream_or_the_given_one(recorder):  # noqa
         assert [c[0] for c in recorder.calls] == ["cs_layer_norm", "cs_layer_norm_backward", "cs_i8_quantise",
                                                   "cs_i8_dequantise", "cs_matmul_i8"]
         assert [args[-1] for _, args in recorder.calls] == [want] * 5
+
+
+def test_projections_in_8_bits_refuse_fp32_and_unknown_formats():
+    from paper_2607_23159_amd import synth
+    out = C.c_void_p()
+    m = synth.MODELS["tiny"]
+    n = synth.weight_count(m)
+
+    def go(dtype, proj, w=P, count=n):
+        return B.lib().cs_model_init_proj(C.byref(B.model_desc(m, dtype)), 0, proj, w, count, None, C.byref(out))
+    refused(go(B.CS_FP32, B.CS_PROJ_8BIT), "UNSUPPORTED", "CS_BF16")
+    refused(go(B.CS_BF16, 2), "INVAL", "proj")
+    refused(go(B.CS_BF16, -1), "INVAL", "proj")
+    refused(go(B.CS_I8, B.CS_PROJ_8BIT), "INVAL", "dtype")
+    refused(go(B.CS_BF16, B.CS_PROJ_8BIT, w=None), "INVAL", "weights")
+    refused(go(B.CS_BF16, B.CS_PROJ_8BIT, count=n - 1), "INVAL", "expected")
