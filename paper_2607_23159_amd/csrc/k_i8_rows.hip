@@ -50,13 +50,15 @@ __global__ __launch_bounds__(256) void k_i8_dequantise(I8RowsArgs a) {
 template <typename X> static hipError_t quantise(const I8RowsArgs& a, hipStream_t st) {
   constexpr int U = sizeof(X) == 2 ? 8 : 4;
   if (a.d.dim > 16384) {   // a workgroup of 16 waves to a row
+    if (const hipError_t s = check_grid(a.d.rows, 1024); s != hipSuccess) return s;
     hipLaunchKernelGGL((k_i8_quantise<X, U, 16, 64 / U, true>), dim3((unsigned)a.d.rows), dim3(1024), 0, st, a);
     return hipGetLastError();
   }
   return with_row_shape<U>(a.d.dim, [&](auto shape) {
     typedef decltype(shape) S;
-    const unsigned grid = (unsigned)(S::WPR == 1 ? ((long)a.d.rows + 3) / 4 : a.d.rows);
-    hipLaunchKernelGGL((k_i8_quantise<X, U, S::WPR, S::NV, S::TAIL>), dim3(grid), dim3(256), 0, st, a);
+    const long grid = S::WPR == 1 ? ((long)a.d.rows + 3) / 4 : a.d.rows;
+    if (const hipError_t s = check_grid(grid, 256); s != hipSuccess) return s;
+    hipLaunchKernelGGL((k_i8_quantise<X, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)grid), dim3(256), 0, st, a);
     return hipGetLastError();
   });
 }
@@ -70,8 +72,9 @@ template <typename X> static hipError_t dequantise(const I8RowsArgs& a, hipStrea
   const bool tail = a.d.dim % U != 0, wide = a.d.dim > 2048;
   const auto kernel = wide ? (tail ? k_i8_dequantise<X, U, 4, true> : k_i8_dequantise<X, U, 4, false>)
                            : (tail ? k_i8_dequantise<X, U, 1, true> : k_i8_dequantise<X, U, 1, false>);
-  const unsigned grid = (unsigned)(wide ? a.d.rows : ((long)a.d.rows + 3) / 4);
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a);
+  const long grid = wide ? a.d.rows : ((long)a.d.rows + 3) / 4;
+  if (const hipError_t s = check_grid(grid, 256); s != hipSuccess) return s;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -29,6 +29,20 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
     const int c = U * (64 * WPR * i + t);
     raw[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
   }
+  const int group = (int)((uint32_t)row / (uint32_t)a.d.rows);   // rows in all are below 2^31
+  const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
+  const float* b = a.bias ? a.bias + group * a.d.b_group : nullptr;
+  const float one = a.d.unit_offset ? 1.0f : 0.0f;
+  f32x4 wv[NV][U / 4], bv[NV][U / 4];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int h = 0; h < U / 4; ++h) {
+      const int c = U * (64 * WPR * i + t) + 4 * h;
+      wv[i][h] = bv[i][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (w) wv[i][h] = load_chunk<float, 4, TAIL>(w + c, dim - c);
+      if (b) bv[i][h] = load_chunk<float, 4, TAIL>(b + c, dim - c);
+    }
   float s = 0.0f, q = 0.0f;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
@@ -49,24 +63,12 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
   }
-  const int group = (int)((uint32_t)row / (uint32_t)a.d.rows);   // rows in all are below 2^31
-  const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
-  const float* b = a.bias ? a.bias + group * a.d.b_group : nullptr;
-  const float one = a.d.unit_offset ? 1.0f : 0.0f;
   // the result of chunk i
   auto result = [&](int i, float* y) {
-    const int c = U * (64 * WPR * i + t);
-    f32x4 wv[U / 4], bv[U / 4];
-#pragma unroll
-    for (int h = 0; h < U / 4; ++h) {
-      wv[h] = bv[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (w) wv[h] = load_chunk<float, 4, TAIL>(w + c + 4 * h, dim - c - 4 * h);
-      if (b) bv[h] = load_chunk<float, 4, TAIL>(b + c + 4 * h, dim - c - 4 * h);
-    }
 #pragma unroll
     for (int e = 0; e < U; ++e) {
       const float n = (to_f(raw[i][e]) - mean) * rstd;
-      y[e] = fmaf(n, w ? one + wv[e / 4][e % 4] : 1.0f, bv[e / 4][e % 4]);
+      y[e] = fmaf(n, w ? one + wv[i][e / 4][e % 4] : 1.0f, bv[i][e / 4][e % 4]);
     }
   };
   if constexpr (std::is_same<Y, int8_t>::value) {
@@ -100,8 +102,9 @@ static hipError_t forward(const LayerNormArgs& a, hipStream_t st) {
   constexpr int U = sizeof(X) == 2 ? 8 : 4;   // x alone decides: a row's sums do not depend on y's type
   return with_row_shape<U>(a.d.dim, [&](auto shape) {
     typedef decltype(shape) S;
-    const unsigned grid = (unsigned)(S::WPR == 1 ? (total + 3) / 4 : total);
-    hipLaunchKernelGGL((k_layer_norm_op<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3(grid), dim3(256), 0, st, a);
+    const long grid = S::WPR == 1 ? (total + 3) / 4 : total;
+    if (const hipError_t s = check_grid(grid, 256); s != hipSuccess) return s;
+    hipLaunchKernelGGL((k_layer_norm_op<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)grid), dim3(256), 0, st, a);
     return hipGetLastError();
   });
 }
@@ -272,18 +275,21 @@ __global__ __launch_bounds__(1024) void k_layer_norm_grad_sum(LayerNormGradArgs 
 template <typename X, typename Y>
 static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
   const int parts = ln_parts(a.d.rows), part_rows = ln_part_rows(a.d.rows);
+  const long blocks = (long)a.d.groups * parts, sums = (long)a.d.groups * cdiv(a.d.dim, 64);
+  if (const hipError_t s = check_grid(blocks, 256); s != hipSuccess) return s;
+  if (const hipError_t s = check_grid(sums, 1024); s != hipSuccess) return s;
   if (a.d.rows > 0) {
     constexpr int U = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
     const hipError_t s = with_row_shape<U>(a.d.dim, [&](auto shape) {
       typedef decltype(shape) S;
-      hipLaunchKernelGGL((k_layer_norm_grad<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)a.d.groups * parts), dim3(256),
+      hipLaunchKernelGGL((k_layer_norm_grad<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)blocks), dim3(256),
                          0, st, a, parts, part_rows);
       return hipGetLastError();
     });
     if (s != hipSuccess) return s;
   }
   if (!a.dweight && !a.dbias) return hipSuccess;
-  hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)((long)cdiv(a.d.dim, 64) * a.d.groups), 2), dim3(1024), 0, st, a,
+  hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)sums, 2), dim3(1024), 0, st, a,
                      parts);
   return hipGetLastError();
 }

@@ -91,6 +91,8 @@ static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream
 template <class To> static hipError_t product(const MatmulI8Args& a, const To& to, hipStream_t st) {
   const EpiI8<To> epi = {a.a_scale, a.w.scales, a.bias, (int)round_up(a.d.k, 16), to};
   const int kp = (int)round_up(a.d.k, 128);
+  // the most workgroups: tiles of 32 x 32 of 4 waves, or an eighth as many of 64 x 128 of 8
+  if (const hipError_t s = check_grid((long)cdiv(a.d.rows, 32) * cdiv(a.d.n, 32), 256); s != hipSuccess) return s;
   constexpr bool RES = EpiIsResidual<To>::value;
   constexpr int PD = RES ? 8 : 2, PD2 = RES ? 4 : 2;   // as in bf16
   if (a.d.rows <= FEW_ROWS && a.d.n <= FEW_COLS) {

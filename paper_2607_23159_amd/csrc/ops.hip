@@ -263,6 +263,13 @@ cs_status cs_kv4_attention(const cs_attn_desc* desc, const void* q, const cs_kv4
   })
 }
 
+// A launch that does not fit a grid, or the error it ended with.
+static cs_status launched(hipError_t s, const char* what) {
+  CHECK(s != hipErrorInvalidConfiguration, CS_E_UNSUPPORTED, "too many %s for one call", what);
+  HIPC(s);
+  return CS_OK;
+}
+
 // ------------------------------------------------------------- layer norm
 // What the two descriptors have in common.
 static cs_status check_norm_rows(int x_dtype, int groups, int rows, int dim, int unit_offset, long w_group) {
@@ -295,8 +302,7 @@ cs_status cs_layer_norm(const cs_layer_norm_desc* d, const void* x, const float*
     if (d->y_dtype == CS_I8) TRY(check_tensor(y_scale, "y_scale"));
     TRY(check_optional(mean, "mean"));
     TRY(check_optional(rstd, "rstd"));
-    HIPC(layer_norm({x, weight, bias, y, y_scale, mean, rstd, *d}, (hipStream_t)stream));
-    return CS_OK;
+    return launched(layer_norm({x, weight, bias, y, y_scale, mean, rstd, *d}, (hipStream_t)stream), "rows");
   })
 }
 
@@ -304,8 +310,6 @@ static cs_status check_norm_grad(const cs_layer_norm_grad_desc* d) {
   CHECK(d, CS_E_INVAL, "desc is NULL");
   TRY(check_norm_rows(d->x_dtype, d->groups, d->rows, d->dim, d->unit_offset, d->w_group));
   CHECK(d->y_dtype == CS_BF16 || d->y_dtype == CS_FP32, CS_E_INVAL, "y_dtype must be CS_BF16 or CS_FP32");
-  // grids: parts of 16 rows at least, and 64 channels of a group
-  CHECK((long)d->groups * (cdiv(d->dim, 64) + 1) < (1L << 31), CS_E_UNSUPPORTED, "too many groups for one call");
   const long total = (long)d->groups * d->rows;
   TRY(check_stride(d->x_row, total, elem(d->x_dtype), "x_row"));
   TRY(check_stride(d->dy_row, total, elem(d->y_dtype), "dy_row"));
@@ -346,8 +350,8 @@ cs_status cs_layer_norm_backward(const cs_layer_norm_grad_desc* d, const void* x
       TRY(check_work(work, work_bytes, layer_norm_backward_workspace(*d)));
       part = (float*)work;
     }
-    HIPC(layer_norm_backward({x, dy, weight, mean, rstd, dx, dweight, dbias, part, *d}, (hipStream_t)stream));
-    return CS_OK;
+    return launched(layer_norm_backward({x, dy, weight, mean, rstd, dx, dweight, dbias, part, *d}, (hipStream_t)stream),
+                    "groups and rows");
   })
 }
 
@@ -366,8 +370,7 @@ static cs_status i8_rows_call(const cs_i8_rows* r, const void* x, void* x_out, c
   TRY(check_tensor(codes, "codes"));
   TRY(check_tensor(scales, "scales"));
   const I8RowsArgs a = {x, x_out, (int8_t*)codes, (float*)scales, *r};
-  HIPC(store ? i8_quantise(a, (hipStream_t)stream) : i8_dequantise(a, (hipStream_t)stream));
-  return CS_OK;
+  return launched(store ? i8_quantise(a, (hipStream_t)stream) : i8_dequantise(a, (hipStream_t)stream), "rows");
 }
 
 cs_status cs_i8_quantise(const cs_i8_rows* rows, const void* x, int8_t* codes, float* scales, void* stream) {
@@ -424,8 +427,6 @@ static cs_status check_matmul(const cs_matmul_i8_desc* d) {
   CHECK(d->rows <= (1 << 30), CS_E_UNSUPPORTED, "rows must be at most 2^30");
   TRY(check_weight_size(d->n, d->k));
   CHECK(d->act == CS_ACT_NONE || d->act == CS_ACT_GELU, CS_E_INVAL, "unknown act %d", d->act);
-  // tiles of 32 x 32 at least
-  CHECK((long)cdiv(d->rows, 32) * cdiv(d->n, 32) < (1L << 31), CS_E_UNSUPPORTED, "too many rows and outputs for one call");
   TRY(check_stride(d->a_row, d->rows, 1, "a_row"));
   // offsets inside a tile of rows are 32-bit byte counts
   CHECK(d->rows <= 1 || d->a_row <= (1 << 22), CS_E_UNSUPPORTED, "stride a_row must be at most 2^22");
@@ -455,8 +456,7 @@ cs_status cs_matmul_i8(const cs_matmul_i8_desc* d, const int8_t* a, const float*
     TRY(check_work(work, work_bytes, matmul_i8_workspace(*d)));
     MatmulI8Args m = {a, a_scales, bias, *weight, out, *d};
     if (d->rows == 1) m.d.a_row = round_up(d->k, 16), m.d.o_row = round_up(d->n, 8);   // never checked
-    HIPC(matmul_i8(m, work, (hipStream_t)stream));
-    return CS_OK;
+    return launched(matmul_i8(m, work, (hipStream_t)stream), "rows and outputs");
   })
 }
 

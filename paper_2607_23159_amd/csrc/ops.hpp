@@ -28,6 +28,11 @@ struct QkNormArgs {
 };
 template <typename T> hipError_t qk_norm_rope(const QkNormArgs& a, hipStream_t st);
 
+// A launch counts its work items in 32 bits.
+inline hipError_t check_grid(long blocks, int threads) {
+  return blocks * threads < (1L << 32) ? hipSuccess : hipErrorInvalidConfiguration;
+}
+
 // ---- layer norm (k_layer_norm.hip)
 constexpr int LN_MAX_DIM = 16384;
 struct LayerNormArgs {

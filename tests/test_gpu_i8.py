@@ -129,7 +129,7 @@ MM = [  # rows, n, k
     (17, 64, 130), (31, 257, 300), (32, 512, 512), (33, 31, 640), (64, 64, 128), (65, 100, 1000), (100, 1000, 65),
     (128, 128, 4096), (129, 255, 1030), (200, 700, 333), (257, 513, 256), (300, 96, 8960), (511, 2049, 70),
     (891, 512, 256), (1, 300, 13824), (5, 260, 65536), (1030, 1540, 200), (2100, 300, 390), (64, 5000, 140),
-    (4200, 1100, 80),
+    (4200, 1100, 80), (16, 4096, 70), (16, 4097, 70), (17, 4096, 70), (9, 4000, 1100),
 ]
 
 

@@ -75,7 +75,7 @@ def test_norm_pointers_and_nothing_to_do():
 @pytest.mark.parametrize("kw,status,word", COMMON + [
     (dict(y_dtype=B.CS_I8), "INVAL", "y_dtype"), (dict(dy_row=4), "INVAL", "dy_row"), (dict(dx_row=2), "INVAL", "dx_row"),
     (dict(dx_row=0), "INVAL", "output stride"), (dict(dw_group=0), "INVAL", "dw_group"),
-    (dict(db_group=2), "INVAL", "db_group"), (dict(groups=1 << 30, rows=0, dim=1024), "UNSUPPORTED", "groups")])
+    (dict(db_group=2), "INVAL", "db_group")])
 def test_norm_grad_descriptors(kw, status, word):
     refused(grad(grad_desc(**kw)), status, word)
 
@@ -180,7 +180,7 @@ def mm(d, a=P, s=P, w="default", b=None, o=P, work=None, nbytes=0):
     (dict(rows=(1 << 30) + 1), "UNSUPPORTED", "2^30"), (dict(n=0), "INVAL", "n and k"), (dict(k=-1), "INVAL", "n and k"),
     (dict(k=70000), "UNSUPPORTED", "65536"), (dict(act=2), "INVAL", "act"), (dict(a_row=40), "INVAL", "a_row"),
     (dict(a_row=(1 << 22) + 16), "UNSUPPORTED", "a_row"), (dict(o_row=20), "INVAL", "o_row"),
-    (dict(o_row=0), "INVAL", "output stride"), (dict(rows=1 << 30, n=1 << 24), "UNSUPPORTED", "too many"),
+    (dict(o_row=0), "INVAL", "output stride"),
     (dict(n=25), "INVAL", "weight's"), (dict(k=39), "INVAL", "weight's")])
 def test_product_descriptors(kw, status, word):
     refused(mm(mm_desc(**kw)), status, word)
@@ -249,6 +249,23 @@ def test_operators_run_on_the_current_stream_or_the_given_one(recorder):  # noqa
         assert [c[0] for c in recorder.calls] == ["cs_layer_norm", "cs_layer_norm_backward", "cs_i8_quantise",
                                                   "cs_i8_dequantise", "cs_matmul_i8"]
         assert [args[-1] for _, args in recorder.calls] == [want] * 5
+
+
+def test_calls_too_large_for_a_grid():
+    """A launch has fewer than 2^32 work items."""
+    wide = dict(groups=1, rows=1 << 24, dim=4096, x_row=4096)
+    refused(norm(norm_desc(y_row=4096, **wide)), "UNSUPPORTED", "too many")
+    refused(norm(norm_desc(groups=1, rows=1 << 27, x_row=40, y_row=40)), "UNSUPPORTED", "too many")
+    refused(grad(grad_desc(groups=1 << 24, rows=1), nbytes=1 << 60), "UNSUPPORTED", "too many")
+    refused(grad(grad_desc(groups=1 << 18, rows=0, dim=1024, w_group=1024, dw_group=1024, db_group=1024)), "UNSUPPORTED",
+            "too many")
+    for kw in (dict(rows=1 << 24, dim=4096, x_row=4096, q_row=4096), dict(rows=1 << 27, dim=16, x_row=16, q_row=16),
+               dict(rows=1 << 22, dim=20000, x_row=20000, q_row=20000)):
+        r = C.byref(rows(**kw))
+        refused(B.lib().cs_i8_quantise(r, P, P, P, None), "UNSUPPORTED", "too many")
+        if kw["dim"] != 20000:
+            refused(B.lib().cs_i8_dequantise(r, P, P, P, None), "UNSUPPORTED", "too many")
+    refused(mm(mm_desc(rows=1 << 30, n=1 << 14, o_row=1 << 14), w=weight(n=1 << 14)), "UNSUPPORTED", "too many")
 
 
 def test_projections_in_8_bits_refuse_fp32_and_unknown_formats():
