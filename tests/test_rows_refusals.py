@@ -220,6 +220,12 @@ def test_binding_refuses_host_tensors_and_other_types():
     for call in (lambda: B.layer_norm_desc(x.half(), x), lambda: B.i8_rows_desc(x.double(), q, s)):
         with pytest.raises(ValueError, match="bfloat16 or float32"):
             call()
+    for bad in (s, s.double(), torch.zeros(3)):
+        with pytest.raises(ValueError):
+            B._vector(bad, 4, "scales", DEV)
+    assert B._vector(s, 4, "scales", s.device) == s.data_ptr()
+    with pytest.raises(ValueError):
+        B._vector(torch.zeros(8)[::2], 4, "scales", s.device)
     with pytest.raises(ValueError, match="3 groups"):
         B._norm_rows(x, 3)
     with pytest.raises(ValueError, match="without it"):
