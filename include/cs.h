@@ -451,7 +451,9 @@ typedef struct {
  * The variance is that of the centred values, over dim; a row whose squared deviations add up
  * to 3.4e38 or more gives its bias.  weight, bias: fp32 [groups][dim], NULL for 1 and 0.  mean,
  * rstd: fp32 [groups * rows], written for the backward pass, or NULL.  y_scale: the rows' scales
- * where y_dtype is CS_I8 (else not read).  y may be x (same pointer, type and stride). */
+ * where y_dtype is CS_I8 (else not read).  y may be x (same pointer, type and stride).  NaN: a row that is
+ * not finite or whose values add up to 3.4e38 or more, and with eps 0 one without variance.  groups *
+ * rows is below 2^30. */
 cs_status cs_layer_norm(const cs_layer_norm_desc* desc, const void* x, const float* weight, const float* bias, void* y,
                         float* y_scale, float* mean, float* rstd, void* stream);
 
@@ -468,7 +470,7 @@ typedef struct {
  *   dweight = sum of dy n and dbias = sum of dy over the rows of each group, fp32
  * [groups][dim] (one group: over all rows).  mean, rstd: as cs_layer_norm wrote them.  dx,
  * dweight and dbias may be NULL; the workspace is needed for the last two only.  A group of no
- * rows gets zeros there.  dx may be x or dy.  The sums over rows are taken in an order that
+ * rows gets zeros there.  dx may be x or dy (same pointer, type and stride).  The sums over rows are taken in an order that
  * depends on rows and dim alone: a group's gradients are bitwise the same alone and among
  * others. */
 cs_status cs_layer_norm_backward_workspace(const cs_layer_norm_grad_desc* desc, size_t* bytes);

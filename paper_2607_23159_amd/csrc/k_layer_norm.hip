@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
     const int c = U * (64 * WPR * i + t);
     raw[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
   }
-  const int group = (int)((uint32_t)row / (uint32_t)a.d.rows);   // rows in all are below 2^31
+  const int group = (int)((uint32_t)row / (uint32_t)a.d.rows);   // rows in all are below 2^30
   const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
   const float* b = a.bias ? a.bias + group * a.d.b_group : nullptr;
   const float one = a.d.unit_offset ? 1.0f : 0.0f;
@@ -150,7 +150,6 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
   const int dim = a.d.dim, t = WPR == 1 ? lane : (int)threadIdx.x;
   const int first = part * part_rows + (WPR == 1 ? wave : 0), last = min((part + 1) * part_rows, a.d.rows);
   const float inv = 1.0f / (float)dim;
-  // gains: past the row's end anything, since dy is zero there
   float gain[NV][U];
   {
     const float one = a.d.unit_offset ? 1.0f : 0.0f;
@@ -192,15 +191,19 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
     if (r + STEP < last) load(r + STEP, next);   // on its way while this row is reduced
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      const int left = dim - U * (64 * WPR * i + t);
+      if (left <= 0) continue;
 #pragma unroll
       for (int e = 0; e < U; ++e) {
+        if (TAIL && e >= left) continue;   // dy is zero there, but n need not be finite
         const float d = to_f(cur.dy[i][e]), n = (to_f(cur.x[i][e]) - cur.mean) * cur.rstd, g = d * gain[i][e];
         dw[i][e] = fmaf(d, n, dw[i][e]);
         db[i][e] += d;
         s1 += g;
         s2 = fmaf(g, n, s2);
       }
+    }
     const float2 m = row_sums<WPR>(s1, s2, lds[odd], wave);
     if (!a.dx) continue;
     const float m1 = m.x * inv, m2 = m.y * inv;

@@ -275,7 +275,7 @@ static cs_status launched(hipError_t s, const char* what) {
 static cs_status check_norm_rows(int x_dtype, int groups, int rows, int dim, int unit_offset, long w_group) {
   CHECK(x_dtype == CS_BF16 || x_dtype == CS_FP32, CS_E_INVAL, "x_dtype must be CS_BF16 or CS_FP32");
   CHECK(groups >= 0 && rows >= 0, CS_E_INVAL, "groups and rows must not be negative");
-  CHECK((long)groups * rows < (1L << 31), CS_E_UNSUPPORTED, "groups * rows must be below 2^31");
+  CHECK((long)groups * rows < (1L << 30), CS_E_UNSUPPORTED, "groups * rows must be below 2^30");
   CHECK(dim >= 1, CS_E_INVAL, "dim must be positive");
   CHECK(dim <= LN_MAX_DIM, CS_E_UNSUPPORTED, "dim must be at most %d", LN_MAX_DIM);
   CHECK(unit_offset == 0 || unit_offset == 1, CS_E_INVAL, "unit_offset must be 0 or 1");

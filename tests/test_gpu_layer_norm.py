@@ -253,6 +253,20 @@ def test_backward_of_no_rows_and_of_groups_alone():
             assert torch.equal(s["x"], t["x"][r]) and torch.equal(s["w"][0], t["w"][g]) and torch.equal(s["b"][0], t["b"][g])
 
 
+@pytest.mark.parametrize("dim", [1, 100, 101, 1536, 5000, 5001])
+def test_backward_of_rows_far_from_zero(dim):
+    """Channels that a row does not have must not count: their n would be -mean rstd, past fp32 here."""
+    x, dy, w, mean, rstd = grad_case(1, 5, dim, FP, FP, False)
+    x.fill_(1e37)
+    mean.fill_(1e37)
+    rstd.fill_(1000.0)
+    t = run_grad(x, dy, w, mean, rstd, 1, False)
+    (dx, off), dw, db = R.layer_norm_grad(x, dy, w, mean, rstd, 1, False)
+    within(t["x"], dx, off + R.HALF[FP] * (dx.abs() + off), "dx")
+    within(t["w"], *dw, "dw")
+    within(t["b"], *db, "db")
+
+
 @pytest.mark.parametrize("dim", [96, 5120])
 def test_backward_in_place(dim):
     x, dy, w, mean, rstd = grad_case(2, 21, dim, BF, BF, False)

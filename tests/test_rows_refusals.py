@@ -42,8 +42,8 @@ def grad(d, x=P, dy=P, w=P, mean=P, rstd=P, dx=P, dw=P, db=P, work=P, nbytes=1 <
 
 COMMON = [
     (dict(x_dtype=B.CS_I8), "INVAL", "x_dtype"), (dict(x_dtype=-1), "INVAL", "x_dtype"), (dict(groups=-1), "INVAL", "groups"),
-    (dict(rows=-1), "INVAL", "rows"), (dict(groups=1 << 16, rows=1 << 15), "UNSUPPORTED", "2^31"),
-    (dict(groups=BIG, rows=BIG), "UNSUPPORTED", "2^31"), (dict(dim=0), "INVAL", "dim"), (dict(dim=-8), "INVAL", "dim"),
+    (dict(rows=-1), "INVAL", "rows"), (dict(groups=1 << 16, rows=1 << 14), "UNSUPPORTED", "2^30"),
+    (dict(groups=BIG, rows=BIG), "UNSUPPORTED", "2^30"), (dict(dim=0), "INVAL", "dim"), (dict(dim=-8), "INVAL", "dim"),
     (dict(dim=16385), "UNSUPPORTED", "dim"), (dict(unit_offset=2), "INVAL", "unit_offset"),
     (dict(w_group=2), "INVAL", "w_group"), (dict(w_group=-4), "INVAL", "w_group"), (dict(x_row=41), "INVAL", "x_row"),
     (dict(x_row=-40), "INVAL", "x_row"), (dict(x_row=1 << 60), "UNSUPPORTED", "x_row"),
