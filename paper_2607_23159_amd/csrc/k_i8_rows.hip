@@ -7,7 +7,7 @@
 
 namespace cs {
 
-template <typename X, int U, int WPR, int NV, bool TAIL>
+template <typename X, int U, int WPR, int NV, bool TAIL, bool FAR>
 __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void k_i8_quantise(I8RowsArgs a) {
   __shared__ uint32_t lds[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -19,7 +19,7 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void k_i8_quantise(I8RowsAr
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = U * (64 * WPR * i + t);
-    raw[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
+    raw[i] = load_chunk<X, U, TAIL, FAR>(x + c, dim - c);
   }
   std::conditional_t<sizeof(X) == 2, u16x2, uint32_t> m = {};
 #pragma unroll
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void k_i8_quantise(I8RowsAr
 }
 
 // WPR: waves of a row (1 or 4).
-template <typename X, int U, int WPR, bool TAIL>
+template <typename X, int U, int WPR, bool TAIL, bool FAR>
 __global__ __launch_bounds__(256) void k_i8_dequantise(I8RowsArgs a) {
   const int t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
   const long row = WPR == 1 ? (long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
@@ -44,22 +44,26 @@ __global__ __launch_bounds__(256) void k_i8_dequantise(I8RowsArgs a) {
     float y[U];
 #pragma unroll
     for (int e = 0; e < U; ++e) y[e] = scale * (float)v[e];
-    store_chunk<X, U, TAIL>(x + c, a.d.dim - c, y);
+    store_chunk<X, U, TAIL, FAR>(x + c, a.d.dim - c, y);
   }
 }
 
 template <typename X> static hipError_t quantise(const I8RowsArgs& a, hipStream_t st) {
   constexpr int U = sizeof(X) == 2 ? 8 : 4;
+  const bool far = past_caches((double)a.d.rows * a.d.dim * (sizeof(X) + 1));
   if (a.d.dim > 16384) {   // a workgroup of 16 waves to a row
     if (const hipError_t s = check_grid(a.d.rows, 1024); s != hipSuccess) return s;
-    hipLaunchKernelGGL((k_i8_quantise<X, U, 16, 64 / U, true>), dim3((unsigned)a.d.rows), dim3(1024), 0, st, a);
+    const auto kernel = far ? k_i8_quantise<X, U, 16, 64 / U, true, true> : k_i8_quantise<X, U, 16, 64 / U, true, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.d.rows), dim3(1024), 0, st, a);
     return hipGetLastError();
   }
   return with_row_shape<U>(a.d.dim, [&](auto shape) {
     typedef decltype(shape) S;
     const long grid = S::WPR == 1 ? ((long)a.d.rows + 3) / 4 : a.d.rows;
     if (const hipError_t s = check_grid(grid, 256); s != hipSuccess) return s;
-    hipLaunchKernelGGL((k_i8_quantise<X, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    const auto kernel = far ? k_i8_quantise<X, U, S::WPR, S::NV, S::TAIL, true>
+                            : k_i8_quantise<X, U, S::WPR, S::NV, S::TAIL, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a);
     return hipGetLastError();
   });
 }
@@ -71,8 +75,14 @@ hipError_t i8_quantise(const I8RowsArgs& a, hipStream_t st) {
 template <typename X> static hipError_t dequantise(const I8RowsArgs& a, hipStream_t st) {
   constexpr int U = sizeof(X) == 2 ? 8 : 4;
   const bool tail = a.d.dim % U != 0, wide = a.d.dim > 2048;
-  const auto kernel = wide ? (tail ? k_i8_dequantise<X, U, 4, true> : k_i8_dequantise<X, U, 4, false>)
-                           : (tail ? k_i8_dequantise<X, U, 1, true> : k_i8_dequantise<X, U, 1, false>);
+  const bool far = past_caches((double)a.d.rows * a.d.dim * (sizeof(X) + 1));
+  auto pick = [&](auto t, auto f) {
+    constexpr bool T = decltype(t)::value, F = decltype(f)::value;
+    return wide ? k_i8_dequantise<X, U, 4, T, F> : k_i8_dequantise<X, U, 1, T, F>;
+  };
+  typedef std::true_type Y;
+  typedef std::false_type N;
+  const auto kernel = tail ? (far ? pick(Y{}, Y{}) : pick(Y{}, N{})) : (far ? pick(N{}, Y{}) : pick(N{}, N{}));
   const long grid = wide ? a.d.rows : ((long)a.d.rows + 3) / 4;
   if (const hipError_t s = check_grid(grid, 256); s != hipSuccess) return s;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a);

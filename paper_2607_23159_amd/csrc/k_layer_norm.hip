@@ -15,7 +15,7 @@ namespace cs {
 // One row to a wave or workgroup, its gains and biases asked for with it: 65,520 x 1536, fp32 to
 // bf16, takes 103 us, 5.9 TB/s (110 with them asked for after the sums, from the first cache).  A loop
 // over rows with the gains in registers and the next row on its way keeps fewer rows in flight: 120.
-template <typename X, typename Y, int U, int WPR, int NV, bool TAIL>
+template <typename X, typename Y, int U, int WPR, int NV, bool TAIL, bool FAR>
 __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
   __shared__ float lds[2][4];
   __shared__ uint32_t lds_max[4];
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = U * (64 * WPR * i + t);
-    raw[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
+    raw[i] = load_chunk<X, U, TAIL, FAR>(x + c, dim - c);
   }
   const int group = (int)((uint32_t)row / (uint32_t)a.d.rows);   // rows in all are below 2^30
   const float* w = a.weight ? a.weight + group * a.d.w_group : nullptr;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
       const int c = U * (64 * WPR * i + t);
       float y[U];
       result(i, y);
-      store_chunk<Y, U, TAIL>((Y*)a.y + row * a.d.y_row + c, dim - c, y);
+      store_chunk<Y, U, TAIL, FAR>((Y*)a.y + row * a.d.y_row + c, dim - c, y);
     }
   }
 }
@@ -105,7 +105,10 @@ static hipError_t forward(const LayerNormArgs& a, hipStream_t st) {
     typedef decltype(shape) S;
     const long grid = S::WPR == 1 ? (total + 3) / 4 : total;
     if (const hipError_t s = check_grid(grid, 256); s != hipSuccess) return s;
-    hipLaunchKernelGGL((k_layer_norm_op<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    const bool far = past_caches((double)total * a.d.dim * (sizeof(X) + sizeof(Y)));
+    const auto kernel = far ? k_layer_norm_op<X, Y, U, S::WPR, S::NV, S::TAIL, true>
+                            : k_layer_norm_op<X, Y, U, S::WPR, S::NV, S::TAIL, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a);
     return hipGetLastError();
   });
 }
@@ -140,7 +143,7 @@ size_t layer_norm_backward_workspace(const cs_layer_norm_grad_desc& d) {
   return (size_t)d.groups * ln_parts(d.rows) * 2 * round_up(d.dim, 4) * sizeof(float);
 }
 
-template <typename X, typename Y, int U, int WPR, int NV, bool TAIL>
+template <typename X, typename Y, int U, int WPR, int NV, bool TAIL, bool FAR>
 __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, int parts, int part_rows) {
   constexpr int STEP = WPR == 1 ? 4 : 1;               // rows of the workgroup's waves
   __shared__ float2 lds[2][4];
@@ -176,8 +179,8 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = U * (64 * WPR * i + t);
-      o.x[i] = load_chunk<X, U, TAIL>(x + c, dim - c);
-      o.dy[i] = load_chunk<Y, U, TAIL>(dy + c, dim - c);
+      o.x[i] = load_chunk<X, U, TAIL, FAR>(x + c, dim - c);
+      o.dy[i] = load_chunk<Y, U, TAIL, FAR>(dy + c, dim - c);
     }
     o.mean = a.mean[row];
     o.rstd = a.rstd[row];
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
         const float n = (to_f(cur.x[i][e]) - cur.mean) * cur.rstd;
         o[e] = cur.rstd * (fmaf(to_f(cur.dy[i][e]), gain[i][e], -m1) - n * m2);
       }
-      store_chunk<X, U, TAIL>(dx + c, dim - c, o);
+      store_chunk<X, U, TAIL, FAR>(dx + c, dim - c, o);
     }
   }
   if (!a.part) return;
@@ -289,8 +292,10 @@ static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
     constexpr int U = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
     const hipError_t s = with_row_shape<U>(a.d.dim, [&](auto shape) {
       typedef decltype(shape) S;
-      hipLaunchKernelGGL((k_layer_norm_grad<X, Y, U, S::WPR, S::NV, S::TAIL>), dim3((unsigned)blocks), dim3(256),
-                         0, st, a, parts, part_rows);
+      const bool far = past_caches((double)a.d.groups * a.d.rows * a.d.dim * (2 * sizeof(X) + sizeof(Y)));
+      const auto kernel = far ? k_layer_norm_grad<X, Y, U, S::WPR, S::NV, S::TAIL, true>
+                              : k_layer_norm_grad<X, Y, U, S::WPR, S::NV, S::TAIL, false>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, parts, part_rows);
       return hipGetLastError();
     });
     if (s != hipSuccess) return s;

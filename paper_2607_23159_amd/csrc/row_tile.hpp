@@ -49,11 +49,18 @@ template <int U, class F> static hipError_t with_row_shape(int dim, F f) {
   return hipErrorInvalidValue;
 }
 
-template <typename T, int U, bool TAIL>
+// Calls of more than one and a half times the last cache (256 MB) pass it by, both ways: their rows
+// are gone before they are wanted again.  (8 x 32,760 x 1536, norm from fp32 to bf16: 411 -> 390 us;
+// 32,760 x 5120 from 8 bits 85 -> 72.  32,760 x 1536 in bf16, 200 MB, would go from 33 to 39.)
+inline bool past_caches(double bytes) { return bytes > 384e6; }
+
+template <typename T, int U, bool TAIL, bool NT = false>
 CS_DEV typename Chunk<T, U>::vec load_chunk(const T* __restrict__ p, int left) {
   typename Chunk<T, U>::vec v = {};
   if (left >= U) {
-    v = *reinterpret_cast<const typename Chunk<T, U>::vec*>(p);
+    const auto* q = reinterpret_cast<const typename Chunk<T, U>::vec*>(p);
+    if constexpr (NT) v = __builtin_nontemporal_load(q);
+    else v = *q;
   } else if constexpr (TAIL) {
 #pragma unroll
     for (int e = 0; e < U - 1; ++e)
@@ -63,12 +70,14 @@ CS_DEV typename Chunk<T, U>::vec load_chunk(const T* __restrict__ p, int left) {
 }
 
 // y: U values, rounded to T.
-template <typename T, int U, bool TAIL> CS_DEV void store_chunk(T* __restrict__ p, int left, const float* y) {
+template <typename T, int U, bool TAIL, bool NT = false>
+CS_DEV void store_chunk(T* __restrict__ p, int left, const float* y) {
   typename Chunk<T, U>::vec v;
 #pragma unroll
   for (int e = 0; e < U; ++e) v[e] = to_t<T>(y[e]);
   if (left >= U) {
-    *reinterpret_cast<typename Chunk<T, U>::vec*>(p) = v;
+    if (NT) __builtin_nontemporal_store(v, reinterpret_cast<typename Chunk<T, U>::vec*>(p));
+    else *reinterpret_cast<typename Chunk<T, U>::vec*>(p) = v;
   } else if constexpr (TAIL) {
 #pragma unroll
     for (int e = 0; e < U - 1; ++e)

@@ -168,6 +168,41 @@ def test_rows_past_32_bits():
     assert torch.equal(q.cpu(), codes) and torch.equal(s.cpu(), scales)
 
 
+@pytest.mark.parametrize("dim", [1536, 2051])
+def test_large_calls_are_those_of_their_parts(dim):
+    """Calls of more than 384 MB read and write past the caches: bitwise the same, forward, in 8 bits and
+    back, and backward."""
+    groups, rows = 6, 8000
+    total = groups * rows
+    x, _ = padded(total, dim, FP, 0.0)
+    x.copy_(torch.randn(total, dim, generator=torch.Generator("cuda").manual_seed(1), device="cuda"))
+    w, b = put(rnd(2, groups, dim), FP), put(rnd(3, groups, dim), FP)
+    y, check_y = padded(total, dim, FP, -77.0, extra=1)
+    mean, rstd = torch.empty(total, device="cuda"), torch.empty(total, device="cuda")
+    B.cs_layer_norm(B.layer_norm_desc(x, y, w, b, groups=groups), x, y, w, b, mean=mean, rstd=rstd)
+    q, check_q = padded(total, dim, I8, 55)
+    s = torch.empty(total, device="cuda")
+    B.cs_i8_quantise(B.i8_rows_desc(x, q, s), x, q, s)
+    back, check_back = padded(total, dim, FP, -77.0)
+    B.cs_i8_dequantise(B.i8_rows_desc(back, q, s), q, s, back)
+    t = run_grad(x, y, w, mean, rstd, groups, True)
+    for g in (0, 2, 5):
+        r = slice(g * rows, (g + 1) * rows)
+        one, wg, bg = padded(rows, dim, FP, 0.0)[0], w[g:g + 1], b[g:g + 1]
+        m, d = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        B.cs_layer_norm(B.layer_norm_desc(x[r], one, wg, bg), x[r], one, wg, bg, mean=m, rstd=d)
+        assert torch.equal(one, y[r]) and torch.equal(m, mean[r]) and torch.equal(d, rstd[r])
+        q1, s1 = padded(rows, dim, I8, 0)[0], torch.empty(rows, device="cuda")
+        B.cs_i8_quantise(B.i8_rows_desc(x[r], q1, s1), x[r], q1, s1)
+        assert torch.equal(q1, q[r]) and torch.equal(s1, s[r])
+        B.cs_i8_dequantise(B.i8_rows_desc(one, q1, s1), q1, s1, one)
+        assert torch.equal(one, back[r])
+        p = run_grad(x[r], y[r], wg, m, d, 1, True)
+        assert torch.equal(p["x"], t["x"][r]) and torch.equal(p["w"][0], t["w"][g]) and torch.equal(p["b"][0], t["b"][g])
+    for check in (check_y, check_q, check_back):
+        check()
+
+
 # ---------------------------------------------------------------------- backward
 def grad_case(groups, rows, dim, xt, dyt, unit, with_w=True, seed=0):
     x, w, _ = data(groups, rows, dim, xt, "w" if with_w else "", seed)
