@@ -144,6 +144,9 @@ template <> struct Mfma16<int8_t> {
 // Batched launches (blockIdx.y = item): the same A against n weight matrices
 // w_stride elements apart, with an epilogue that moves to item z (Epi::item).
 template <class Epi> struct EpiBatched : std::false_type {};
+// Launches whose items (blockIdx.y) are parts of K (8-bit k_gemm_ring): Epi::per slices each, the sums
+// as they are to item z's place (Epi::item).
+template <class Epi> struct EpiSplitsK : std::false_type {};
 
 // Tile order: the launch is split into 8 contiguous ranges, one per XCD
 // (workgroups are dealt round-robin to the 8 dies).  Inside a range, tiles are
@@ -487,7 +490,15 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
   for (int i = 0; i < B_INST; ++i) b_off[i] = (wave * B_INST + i) * 1024 + lane * 16;
   // An odd slice count leaves half a step at the end: the last slice is loaded
   // twice (the wait counts stay uniform) and multiplied once.
-  const int nslice = K / BK, nstep = (nslice + SL - 1) / SL;
+  int nslice = K / BK;
+  if constexpr (EpiSplitsK<Epi>::value) {
+    const int first = blockIdx.y * epi.per;
+    nslice = min(epi.per, nslice - first);
+    a_base += (long)first * BK;
+    b_base += (long)first * W_BLOCK_ROWS * BK;
+    epi.item(blockIdx.y, first * BK);
+  }
+  const int nstep = (nslice + SL - 1) / SL;
   auto issue = [&](int step, int st) {
 #pragma unroll
     for (int l = 0; l < SL; ++l) {
@@ -579,7 +590,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_ring(const T* __re
   }
   if (k < nstep) step(k, f[0], f[1]);
 
-  if constexpr (I8) {
+  if constexpr (EpiSplitsK<Epi>::value) {
+    epi.store(acc, m0 + wm * WM, n0 + wn * WN, lane, M, N);
+  } else if constexpr (I8) {
     f32x4 out[TM][TN];
     epi.scaled(acc, out, m0 + wm * WM, n0 + wn * WN, lane, M, N);
     gemm_epilogue16_deep<2>(out, m0 + wm * WM, n0 + wn * WN, lane, M, N, epi.to);
@@ -891,6 +904,26 @@ template <class To> struct EpiI8 {
     }
   }
 };
+
+// Sums of a part of K: [part][M][ld] 32-bit integers.
+struct EpiSums {
+  int* part; long ld, stride; int per, a_row;
+  CS_DEV void item(int z, int k0) {
+    part += z * stride;
+    a_row -= k0;
+  }
+  template <int TM, int TN>
+  CS_DEV void store(const i32x4 (&acc)[TM][TN], int row_base, int col_base, int lane, int M, int N) const {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int row = row_base + 16 * i + (lane & 15), col0 = col_base + 16 * j + 4 * (lane >> 4);
+        if (row < M && col0 < N) *reinterpret_cast<i32x4*>(part + (long)row * ld + col0) = acc[i][j];
+      }
+  }
+};
+template <> struct EpiSplitsK<EpiSums> : std::true_type {};
 
 // The product by itself: T [M][N] of any N, rows on 16 bytes.
 template <typename T, int ACT> struct EpiMatmul {

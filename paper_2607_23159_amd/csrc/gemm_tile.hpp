@@ -67,8 +67,8 @@ static constexpr TileCost TILE_COST_I8[N_TILES] = {
 
 // The loop is unrolled so that every division is by a constant (0.07 us a launch
 // instead of 0.12).
-template <const TileCost (&COST)[N_TILES]>
-static Bf16Tile cheapest_tile(long M, long N, double nk, long batch, bool residual) {
+template <const TileCost (&COST)[N_TILES], int FIRST = 0>
+static Bf16Tile cheapest_tile(long M, long N, double nk, long batch, bool residual, double* time = nullptr) {
   auto cost = [&](int i) {
     const TileCost& c = COST[i];
     const long tiles = (M + c.bm - 1) / c.bm * ((N + c.bn - 1) / c.bn) * batch, round = 256L * c.slots;
@@ -77,13 +77,14 @@ static Bf16Tile cheapest_tile(long M, long N, double nk, long batch, bool residu
     if (r > 0) t += nk * (c.lone + (c.full - c.lone) * r) + epi * 0.5 * (1.0 + r);
     return t;
   };
-  int best = 0;
-  double best_t = cost(0);
+  int best = FIRST;
+  double best_t = cost(FIRST);
 #pragma clang loop unroll(full)
-  for (int i = 1; i < N_TILES; ++i) {
+  for (int i = FIRST + 1; i < N_TILES; ++i) {
     const double t = cost(i);
     if (t < best_t) { best = i; best_t = t; }
   }
+  if (time) *time = best_t;
   return (Bf16Tile)best;
 }
 
@@ -93,6 +94,43 @@ static Bf16Tile choose_tile(long M, long N, long K, long batch, bool residual) {
 
 static inline Bf16Tile choose_tile_i8(long M, long N, long K, bool residual) {
   return cheapest_tile<TILE_COST_I8>(M, N, (double)((K + 127) / 128), 1, residual);
+}
+
+// Up to 16 rows of up to FEW_COLS outputs are k_matmul_few's.  1 x 1536 x 8960: 6.0 us against
+// 11.0 with the best tile, 16 rows 8.3 against 11.2; 16 x 1536 x 1536 4.0 against 4.3.  Past them one
+// row is as fast either way (1 x 13,824 x 5120: 16.1 us both, weights from HBM), and for more the
+// rows, which every workgroup reads past LDS, cost more than the tiles' latency (16 x 13,824 x 5120
+// 21.3 against 16.5).
+constexpr int FEW_ROWS = 16, FEW_COLS = 4096;
+
+// Parts of K for 8-bit products: their sums in one launch, joined by a second.  For few rows and a long
+// K, where one launch of small tiles is a chain of slices on a part of the chip.  64 x 5120 x 13,824
+// takes 20.5 us in 3 parts against 29.1, 32 x 512 x 8960 7.0 in 6 against 11.2, 400 x 1536 x 8960
+// 18.4 in 3 against 21.6.  The parts' time is that of as many tiles with their share of K, 2.5 us and the
+// sums at 8 bytes each and way: over 99 measured shapes (8 to 700 rows, k 1536 to 13,824) the choice costs
+// 1.9% against the best, and is 12% faster than one launch where it takes parts.
+// A tenth has to be had: the second launch is the host's time too.
+struct SplitK { int parts, per; Bf16Tile tile; };   // per: slices of a part
+
+static inline SplitK split_k_i8(long M, long N, long K) {
+  const long nk = (K + 127) / 128;
+  SplitK best = {1, (int)nk, RING_32x32};
+  if (nk < 48 || M > 1024 || (M <= FEW_ROWS && N <= FEW_COLS)) return best;
+  double least;
+  cheapest_tile<TILE_COST_I8>(M, N, (double)nk, 1, false, &least);
+  least *= 0.9;
+  static constexpr int TRIES[] = {2, 3, 4, 6};
+  for (int s : TRIES) {
+    const long per = (nk + s - 1) / s, parts = (nk + per - 1) / per;
+    double t;
+    const Bf16Tile tile = cheapest_tile<TILE_COST_I8, RING_64x128>(M, N, (double)per, parts, false, &t);
+    t += 2.5 + (double)(parts * M * N) * 1e-6;
+    if (t < least) {
+      least = t;
+      best = {(int)parts, (int)per, tile};
+    }
+  }
+  return best;
 }
 
 }  // namespace cs

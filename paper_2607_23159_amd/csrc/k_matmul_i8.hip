@@ -15,13 +15,6 @@ namespace cs {
 
 constexpr int GROUP_M = 4;
 
-// Up to 16 rows of up to FEW_COLS outputs are k_matmul_few's.  1 x 1536 x 8960: 6.0 us against
-// 11.0 with the best tile, 16 rows 8.3 against 11.2; 16 x 1536 x 1536 4.0 against 4.3.  Past them one
-// row is as fast either way (1 x 13,824 x 5120: 16.1 us both, weights from HBM), and for more the
-// rows, which every workgroup reads past LDS, cost more than the tiles' latency (16 x 13,824 x 5120
-// 21.3 against 16.5).
-constexpr int FEW_ROWS = 16, FEW_COLS = 4096;
-
 // Few rows: the weights are all there is to read, once, so they go straight from memory to the
 // operand registers.  A workgroup has 16 columns; its 8 waves take the K slices in turn, 4 each in
 // flight, and add their sums up in LDS.  Rows past M repeat the last one, and bytes past the end of a
@@ -88,9 +81,9 @@ static void launch_w4(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t
 }
 
 template <int BM, int BN, int WGM, int WGN, int SL, int STAGES, int OCC, class Epi>
-static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st) {
+static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st, int parts = 1) {
   const unsigned tiles = (unsigned)((long)cdiv(a.d.rows, BM) * cdiv(a.d.n, BN));
-  hipLaunchKernelGGL((k_gemm_ring<int8_t, BM, BN, WGM, WGN, SL, STAGES, OCC, GROUP_M, Epi>), dim3(tiles),
+  hipLaunchKernelGGL((k_gemm_ring<int8_t, BM, BN, WGM, WGN, SL, STAGES, OCC, GROUP_M, Epi>), dim3(tiles, (unsigned)parts),
                      dim3(64 * WGM * WGN), 0, st, a.a, a.d.a_row, a.w.codes, a.d.rows, a.d.n, kp, 0L, epi);
 }
 
@@ -121,14 +114,59 @@ template <class To> static hipError_t product(const MatmulI8Args& a, const To& t
   return hipGetLastError();
 }
 
-size_t matmul_i8_workspace(const cs_matmul_i8_desc&) { return 0; }
+// ------------------------------------------------------------- parts of K
+// The parts' sums, scaled: four columns a thread.
+template <class To>
+__global__ __launch_bounds__(256) void k_matmul_join(const int* __restrict__ part, long ld, long stride, int parts, int M,
+                                                     int N, EpiI8<To> epi) {
+  const int cols = (N + 3) / 4, q = blockIdx.x * 256 + threadIdx.x, row = q / cols, col0 = 4 * (q - row * cols);
+  if (row >= M) return;
+  const int* p = part + (long)row * ld + col0;
+  i32x4 v = *reinterpret_cast<const i32x4*>(p);
+#pragma unroll 4
+  for (int i = 1; i < parts; ++i) v += *reinterpret_cast<const i32x4*>(p + i * stride);
+  const float sa = epi.scale_a[row];
+  const f32x4 sw = epi.four(epi.scale_w, col0, N), b = epi.bias ? epi.four(epi.bias, col0, N) : f32x4{0.f, 0.f, 0.f, 0.f};
+  float y[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) y[r] = i8_value(v[r], sa, sw[r], b[r]);
+  epi.to(row, col0, y, epi.to.pre(row, col0));
+}
 
-hipError_t matmul_i8(const MatmulI8Args& a, void*, hipStream_t st) {
+static size_t part_bytes(const cs_matmul_i8_desc& d) { return (size_t)d.rows * round_up(d.n, 4) * sizeof(int); }
+
+size_t matmul_i8_workspace(const cs_matmul_i8_desc& d) {
+  const int parts = split_k_i8(d.rows, d.n, d.k).parts;
+  return parts > 1 ? parts * part_bytes(d) : 0;
+}
+
+template <class To> static hipError_t product_of_parts(const MatmulI8Args& a, const To& to, int* part, hipStream_t st) {
+  const SplitK s = split_k_i8(a.d.rows, a.d.n, a.d.k);
+  if (s.parts == 1) return product(a, to, st);
+  const long ld = round_up(a.d.n, 4), stride = a.d.rows * ld;
+  const int kp = (int)round_up(a.d.k, 128), a_row = (int)round_up(a.d.k, 16);
+  const EpiSums sums = {part, ld, stride, s.per, a_row};
+  switch (s.tile) {
+    case RING_64x128: launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, sums, st, s.parts); break;
+    case RING_64x64: launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, sums, st, s.parts); break;
+    case RING_32x64: launch_ring<32, 64, 1, 4, 2, 3, 2>(a, kp, sums, st, s.parts); break;
+    default: launch_ring<32, 32, 2, 2, 2, 4, 2>(a, kp, sums, st, s.parts);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const EpiI8<To> epi = {a.a_scale, a.w.scales, a.bias, a_row, to};
+  hipLaunchKernelGGL(k_matmul_join<To>, dim3((unsigned)cdiv(a.d.rows * (ld / 4), 256)), dim3(256), 0, st, part, ld, stride,
+                     s.parts, a.d.rows, a.d.n, epi);
+  return hipGetLastError();
+}
+
+hipError_t matmul_i8(const MatmulI8Args& a, void* work, hipStream_t st) {
+  int* part = (int*)work;
   if (a.d.out_dtype == CS_BF16)
-    return a.d.act == CS_ACT_GELU ? product(a, EpiMatmul<bf16, 1>{(bf16*)a.out, a.d.o_row, a.d.n}, st)
-                                  : product(a, EpiMatmul<bf16, 0>{(bf16*)a.out, a.d.o_row, a.d.n}, st);
-  return a.d.act == CS_ACT_GELU ? product(a, EpiMatmul<float, 1>{(float*)a.out, a.d.o_row, a.d.n}, st)
-                                : product(a, EpiMatmul<float, 0>{(float*)a.out, a.d.o_row, a.d.n}, st);
+    return a.d.act == CS_ACT_GELU ? product_of_parts(a, EpiMatmul<bf16, 1>{(bf16*)a.out, a.d.o_row, a.d.n}, part, st)
+                                  : product_of_parts(a, EpiMatmul<bf16, 0>{(bf16*)a.out, a.d.o_row, a.d.n}, part, st);
+  return a.d.act == CS_ACT_GELU ? product_of_parts(a, EpiMatmul<float, 1>{(float*)a.out, a.d.o_row, a.d.n}, part, st)
+                                : product_of_parts(a, EpiMatmul<float, 0>{(float*)a.out, a.d.o_row, a.d.n}, part, st);
 }
 
 // ------------------------------------------------- the transformer's projections

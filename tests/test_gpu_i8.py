@@ -130,6 +130,8 @@ MM = [  # rows, n, k
     (128, 128, 4096), (129, 255, 1030), (200, 700, 333), (257, 513, 256), (300, 96, 8960), (511, 2049, 70),
     (891, 512, 256), (1, 300, 13824), (5, 260, 65536), (1030, 1540, 200), (2100, 300, 390), (64, 5000, 140),
     (4200, 1100, 80), (16, 4096, 70), (16, 4097, 70), (17, 4096, 70), (9, 4000, 1100),
+    # in parts of K
+    (17, 512, 8960), (33, 70, 9000), (64, 300, 13824), (100, 515, 6300), (300, 513, 8961), (16, 4100, 16000), (40, 33, 65536),
 ]
 
 
@@ -160,7 +162,7 @@ def test_weights_from_values(n, k, dtype):
 
 
 def test_product_does_not_depend_on_the_batch_or_the_kernel():
-    for n, k in ((70, 200), (1536, 512), (640, 5120)):
+    for n, k in ((70, 200), (1536, 512), (640, 5120), (130, 9000)):
         w, _, _ = weight_of(n, k)
         bias = rnd(1, n).cuda()
         a, s = rows_of(1300, k, seed=4)
@@ -251,3 +253,34 @@ def test_products_on_two_streams_at_once():
             B.cs_matmul_i8(d, a, s, w, o, work=k, stream=st)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+# Shapes that the choices give each of the tiles (test_i8_tile_choice.py), whole and in parts of K, odd in
+# every direction.
+TILES = {"W4_256x256": (7000, 4330, 930), "W4_224x256": (6265, 1818, 924), "W4_192x256": (1305, 8018, 553),
+         "W4_160x256": (4104, 2273, 417), "W4_128x128": (1740, 3589, 132), "W4_64x64": (3013, 65, 100),
+         "RING_128x128": (7184, 417, 514), "RING_64x128": (4499, 200, 1821), "RING_64x64": (38, 8454, 1236),
+         "RING_32x64": (17, 3325, 101), "RING_32x32": (17, 17, 103)}
+PARTS = {"RING_64x128": (38, 5330, 12175), "RING_64x64": (33, 1581, 8752), "RING_32x64": (33, 2156, 6061),
+         "RING_32x32": (17, 17, 6395)}
+
+
+@pytest.mark.parametrize("m,n,k", [*TILES.values(), *PARTS.values()])
+def test_product_in_every_tile(m, n, k):
+    """The integer sums are exact; what is made of them rounds twice on the way and once at the end."""
+    g = torch.Generator("cuda").manual_seed(m)
+    a, wq = padded(m, k, I8, 0)[0], padded(n, k, I8, 0)[0]
+    for t in (a, wq):
+        t.copy_(torch.randint(-128, 128, t.shape, generator=g, device="cuda", dtype=torch.int32))
+    s, ws = torch.rand(m, generator=g, device="cuda") / 64, torch.rand(n, generator=g, device="cuda") / 64
+    bias = torch.randn(n, generator=g, device="cuda")
+    w = B.I8Weight(n, k)
+    B.cs_i8_weight_pack(w, wq, ws)
+    p = (a.double() @ wq.double().t().contiguous()) * s.double()[:, None] * ws.double()
+    ref = p + bias.double()
+    off = 2 * R.U * p.abs() + R.U * ref.abs()
+    del p
+    for t in (FP, BF):
+        o = product(a, s, w, t, bias)
+        bad = (o.double() - ref).abs() > 1.01 * off + R.HALF[t] * (ref.abs() + off) + 1e-37
+        assert not bad.any(), (t, int(bad.sum()), [int(x[0]) for x in bad.nonzero(as_tuple=True)])
