@@ -284,3 +284,43 @@ def test_product_in_every_tile(m, n, k):
         o = product(a, s, w, t, bias)
         bad = (o.double() - ref).abs() > 1.01 * off + R.HALF[t] * (ref.abs() + off) + 1e-37
         assert not bad.any(), (t, int(bad.sum()), [int(x[0]) for x in bad.nonzero(as_tuple=True)])
+
+
+@pytest.mark.parametrize("m,n,k,stride", [(600, 130, 200, 1 << 22), (3013, 65, 100, 1 << 21), (33, 70, 9000, 1 << 22)])
+def test_rows_past_32_bits(m, n, k, stride):
+    """Rows of codes and outputs that lie past 2^31 bytes and elements of the first (600, 3,013 rows)."""
+    w, wq, ws = weight_of(n, k)
+    whole = torch.empty((m - 1) * stride + 4096 * 4, dtype=I8, device="cuda")
+    a = torch.as_strided(whole, (m, k), (stride, 1))
+    q, s = rows_of(m, k)
+    a.copy_(q)
+    out = torch.empty((m - 1) * stride + 4096, dtype=BF, device="cuda")
+    o = torch.as_strided(out, (m, n), (stride, 1))
+    d = B.matmul_i8_desc(a, s, w, o)
+    work = torch.empty(max(1, B.cs_matmul_i8_workspace(d)), dtype=torch.uint8, device="cuda")
+    B.cs_matmul_i8(d, a, s, w, o, work=work)
+    assert torch.equal(o, product(q, s, w, BF))
+
+
+def test_graphs_that_share_a_workspace_of_parts():
+    w1, _, _ = weight_of(300, 9000)
+    w2, _, _ = weight_of(500, 13824)
+    runs, work = [], None
+    for w, m in ((w1, 40), (w2, 64)):
+        a, s = rows_of(m, w.c.k, seed=m)
+        o = torch.empty(m, (w.c.n + 7) // 8 * 8, dtype=BF, device="cuda")[:, :w.c.n]
+        d = B.matmul_i8_desc(a, s, w, o)
+        assert B.cs_matmul_i8_workspace(d) > 0
+        work = torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda") if work is None else work
+        B.cs_matmul_i8(d, a, s, w, o, work=work)
+        want = o.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.cs_matmul_i8(d, a, s, w, o, work=work)
+        runs.append((graph, o, want, a, s))     # what a graph reads has to live as long
+    for order in ((0, 1), (1, 0), (0, 0)):
+        for i in order:
+            runs[i][1].fill_(9.0)
+            runs[i][0].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(runs[i][1], runs[i][2]) for i in order)

@@ -345,3 +345,60 @@ def test_norms_in_a_graph_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, t) for a, t in zip(want, (y, dx, dw, db)))
+
+
+@pytest.mark.parametrize("groups,rows,dim", [(1, 40, 130), (3, 33, 1536), (2, 19, 5120)])
+def test_forward_then_backward_is_the_gradient(groups, rows, dim):
+    """The kept statistics lead to the gradient that float64's own differentiation gives."""
+    x, w, b = data(groups, rows, dim, FP, "wb", seed=70)
+    dy = put(rnd(77, groups * rows, dim), FP)
+    y, mean, rstd = padded(groups * rows, dim, FP, 0.0)[0], *(torch.empty(groups * rows, device="cuda") for _ in range(2))
+    B.cs_layer_norm(B.layer_norm_desc(x, y, w, b, groups=groups, unit_offset=True), x, y, w, b, mean=mean, rstd=rstd)
+    t = run_grad(x, dy, w, mean, rstd, groups, True)
+    leaves = [v.double().cpu().requires_grad_() for v in (x, w, b)]
+    out = torch.nn.functional.layer_norm(leaves[0], (dim,), eps=1e-6).reshape(groups, rows, dim)
+    out = out * (1.0 + leaves[1])[:, None] + leaves[2][:, None]
+    out.backward(dy.double().cpu().reshape(out.shape))
+    # what the kernel is off by for its statistics, and what they are off by themselves: m rstd and rel of
+    # layer_norm's bound, through n and the factor rstd
+    (_, off), (_, w_off), (_, b_off) = R.layer_norm_grad(x, dy, w, mean, rstd, groups, True)
+    m, rel = R.layer_norm(x, w, b, groups, True, 1e-6)[3::2]
+    r = rstd.double().cpu()
+    stat = (m * r + 2 * rel)[:, None]                       # of n, relative to 1 + |n|
+    n = (x.double().cpu() - mean.double().cpu()[:, None]) * r[:, None]
+    g = dy.double().cpu() * (1.0 + w.double().cpu().repeat_interleave(rows, 0))
+    more = r[:, None] * stat * 4 * ((1 + n.abs()) * (g * n).abs().mean(-1, keepdim=True) + g.abs().mean(-1, keepdim=True) + g.abs() +
+                                    n.abs() * (g.abs() * (1 + n.abs())).mean(-1, keepdim=True))
+    grad = [v.grad for v in leaves]
+    within(t["x"], grad[0], off + more + R.HALF[FP] * grad[0].abs(), "dx")
+    w_more = (dy.double().cpu().abs() * stat * (1 + n.abs())).reshape(groups, rows, dim).sum(1)
+    within(t["w"], grad[1], w_off + 1.01 * w_more, "dw")
+    within(t["b"], grad[2], b_off, "db")
+
+
+def test_two_graphs_that_share_a_workspace():
+    """One after the other, in either order: a workspace carries nothing over."""
+    runs = []
+    work = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    for groups, rows, dim in ((2, 70, 640), (1, 300, 1000)):
+        x, dy, w, mean, rstd = grad_case(groups, rows, dim, BF, BF, False, seed=dim)
+        dw, db = torch.empty(groups, dim, device="cuda"), torch.empty(groups, dim, device="cuda")
+        d = B.layer_norm_grad_desc(x, dy, w, None, dw, db, groups=groups)
+        assert B.cs_layer_norm_backward_workspace(d) <= work.numel()
+
+        def call(d=d, x=x, dy=dy, w=w, mean=mean, rstd=rstd, dw=dw, db=db):
+            B.cs_layer_norm_backward(d, x, dy, w, mean, rstd, None, dw, db, work=work)
+        call()
+        want = dw.clone(), db.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        runs.append((graph, (dw, db), want, call))     # what a graph reads has to live as long
+    for order in ((0, 1), (1, 0), (0, 0), (1, 1)):
+        for i in order:
+            for t in runs[i][1]:
+                t.fill_(9.0)
+            runs[i][0].replay()
+        torch.cuda.synchronize()
+        for i in order:
+            assert all(torch.equal(a, b) for a, b in zip(runs[i][1], runs[i][2]))
