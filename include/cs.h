@@ -469,7 +469,7 @@ typedef struct {
  *   dx = rstd (g - mean(g) - n mean(g n)),
  *   dweight = sum of dy n and dbias = sum of dy over the rows of each group, fp32
  * [groups][dim] (one group: over all rows).  mean, rstd: as cs_layer_norm wrote them.  dx,
- * dweight and dbias may be NULL; the workspace is needed for the last two only.  A group of no
+ * dweight and dbias may be NULL; the workspace (of 0 bytes for few rows) is needed for the last two only.  A group of no
  * rows gets zeros there.  dx may be x or dy (same pointer, type and stride).  The sums over rows are taken in an order that
  * depends on rows and dim alone: a group's gradients are bitwise the same alone and among
  * others. */

@@ -134,12 +134,15 @@ hipError_t layer_norm(const LayerNormArgs& a, hipStream_t st) {
 int ln_part_rows(int rows) {
   // About 512 parts of a long group, so that one alone fills the card, 16 rows at least: what is
   // written and read of the sums, 16 bytes a channel and part, stays a tenth of the rows' bytes.  Rows
-  // of the group alone decide, so that its gradients do not depend on other groups.
+  // of the group alone decide, so that its gradients do not depend on other groups.  Up to 32 rows are
+  // one part, whose sums are the gradient: the second launch costs more than 16 rows do.
+  if (rows <= 32) return 32;
   return (int)std::max<long>(16, (cdiv(rows, 512) + 3) / 4 * 4);
 }
 static int ln_parts(int rows) { return cdiv(rows, ln_part_rows(rows)); }
 
 size_t layer_norm_backward_workspace(const cs_layer_norm_grad_desc& d) {
+  if (ln_parts(d.rows) == 1) return 0;
   return (size_t)d.groups * ln_parts(d.rows) * 2 * round_up(d.dim, 4) * sizeof(float);
 }
 
@@ -223,14 +226,19 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
       store_chunk<X, U, TAIL, FAR>(dx + c, dim - c, o);
     }
   }
-  if (!a.part) return;
+  if (!a.dweight && !a.dbias) return;
   const long ld = (dim + 3) & ~3;
-  float* out = a.part + ((long)group * parts + part) * 2 * ld;
+  float* sum[2] = {a.dweight + group * a.d.dw_group, a.dbias + group * a.d.db_group};
+  if (parts > 1) {
+    sum[0] = a.part + ((long)group * parts + part) * 2 * ld;
+    sum[1] = sum[0] + ld;
+  }
+  const bool wanted[2] = {parts > 1 || a.dweight, parts > 1 || a.dbias};
+  // whole chunks to the workspace, whose rows are padded to 4
+  const int end = parts > 1 ? (int)ld : dim;
   auto store = [&](float* p, int c, const float* v) {
 #pragma unroll
-    for (int h = 0; h < U / 4; ++h)
-      if (c + 4 * h < dim)   // whole chunks: the workspace's rows are padded to 4
-        *reinterpret_cast<f32x4*>(p + c + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+    for (int h = 0; h < U / 4; ++h) store_chunk<float, 4, TAIL>(p + c + 4 * h, end - c - 4 * h, v + 4 * h);
   };
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -249,11 +257,12 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
           const int q = 64 * (U * i + e) + lane;
           v[e] = ((sums[0][q] + sums[1][q]) + sums[2][q]) + sums[3][q];
         }
-        store(out + k * ld, U * (64 * i + lane), v);
+        if (wanted[k]) store(sum[k], U * (64 * i + lane), v);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) store(out + k * ld, U * (64 * WPR * i + t), k ? db[i] : dw[i]);
+      for (int i = 0; i < NV; ++i)
+        if (wanted[k]) store(sum[k], U * (64 * WPR * i + t), k ? db[i] : dw[i]);
     }
   }
 }
@@ -300,7 +309,7 @@ static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
     });
     if (s != hipSuccess) return s;
   }
-  if (!a.dweight && !a.dbias) return hipSuccess;
+  if (parts == 1 || (!a.dweight && !a.dbias)) return hipSuccess;
   hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)sums, 2), dim3(1024), 0, st, a,
                      parts);
   return hipGetLastError();

@@ -49,7 +49,7 @@ struct LayerNormGradArgs {
   const float *weight, *mean, *rstd;
   void* dx;                      // may be NULL
   float *dweight, *dbias;        // may be NULL
-  float* part;                   // layer_norm_backward_workspace bytes, or NULL without dweight and dbias
+  float* part;                   // layer_norm_backward_workspace bytes
   cs_layer_norm_grad_desc d;
 };
 size_t layer_norm_backward_workspace(const cs_layer_norm_grad_desc& d);

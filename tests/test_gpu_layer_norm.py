@@ -230,7 +230,7 @@ def run_grad(x, dy, w, mean, rstd, groups, unit, want="xwb", stream=None):
     return t
 
 
-GRADS = SHAPES + [(1, 16, 100), (1, 17, 100), (2, 600, 40), (1, 8300, 24), (5, 33, 1536), (2, 40, 5120)]
+GRADS = SHAPES + [(1, 16, 100), (1, 32, 101), (2, 32, 5121), (1, 33, 100), (4, 33, 2050), (2, 32, 1536), (2, 600, 40), (1, 8300, 24), (5, 33, 1536), (2, 40, 5120)]
 
 
 @pytest.mark.parametrize("xt,dyt", TYPES)

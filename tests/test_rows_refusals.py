@@ -89,12 +89,14 @@ def test_norm_grad_pointers_workspace_and_nothing_to_do():
     fn, n = B.lib().cs_layer_norm_backward_workspace, C.c_size_t(77)
     assert fn(C.byref(grad_desc()), None) == B.CS_E_INVAL
     assert fn(C.byref(grad_desc(dim=0)), C.byref(n)) == B.CS_E_INVAL and n.value == 77
-    for kw in (dict(), dict(rows=1), dict(groups=1, rows=100000, dim=16384)):
+    for kw in (dict(rows=33), dict(rows=300), dict(groups=1, rows=100000, dim=16384)):
         assert fn(C.byref(grad_desc(**kw)), C.byref(n)) == B.CS_OK and 0 < n.value < 1 << 31
-    assert fn(C.byref(grad_desc()), C.byref(n)) == B.CS_OK
+    for rows in (0, 1, 32):
+        assert fn(C.byref(grad_desc(rows=rows)), C.byref(n)) == B.CS_OK and n.value == 0
+    assert fn(C.byref(grad_desc(rows=70)), C.byref(n)) == B.CS_OK
     for kw in (dict(work=None), dict(work=P + 8), dict(nbytes=n.value - 1)):
         for only in (dict(), dict(dx=None, dw=None), dict(db=None)):
-            refused(grad(grad_desc(), **kw, **only), "INVAL", "workspace")
+            refused(grad(grad_desc(rows=70), **kw, **only), "INVAL", "workspace")
     assert grad(grad_desc(), dx=None, dw=None, db=None, work=None, nbytes=0) == B.CS_OK
     assert grad(grad_desc(groups=0), x=None, dy=None, work=None) == B.CS_OK
     # the part of a group does not depend on how many groups there are
