@@ -129,7 +129,7 @@ hipError_t layer_norm(const LayerNormArgs& a, hipStream_t st) {
 // A workgroup takes ln_part_rows of a group's rows, with the gains and its lanes' sums dw and db in
 // registers and the next row on its way while one is reduced; its sums go to the workspace,
 // [group][part][2][dim], and a second launch adds a group's parts up in order.  12,480 x 1536 with fp32
-// x and bf16 dy take 32 us (6.0 TB/s) and 4.4 for the parts, 32,760 x 5120 in bf16 192 (5.2
+// x and bf16 dy take 33 us (5.8 TB/s) and 4.2 for the parts, 32,760 x 5120 in bf16 197 (5.1
 // TB/s) and 5.0.
 int ln_part_rows(int rows) {
   // About 512 parts of a long group, so that one alone fills the card, 16 rows at least: what is

@@ -188,15 +188,15 @@ CS_DEV uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
 // c scale leaves says whether it is the quotient's.  Values of 24 bits lie next to a halfway value once
 // in a few hundred chunks: the largest remainder is kept, and where it reaches half a scale in
 // a wave the codes are made again, one by one.  Values of 8 bits (COARSE) do in most rows (half the
-// largest magnitude is one): there a step up or down follows from the remainder, and only exact
-// halves are left for the second way.  With all of code()'s steps for every value the vector unit was
+// largest magnitude is one): there a step up or down follows from the remainder.  Exact halves are
+// left for the second way: an odd number of half scales that has 8 significant bits is there only if
+// the scale has no more.  With all of code()'s steps for every value the vector unit was
 // the bound: 32,760 x 8960 in bf16 took 215 us.
 template <int U, int NV, int WPR, bool TAIL, bool COARSE, class F>
 CS_DEV void store_codes(const I8Scale& s, int8_t* __restrict__ p, int dim, int t, F value) {
   constexpr float MAGIC = 12582912.0f;
   uint32_t w[NV][U / 4];
   float worst = 0.0f;
-  bool tie = false;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     // a chunk after the other: widened all at once, bf16 values take twice the registers
@@ -210,8 +210,8 @@ CS_DEV void store_codes(const I8Scale& s, int8_t* __restrict__ p, int dim, int t
         const float left = fmaf(MAGIC - f, s.unit, x);
         b[e] = __float_as_uint(f);
         if constexpr (COARSE) {
-          b[e] += fabsf(left) > s.half ? (uint32_t)(((int)__float_as_uint(left) >> 31) | 1) : 0u;
-          tie |= fabsf(left) == s.half;
+          b[e] += left > s.half ? 1u : 0u;
+          b[e] -= left < -s.half ? 1u : 0u;
         } else {
           worst = fmaxf(worst, fabsf(left));
         }
@@ -219,7 +219,7 @@ CS_DEV void store_codes(const I8Scale& s, int8_t* __restrict__ p, int dim, int t
       w[i][h] = pack_bytes(b[0], b[1], b[2], b[3]);
     }
   }
-  if (!s.plain() || __any(COARSE ? tie : worst >= s.half)) {
+  if (!s.plain() || (COARSE ? (__float_as_uint(s.scale) & 0xFFFFu) == 0 : __any(worst >= s.half))) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       __builtin_amdgcn_sched_barrier(0);
