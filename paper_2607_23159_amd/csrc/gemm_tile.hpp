@@ -115,7 +115,7 @@ struct SplitK { int parts, per; Bf16Tile tile; };   // per: slices of a part
 static inline SplitK split_k_i8(long M, long N, long K) {
   const long nk = (K + 127) / 128;
   SplitK best = {1, (int)nk, RING_32x32};
-  if (nk < 48 || M > 1024 || (M <= FEW_ROWS && N <= FEW_COLS)) return best;
+  if (nk < 48 || M > 1024 || N > 65536 || (M <= FEW_ROWS && N <= FEW_COLS)) return best;
   double least;
   cheapest_tile<TILE_COST_I8>(M, N, (double)nk, 1, false, &least);
   least *= 0.9;

@@ -1,5 +1,7 @@
 """The transformer with its projections in 8 bits (cs_model_init_proj) against the float64 oracle, as it is
 and with its projections' weights and inputs rounded to 8 bits."""
+import dataclasses
+
 import numpy as np
 import pytest
 
@@ -10,7 +12,7 @@ from oracle import dit as odit
 from paper_2607_23159_amd import binding as B
 from paper_2607_23159_amd import synth
 from paper_2607_23159_amd.search import GpuModel, run_rollout
-from parity import rel_l2
+from parity import rel_l2, token_errors
 
 PROJECTIONS = ("qkv_w", "o_w", "caq_w", "cao_w", "ffn1_w", "ffn2_w")
 
@@ -72,6 +74,42 @@ def test_velocity(name, norm, monkeypatch):
     for i in range(n if n > 1 else 0):
         assert np.array_equal(run(gm, x[i:i + 1], 0.6, ctx)[0], v[i])
     gm.close()
+
+
+def test_few_tokens():
+    """Latents of four tokens: the few-row product under every epilogue of the transformer."""
+    m = dataclasses.replace(synth.MODELS["tiny"], lat_f=1, lat_h=4, lat_w=4, dtype=synth.DTYPE_BF16)
+    flat = synth.make_weights(m, init="stress")
+    W = {k: v.astype(np.float64) for k, v in synth.unflatten(m, flat).items()}
+    gm = GpuModel(m, flat, proj=B.CS_PROJ_8BIT)
+    ctx = synth.make_context(m, 33)
+    x = synth.make_noise(m, 5, seed0=920)
+    v = run(gm, x, 0.7, ctx)
+    emb = odit.text_embedding(ctx, W)
+    for i in range(5):       # five latents take other kernels than one
+        assert np.array_equal(run(gm, x[i:i + 1], 0.7, ctx)[0], v[i])
+        assert rel_l2(v[i], odit.velocity(x[i], 0.7, emb, W, m)) < FAR
+    gm.close()
+
+
+@pytest.mark.parametrize("name,frames", [("wan13b", 5), ("wan14b", 2)])
+def test_many_tokens(name, frames):
+    """The large tiles under every epilogue (v transposed, gated residual, GELU): a latent alone, whose products
+    take other tiles, is bitwise what it is among others, and the compute type's result is near."""
+    m = dataclasses.replace(synth.MODELS[name], n_blocks=1, lat_f=frames, dtype=synth.DTYPE_BF16)
+    flat = synth.make_weights(m, init="stress")
+    ctx = synth.make_context(m, 34)
+    x = synth.make_noise(m, 3, seed0=930)
+    gm = GpuModel(m, flat, proj=B.CS_PROJ_8BIT)
+    v = run(gm, x, 0.4, ctx)
+    for i in (0, 2):
+        assert np.array_equal(run(gm, x[i:i + 1], 0.4, ctx)[0], v[i])
+    gm.close()
+    native = GpuModel(m, flat)
+    ref = run(native, x, 0.4, ctx)
+    native.close()
+    for i in range(3):
+        assert rel_l2(v[i], ref[i]) < FAR and token_errors(v[i], ref[i]).max() < 2 * FAR
 
 
 def test_prompts_and_one_text_agree():
