@@ -105,10 +105,10 @@ constexpr int FEW_ROWS = 16, FEW_COLS = 4096;
 
 // Parts of K for 8-bit products: their sums in one launch, joined by a second.  For few rows and a long
 // K, where one launch of small tiles is a chain of slices on a part of the chip.  64 x 5120 x 13,824
-// takes 20.5 us in 3 parts against 29.1, 32 x 512 x 8960 7.0 in 6 against 11.2, 400 x 1536 x 8960
-// 18.4 in 3 against 21.6.  The parts' time is that of as many tiles with their share of K, 2.5 us and the
+// takes 20.5 us in 3 parts against 29.1, 32 x 512 x 8960 7.0 in 6 against 11.2, 128 x 5120 x
+// 13,824 25.9 in 3 against 34.6.  The parts' time is that of as many tiles with their share of K, 2.5 us and the
 // sums at 8 bytes each and way: over 99 measured shapes (8 to 700 rows, k 1536 to 13,824) the choice costs
-// 1.9% against the best, and is 12% faster than one launch where it takes parts.
+// 2.3% against the best; the 21 shapes that it cuts are 21% faster than in one launch (0.9% slower at worst).
 // A tenth has to be had: the second launch is the host's time too.
 struct SplitK { int parts, per; Bf16Tile tile; };   // per: slices of a part
 

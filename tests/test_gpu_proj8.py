@@ -95,7 +95,8 @@ def test_few_tokens():
 @pytest.mark.parametrize("name,frames", [("wan13b", 5), ("wan14b", 2)])
 def test_many_tokens(name, frames):
     """The large tiles under every epilogue (v transposed, gated residual, GELU): a latent alone, whose products
-    take other tiles, is bitwise what it is among others, and the compute type's result is near."""
+    take other tiles, is bitwise what it is among others, and the compute type's result is near.  A token's
+    error is held against the tokens' mean norm: twice the bound, as a token is up to twice that norm."""
     m = dataclasses.replace(synth.MODELS[name], n_blocks=1, lat_f=frames, dtype=synth.DTYPE_BF16)
     flat = synth.make_weights(m, init="stress")
     ctx = synth.make_context(m, 34)
