@@ -35,7 +35,10 @@ class GpuModel:
             raise ValueError(f"weight array has {weights.size} values, model needs {n}")
         w = _dev(weights)
         self.stream = stream
-        self.h = B.cs_model_init_proj(self.desc, qk_norm, proj, w, n, stream)
+        if proj == B.CS_PROJ_NATIVE:
+            self.h = B.cs_model_init_norm(self.desc, qk_norm, w, n, stream)
+        else:
+            self.h = B.cs_model_init_proj(self.desc, qk_norm, proj, w, n, stream)
         del w
         torch.cuda.synchronize()
 
