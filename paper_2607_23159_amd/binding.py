@@ -250,17 +250,24 @@ def cs_model_init(desc: cs_model_desc, weights, n_weights: int, stream=None) -> 
     return cs_model_init_norm(desc, CS_QK_NORM_FULL, weights, n_weights, stream)
 
 
+def _opened(model, desc: cs_model_desc) -> int:
+    _model_D[model.value] = desc.in_ch * desc.lat_f * desc.lat_h * desc.lat_w
+    _model_text[model.value] = (desc.text_len, desc.text_dim)
+    return model.value
+
+
 def cs_model_init_norm(desc: cs_model_desc, qk_norm: int, weights, n_weights: int, stream=None) -> int:
-    return cs_model_init_proj(desc, qk_norm, CS_PROJ_NATIVE, weights, n_weights, stream)
+    out = C.c_void_p()
+    _check(lib().cs_model_init_norm(C.byref(desc), int(qk_norm), _ptr(weights, n_weights, name="weights"), n_weights,
+                                    _stream(stream), C.byref(out)))
+    return _opened(out, desc)
 
 
 def cs_model_init_proj(desc: cs_model_desc, qk_norm: int, proj: int, weights, n_weights: int, stream=None) -> int:
     out = C.c_void_p()
     _check(lib().cs_model_init_proj(C.byref(desc), int(qk_norm), int(proj), _ptr(weights, n_weights, name="weights"),
                                     n_weights, _stream(stream), C.byref(out)))
-    _model_D[out.value] = desc.in_ch * desc.lat_f * desc.lat_h * desc.lat_w
-    _model_text[out.value] = (desc.text_len, desc.text_dim)
-    return out.value
+    return _opened(out, desc)
 
 
 def cs_model_free(model: int) -> None:
