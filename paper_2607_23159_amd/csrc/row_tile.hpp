@@ -41,7 +41,10 @@ template <int U, class F> static hipError_t with_row_shape(int dim, F f) {
     }
   }
   const int nv = (dim / U + 255) / 256;
-  CS_SHAPE(4, 2) CS_SHAPE(4, 3) CS_SHAPE(4, 4) CS_SHAPE(4, 5) CS_SHAPE(4, 6) CS_SHAPE(4, 8)
+  if constexpr (U == 8) {
+    CS_SHAPE(4, 2)
+  }
+  CS_SHAPE(4, 3) CS_SHAPE(4, 4) CS_SHAPE(4, 5) CS_SHAPE(4, 6) CS_SHAPE(4, 8)
   if constexpr (U == 4) {
     CS_SHAPE(4, 12) CS_SHAPE(4, 16)
   }

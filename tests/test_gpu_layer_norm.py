@@ -63,7 +63,7 @@ def data(groups, rows, dim, xt, params, seed=0, mean=0.5):
 SHAPES = [  # groups, rows, dim: lanes, chunks and waves that are partly or just filled
     (1, 1, 1), (1, 3, 2), (2, 5, 7), (1, 1, 64), (3, 4, 100), (1, 2, 256), (1, 9, 511), (2, 3, 512), (1, 5, 513),
     (1, 6, 1536), (3, 297, 256), (1, 4, 2047), (1, 7, 2048), (2, 3, 2049), (1, 3, 5120), (1, 2, 8192), (2, 2, 8200),
-    (1, 2, 13824), (1, 3, 16383), (1, 1, 16384),
+    (2, 2, 8960), (2, 1, 12287), (2, 2, 12288), (1, 2, 13824), (1, 3, 16383), (1, 1, 16384),
 ]
 TYPES = [(BF, BF), (BF, FP), (FP, BF), (FP, FP)]
 
