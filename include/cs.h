@@ -453,7 +453,8 @@ typedef struct {
  * rstd: fp32 [groups * rows], written for the backward pass, or NULL.  y_scale: the rows' scales
  * where y_dtype is CS_I8 (else not read).  y may be x (same pointer, type and stride).  NaN: a row that is
  * not finite or whose values add up to 3.4e38 or more, and with eps 0 one without variance.  groups *
- * rows is below 2^30. */
+ * rows is below 2^30, and a call fits a launch of fewer than 2^32 work items (else CS_E_UNSUPPORTED): below
+ * 2^24 rows, 2^26 up to 2048 channels. */
 cs_status cs_layer_norm(const cs_layer_norm_desc* desc, const void* x, const float* weight, const float* bias, void* y,
                         float* y_scale, float* mean, float* rstd, void* stream);
 
@@ -472,7 +473,9 @@ typedef struct {
  * dweight and dbias may be NULL; the workspace (of 0 bytes for few rows) is needed for the last two only.  A group of no
  * rows gets zeros there.  dx may be x or dy (same pointer, type and stride).  The sums over rows are taken in an order that
  * depends on rows and dim alone: a group's gradients are bitwise the same alone and among
- * others. */
+ * others.  A launch takes fewer than 2^24 parts of groups (of 16 rows and more; up to 32 rows are one), and
+ * where groups of more parts, or of no rows, are summed, groups * ceil(dim / 64) is below 2^22; else
+ * CS_E_UNSUPPORTED. */
 cs_status cs_layer_norm_backward_workspace(const cs_layer_norm_grad_desc* desc, size_t* bytes);
 cs_status cs_layer_norm_backward(const cs_layer_norm_grad_desc* desc, const void* x, const void* dy,
                                  const float* weight, const float* mean, const float* rstd, void* dx, float* dweight,
@@ -483,7 +486,8 @@ cs_status cs_layer_norm_backward(const cs_layer_norm_grad_desc* desc, const void
  * largest magnitude / 127, rounded to fp32; its codes are the integers nearest to value / scale
  * (of the exact quotients, halfway ones to the even code), within -127..127; it stands for
  * code * scale.  A row of zeros, or whose scale underflows to 0, has scale 0 and codes 0; one that holds an
- * infinity or a NaN has scale NaN and codes 0.  cs_layer_norm writes the same of its results. */
+ * infinity or a NaN has scale NaN and codes 0.  cs_layer_norm writes the same of its results.  Rows are
+ * below 2^24 (2^26 up to 2048 channels, to codes 2^22 beyond 16384; else CS_E_UNSUPPORTED). */
 typedef struct {
   int32_t dtype, rows, dim;
   int64_t x_row, q_row;

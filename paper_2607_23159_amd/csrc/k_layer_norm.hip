@@ -305,8 +305,9 @@ template <typename X, typename Y>
 static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
   const int parts = ln_parts(a.d.rows), part_rows = ln_part_rows(a.d.rows);
   const long blocks = (long)a.d.groups * parts, sums = (long)a.d.groups * cdiv(a.d.dim, 64);
+  const bool join = parts != 1 && (a.dweight || a.dbias);   // parts 0: no rows, whose sums are zeros
   if (const hipError_t s = check_grid(blocks, 256); s != hipSuccess) return s;
-  if (const hipError_t s = check_grid(sums, 1024); s != hipSuccess) return s;
+  if (const hipError_t s = join ? check_grid(sums, 1024) : hipSuccess; s != hipSuccess) return s;
   if (a.d.rows > 0) {
     constexpr int U = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
     const hipError_t s = with_row_shape<U>(a.d.dim, [&](auto shape) {
@@ -319,7 +320,7 @@ static hipError_t backward(const LayerNormGradArgs& a, hipStream_t st) {
     });
     if (s != hipSuccess) return s;
   }
-  if (parts == 1 || (!a.dweight && !a.dbias)) return hipSuccess;
+  if (!join) return hipSuccess;
   hipLaunchKernelGGL(k_layer_norm_grad_sum, dim3((unsigned)sums, 2), dim3(1024), 0, st, a,
                      parts);
   return hipGetLastError();
