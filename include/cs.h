@@ -522,7 +522,8 @@ typedef struct {
  * an exact 32-bit integer (codes may be -128 too); it is scaled in fp32, by the row's scale first,
  * and rounded once to the output's type.  bias: fp32 [n] or NULL.  Rows of a are read in whole
  * 16-byte units: what lies between k and the next multiple of 16 may hold anything.  out must
- * not overlap the inputs.  cs_matmul_i8_workspace gives the bytes of `work` (0: work may be NULL). */
+ * not overlap the inputs.  ceil(rows / 256) * ceil(n / 256) is below 2^24 (else CS_E_UNSUPPORTED).
+ * cs_matmul_i8_workspace gives the bytes of `work` (0: work may be NULL). */
 cs_status cs_matmul_i8_workspace(const cs_matmul_i8_desc* desc, size_t* bytes);
 cs_status cs_matmul_i8(const cs_matmul_i8_desc* desc, const int8_t* a, const float* a_scales,
                        const cs_i8_weight* weight, const float* bias, void* out, void* work, size_t work_bytes,

@@ -74,44 +74,52 @@ template <class To> static void launch_few(const MatmulI8Args& a, int kp, const 
 }
 
 template <int BM, int BN, int OCC, int PD, class Epi>
-static void launch_w4(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st) {
-  const unsigned tiles = (unsigned)((long)cdiv(a.d.rows, BM) * cdiv(a.d.n, BN));
-  hipLaunchKernelGGL((k_gemm_w4<int8_t, BM, BN, OCC, GROUP_M, PD, Epi>), dim3(tiles), dim3(256), 0, st, a.a, a.d.a_row,
-                     a.w.codes, a.d.rows, a.d.n, kp, 0L, epi);
+static hipError_t launch_w4(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st) {
+  const long tiles = (long)cdiv(a.d.rows, BM) * cdiv(a.d.n, BN);
+  if (const hipError_t s = check_grid(tiles, 256); s != hipSuccess) return s;
+  hipLaunchKernelGGL((k_gemm_w4<int8_t, BM, BN, OCC, GROUP_M, PD, Epi>), dim3((unsigned)tiles), dim3(256), 0, st, a.a,
+                     a.d.a_row, a.w.codes, a.d.rows, a.d.n, kp, 0L, epi);
+  return hipGetLastError();
 }
 
 template <int BM, int BN, int WGM, int WGN, int SL, int STAGES, int OCC, class Epi>
-static void launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st, int parts = 1) {
-  const unsigned tiles = (unsigned)((long)cdiv(a.d.rows, BM) * cdiv(a.d.n, BN));
-  hipLaunchKernelGGL((k_gemm_ring<int8_t, BM, BN, WGM, WGN, SL, STAGES, OCC, GROUP_M, Epi>), dim3(tiles, (unsigned)parts),
-                     dim3(64 * WGM * WGN), 0, st, a.a, a.d.a_row, a.w.codes, a.d.rows, a.d.n, kp, 0L, epi);
+static hipError_t launch_ring(const MatmulI8Args& a, int kp, const Epi& epi, hipStream_t st, int parts = 1) {
+  constexpr int THREADS = 64 * WGM * WGN;
+  const long tiles = (long)cdiv(a.d.rows, BM) * cdiv(a.d.n, BN);
+  if (const hipError_t s = check_grid(tiles * parts, THREADS); s != hipSuccess) return s;
+  hipLaunchKernelGGL((k_gemm_ring<int8_t, BM, BN, WGM, WGN, SL, STAGES, OCC, GROUP_M, Epi>),
+                     dim3((unsigned)tiles, (unsigned)parts), dim3(THREADS), 0, st, a.a, a.d.a_row, a.w.codes, a.d.rows, a.d.n,
+                     kp, 0L, epi);
+  return hipGetLastError();
 }
 
 template <class To> static hipError_t product(const MatmulI8Args& a, const To& to, hipStream_t st) {
   const EpiI8<To> epi = {a.a_scale, a.w.scales, a.bias, (int)round_up(a.d.k, 16), to};
   const int kp = (int)round_up(a.d.k, 128);
-  // the most workgroups: tiles of 32 x 32 of 4 waves, or an eighth as many of 64 x 128 of 8
-  if (const hipError_t s = check_grid((long)cdiv(a.d.rows, 32) * cdiv(a.d.n, 32), 256); s != hipSuccess) return s;
   constexpr bool RES = EpiIsResidual<To>::value;
   constexpr int PD = RES ? 8 : 2, PD2 = RES ? 4 : 2;   // as in bf16
   if (a.d.rows <= FEW_ROWS && a.d.n <= FEW_COLS) {
     launch_few(a, kp, epi, st);
     return hipGetLastError();
   }
-  switch (choose_tile_i8(a.d.rows, a.d.n, a.d.k, RES)) {
-    case W4_256x256: launch_w4<256, 256, 1, PD>(a, kp, epi, st); break;
-    case W4_224x256: launch_w4<224, 256, 1, PD>(a, kp, epi, st); break;
-    case W4_192x256: launch_w4<192, 256, 1, PD>(a, kp, epi, st); break;
-    case W4_160x256: launch_w4<160, 256, 1, PD>(a, kp, epi, st); break;
-    case W4_128x128: launch_w4<128, 128, 2, PD2>(a, kp, epi, st); break;
-    case W4_64x64: launch_w4<64, 64, 3, 2>(a, kp, epi, st); break;
-    case RING_128x128: launch_ring<128, 128, 2, 4, 1, 4, 2>(a, kp, epi, st); break;
-    case RING_64x128: launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, epi, st); break;
-    case RING_64x64: launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, epi, st); break;
-    case RING_32x64: launch_ring<32, 64, 1, 4, 2, 3, 2>(a, kp, epi, st); break;
-    default: launch_ring<32, 32, 2, 2, 2, 4, 2>(a, kp, epi, st);
-  }
-  return hipGetLastError();
+  auto launch = [&](Bf16Tile tile) {
+    switch (tile) {
+      case W4_256x256: return launch_w4<256, 256, 1, PD>(a, kp, epi, st);
+      case W4_224x256: return launch_w4<224, 256, 1, PD>(a, kp, epi, st);
+      case W4_192x256: return launch_w4<192, 256, 1, PD>(a, kp, epi, st);
+      case W4_160x256: return launch_w4<160, 256, 1, PD>(a, kp, epi, st);
+      case W4_128x128: return launch_w4<128, 128, 2, PD2>(a, kp, epi, st);
+      case W4_64x64: return launch_w4<64, 64, 3, 2>(a, kp, epi, st);
+      case RING_128x128: return launch_ring<128, 128, 2, 4, 1, 4, 2>(a, kp, epi, st);
+      case RING_64x128: return launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, epi, st);
+      case RING_64x64: return launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, epi, st);
+      case RING_32x64: return launch_ring<32, 64, 1, 4, 2, 3, 2>(a, kp, epi, st);
+      default: return launch_ring<32, 32, 2, 2, 2, 4, 2>(a, kp, epi, st);
+    }
+  };
+  const hipError_t s = launch(choose_tile_i8(a.d.rows, a.d.n, a.d.k, RES));
+  // more tiles than a launch has: the largest are the fewest
+  return s == hipErrorInvalidConfiguration ? launch(W4_256x256) : s;
 }
 
 // ------------------------------------------------------------- parts of K
@@ -146,13 +154,15 @@ template <class To> static hipError_t product_of_parts(const MatmulI8Args& a, co
   const long ld = round_up(a.d.n, 4), stride = a.d.rows * ld;
   const int kp = (int)round_up(a.d.k, 128), a_row = (int)round_up(a.d.k, 16);
   const EpiSums sums = {part, ld, stride, s.per, a_row};
-  switch (s.tile) {
-    case RING_64x128: launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, sums, st, s.parts); break;
-    case RING_64x64: launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, sums, st, s.parts); break;
-    case RING_32x64: launch_ring<32, 64, 1, 4, 2, 3, 2>(a, kp, sums, st, s.parts); break;
-    default: launch_ring<32, 32, 2, 2, 2, 4, 2>(a, kp, sums, st, s.parts);
-  }
-  const hipError_t e = hipGetLastError();
+  auto launch = [&] {
+    switch (s.tile) {
+      case RING_64x128: return launch_ring<64, 128, 2, 4, 2, 3, 2>(a, kp, sums, st, s.parts);
+      case RING_64x64: return launch_ring<64, 64, 2, 4, 2, 4, 2>(a, kp, sums, st, s.parts);
+      case RING_32x64: return launch_ring<32, 64, 1, 4, 2, 3, 2>(a, kp, sums, st, s.parts);
+      default: return launch_ring<32, 32, 2, 2, 2, 4, 2>(a, kp, sums, st, s.parts);
+    }
+  };
+  const hipError_t e = launch();
   if (e != hipSuccess) return e;
   const EpiI8<To> epi = {a.a_scale, a.w.scales, a.bias, a_row, to};
   hipLaunchKernelGGL(k_matmul_join<To>, dim3((unsigned)cdiv(a.d.rows * (ld / 4), 256)), dim3(256), 0, st, part, ld, stride,

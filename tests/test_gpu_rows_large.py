@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 
 import rows_ref as R
 from paper_2607_23159_amd import binding as B
-from test_gpu_layer_norm import BF, FP, padded, run_grad, within
+from test_gpu_layer_norm import BF, FP, I8, padded, run_grad, within
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -62,3 +62,28 @@ def test_gradient_of_the_rows_alone():
     for g in (0, 3000001, groups - 1):
         dx, off = ref(g)[0]
         within(t["x"][g * rows:(g + 1) * rows], dx, off + R.HALF[BF] * (dx.abs() + off), "dx")
+
+
+# ------------------------------------------------------------------------- products
+@pytest.mark.parametrize("m,n,k", [(59 * 32760, 8960, 64), (1 << 30, 7, 16)])
+def test_products_of_more_outputs_than_small_tiles_cover(m, n, k):
+    """Sizes whose 32 x 32 tiles (in the second case those that the costs ask for too) pass a launch's 2^32 work items,
+    in larger tiles; slices are bitwise what they are alone."""
+    assert -(-m // 32) * -(-n // 32) * 256 >= 1 << 32
+    w = B.I8Weight(n, k)
+    wq = padded(n, k, I8, 0)[0]
+    wq.copy_(torch.randint(-128, 128, (n, k), device="cuda", dtype=torch.int32))
+    B.cs_i8_weight_pack(w, wq, torch.rand(n, device="cuda") / 64)
+    a = torch.empty(m, k, dtype=I8, device="cuda").random_(-128, 128, generator=torch.Generator("cuda").manual_seed(2))
+    s = torch.rand(m, device="cuda") / 64
+    o = torch.full((m, (n + 7) // 8 * 8), -77.0, dtype=BF, device="cuda")
+    out = o[:, :n]
+    d = B.matmul_i8_desc(a, s, w, out)
+    assert B.cs_matmul_i8_workspace(d) == 0
+    B.cs_matmul_i8(d, a, s, w, out)
+    for first, rows in ((0, 300), (m // 2 // 4 * 4, 513), (m - 256 - m % 4, 256 + m % 4)):
+        r = slice(first, first + rows)
+        part = padded(rows, n, BF, 0.0)[0]
+        B.cs_matmul_i8(B.matmul_i8_desc(a[r], s[r], w, part), a[r], s[r], w, part)
+        assert torch.equal(part, out[r]), first
+    assert (o[:, n:] == -77.0).all() and not (out[::1021] == -77.0).any()
