@@ -466,7 +466,7 @@ typedef struct {
   int64_t x_row, dy_row, dx_row, w_group, dw_group, db_group;
 } cs_layer_norm_grad_desc;
 
-/* With n = (x - mean) rstd and g = dy gain, sums in fp32:
+/* With n = (x - mean) rstd and g = dy gain, sums in fp32 (over rows, of up to 256 rows; those in 64 bits):
  *   dx = rstd (g - mean(g) - n mean(g n)),
  *   dweight = sum of dy n and dbias = sum of dy over the rows of each group, fp32
  * [groups][dim] (one group: over all rows).  mean, rstd: as cs_layer_norm wrote them.  dx,

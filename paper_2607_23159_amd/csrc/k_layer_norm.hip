@@ -144,9 +144,11 @@ int ln_part_rows(int rows) {
   // About 512 parts of a long group, so that one alone fills the card, 16 rows at least: what is
   // written and read of the sums, 16 bytes a channel and part, stays a tenth of the rows' bytes.  Rows
   // of the group alone decide, so that its gradients do not depend on other groups.  Up to 32 rows are
-  // one part, whose sums are the gradient: the second launch costs more than 16 rows do.
+  // one part, whose sums are the gradient: the second launch costs more than 16 rows do.  256 rows at most:
+  // a part's sums are fp32, so that more would lose digits (at 8 M rows, in parts of 16,384, 1024 half
+  // steps of a sum of equal values); past 131,072 rows there are more parts instead.
   if (rows <= 32) return 32;
-  return (int)std::max<long>(16, (cdiv(rows, 512) + 3) / 4 * 4);
+  return std::clamp((cdiv(rows, 512) + 3) / 4 * 4, 16, 256);
 }
 static int ln_parts(int rows) { return cdiv(rows, ln_part_rows(rows)); }
 
@@ -276,8 +278,8 @@ __global__ __launch_bounds__(256) void k_layer_norm_grad(LayerNormGradArgs a, in
   }
 }
 
-// The parts' sums, a channel a lane and a sixteenth of the parts a wave, in 64 bits: up to 512
-// numbers that partly cancel, and the launch waits for memory anyway.  With four waves, a load
+// The parts' sums, a channel a lane and a sixteenth of the parts a wave, in 64 bits: 512 or
+// more numbers that partly cancel, and the launch waits for memory anyway.  With four waves, a load
 // behind the other, 512 parts of 5120 channels took 33 us.
 __global__ __launch_bounds__(1024) void k_layer_norm_grad_sum(LayerNormGradArgs a, int parts) {
   __shared__ double sums[16][64];

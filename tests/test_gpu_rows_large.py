@@ -64,6 +64,36 @@ def test_gradient_of_the_rows_alone():
         within(t["x"][g * rows:(g + 1) * rows], dx, off + R.HALF[BF] * (dx.abs() + off), "dx")
 
 
+# ------------------------------------------------------------------------ long groups
+def test_gradients_of_a_long_group():
+    """The bound of the sums over rows, 316 half steps of fp32, holds at any length.  Every row adds the same value, 1 +
+    1023 steps, which a sum between 2048 and 4096 takes as 1: 4096 rows in one fp32 sum would lose 1023 steps in half of
+    them, 1024 half steps of the sum."""
+    rows, dim, value = 1 << 23, 8, 1.0 + 1023 * 2.0 ** -23
+    x, dy = (torch.full((rows, dim), v, device="cuda") for v in (1.0, value))
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")     # so that n is 1
+    t = run_grad(x, dy, None, mean, rstd, 1, False, want="wb")
+    bound = 1.01 * (300 + 16) * R.U * rows * value
+    for k in "wb":
+        within(t[k], torch.full((1, dim), rows * value, dtype=torch.float64), bound, k)
+
+
+@pytest.mark.parametrize("rows,dim", [(131073, 24), (200001, 2056)])
+def test_backward_of_groups_past_131072_rows(rows, dim):
+    """As the shorter groups, against float64 (on the GPU, in slices)."""
+    x, dy, _, mean, rstd, _ = many_groups(1, rows, dim, seed=20)
+    t = run_grad(x, dy, None, mean, rstd, 1, False, want="wb")
+    sums = torch.zeros(4, dim, dtype=torch.float64, device="cuda")
+    for r in range(0, rows, 20000):
+        p = slice(r, r + 20000)
+        d = dy[p].double()
+        dn = d * (x[p].double() - mean[p].double()[:, None]) * rstd[p].double()[:, None]
+        sums += torch.stack([dn.sum(0), dn.abs().sum(0), d.sum(0), d.abs().sum(0)])
+    dw, dw_abs, db, db_abs = sums.cpu()[:, None]
+    within(t["w"], dw, 1.01 * (316 + 4) * R.U * dw_abs, "dw")
+    within(t["b"], db, 1.01 * 316 * R.U * db_abs, "db")
+
+
 # ------------------------------------------------------------------------- products
 @pytest.mark.parametrize("m,n,k", [(59 * 32760, 8960, 64), (1 << 30, 7, 16)])
 def test_products_of_more_outputs_than_small_tiles_cover(m, n, k):
