@@ -17,7 +17,8 @@ namespace cs {
 // over rows with the gains in registers and the next row on its way keeps fewer rows in flight: 120.
 // Rows of 48 values a lane and more take theirs after the sums: registers for them would leave one or two
 // waves a SIMD.  16,000 x 13,824: fp32 to fp32 364 -> 306 us, to codes 366 -> 235, bf16 to bf16 187 -> 169;
-// 16,000 x 13,825 in bf16 298 -> 214, but fp32 to codes 598 -> 650.
+// 16,000 x 13,825 in bf16 298 -> 214.  fp32 rows to codes at lengths that end inside a chunk keep a wave a SIMD
+// either way and ask early: 627 us against 660.
 template <typename X, typename Y, int U, int WPR, int NV, bool TAIL, bool FAR>
 __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
   __shared__ float lds[2][4];
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_op(LayerNormArgs a) {
       if (b) bv[i][h] = load_chunk<float, 4, TAIL>(b + c, dim - c);
     }
   };
-  constexpr bool LATE = U * NV >= 48;
+  constexpr bool LATE = U * NV >= 48 && !(TAIL && sizeof(X) == 4 && std::is_same<Y, int8_t>::value);
   if constexpr (!LATE) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) params(i);
