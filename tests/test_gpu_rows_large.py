@@ -117,3 +117,75 @@ def test_products_of_more_outputs_than_small_tiles_cover(m, n, k):
         B.cs_matmul_i8(B.matmul_i8_desc(a[r], s[r], w, part), a[r], s[r], w, part)
         assert torch.equal(part, out[r]), first
     assert (o[:, n:] == -77.0).all() and not (out[::1021] == -77.0).any()
+
+
+# ------------------------------------------------------------- accesses past the caches
+PAST = 384e6      # bytes of a call from which on it reads and writes past the caches
+
+
+def streamed(rows, dim, *tensors):
+    assert sum(rows * dim * t.element_size() for t in tensors) > PAST, "the call would stay in the caches"
+
+
+def same(a, b):
+    return torch.equal(a.nan_to_num(7.5e8) if a.is_floating_point() else a, b.nan_to_num(7.5e8) if b.is_floating_point() else b)
+
+
+@pytest.mark.parametrize("xt", [BF, FP])
+@pytest.mark.parametrize("rows,dim", [(96000, 1536), (72000, 2051), (8000, 17000)])
+def test_rows_in_8_bits_past_the_caches(rows, dim, xt):
+    """To codes and back, in one call and in calls that stay in the caches: bitwise the same."""
+    rows *= 1 if xt == FP or dim == 17000 else 2
+    x, _ = padded(rows, dim, xt, 0.0)
+    for r in range(0, rows, 16000):
+        n = min(16000, rows - r)
+        x[r:r + n] = device_randn(r, n, dim, dtype=xt)
+    x[3], x[rows - 2, dim - 1], x[rows // 2, 0] = 0.0, float("nan"), float("inf")
+    q, check_q = padded(rows, dim, I8, 55, extra=1)
+    s = torch.empty(rows, device="cuda")
+    streamed(rows, dim, x, q)
+    B.cs_i8_quantise(B.i8_rows_desc(x, q, s), x, q, s)
+    back, check_back = padded(rows, dim, xt, -77.0, extra=1)
+    B.cs_i8_dequantise(B.i8_rows_desc(back, q, s), q, s, back)
+    step = 4000
+    q1, s1, back1 = padded(step, dim, I8, 0)[0], torch.empty(step, device="cuda"), padded(step, dim, xt, 0.0)[0]
+    for first in range(0, rows, step):
+        p = slice(first, first + step)
+        B.cs_i8_quantise(B.i8_rows_desc(x[p], q1, s1), x[p], q1, s1)
+        assert same(q1, q[p]) and same(s1, s[p]), first
+        B.cs_i8_dequantise(B.i8_rows_desc(back1, q1, s1), q1, s1, back1)
+        assert same(back1, back[p]), first
+    check_q()
+    check_back()
+
+
+@pytest.mark.parametrize("xt,yt", [(BF, BF), (BF, FP), (FP, BF), (BF, I8), (FP, I8)])
+@pytest.mark.parametrize("dim", [1536, 2051, 5120])
+def test_norms_past_the_caches(dim, xt, yt):
+    """Forward, and backward with gradients of the forward's type."""
+    groups, rows = 4, 64 * (-(-100_000_000 // (dim * (torch.empty(0, dtype=xt).element_size() + torch.empty(0, dtype=yt).element_size())))
+                            // 64 + 1)
+    total = groups * rows
+    x, _ = padded(total, dim, xt, 0.0)
+    x.copy_(device_randn(1, total, dim, dtype=xt))
+    w, b = padded(groups, dim, FP, 0.0)[0], padded(groups, dim, FP, 0.0)[0]
+    w.copy_(device_randn(2, groups, dim))
+    b.copy_(device_randn(3, groups, dim))
+    y, check = padded(total, dim, yt, 55 if yt == I8 else -77.0, extra=1)
+    mean, rstd, s = (torch.empty(total, device="cuda") for _ in range(3))
+    streamed(total, dim, x, y)
+    B.cs_layer_norm(B.layer_norm_desc(x, y, w, b, groups=groups), x, y, w, b, y_scale=s, mean=mean, rstd=rstd)
+    t = None
+    if yt != I8:
+        streamed(total, dim, x, y, x)
+        t = run_grad(x, y, w, mean, rstd, groups, True)
+    for g in range(groups):
+        r, wg, bg = slice(g * rows, (g + 1) * rows), w[g:g + 1], b[g:g + 1]
+        one = padded(rows, dim, yt, 0)[0]
+        m, d, s1 = (torch.empty(rows, device="cuda") for _ in range(3))
+        B.cs_layer_norm(B.layer_norm_desc(x[r], one, wg, bg), x[r], one, wg, bg, y_scale=s1, mean=m, rstd=d)
+        assert same(one, y[r]) and same(m, mean[r]) and same(d, rstd[r]) and (yt != I8 or same(s1, s[r]))
+        if t is not None:
+            p = run_grad(x[r], y[r], wg, m, d, 1, True)
+            assert same(p["x"], t["x"][r]) and same(p["w"][0], t["w"][g]) and same(p["b"][0], t["b"][g])
+    check()
