@@ -553,21 +553,34 @@ struct PabIO {
 };
 
 // The inputs of a block's projections in 8 bits, into the workspace: a norm of the residual
-// stream (gain weight, or 1 + weight), or rows of the compute type.
+// stream (gain weight, or 1 + weight), or rows of the compute type.  In slices of ROWS_8BIT rows, which
+// one launch has at any width.
+constexpr long ROWS_8BIT = 1L << 21;
+
 static hipError_t norm_rows_8bit(const cs_model* m, const Workspace& w, long rows, const float* weight,
                                  const float* bias, bool unit_offset) {
-  LayerNormArgs a = {};
-  a.x = w.z;
-  a.weight = weight;
-  a.bias = bias;
-  a.y = w.u8;
-  a.y_scale = w.s8;
-  a.d = {CS_FP32, CS_I8, 1, (int32_t)rows, (int32_t)m->d, unit_offset, 1e-6f, m->d, m->d, 0, 0};
-  return layer_norm(a, m->stream);
+  hipError_t s = hipSuccess;
+  for (long r = 0; r < rows && s == hipSuccess; r += ROWS_8BIT) {
+    const int n = (int)std::min(ROWS_8BIT, rows - r);
+    LayerNormArgs a = {};
+    a.x = w.z + r * m->d;
+    a.weight = weight;
+    a.bias = bias;
+    a.y = w.u8 + r * m->d;
+    a.y_scale = w.s8 + r;
+    a.d = {CS_FP32, CS_I8, 1, n, (int32_t)m->d, unit_offset, 1e-6f, m->d, m->d, 0, 0};
+    s = layer_norm(a, m->stream);
+  }
+  return s;
 }
 
-static hipError_t rows_8bit(const cs_model* m, const Workspace& w, const void* x, long rows, int dim) {
-  return i8_quantise({x, nullptr, w.u8, w.s8, {CS_BF16, (int32_t)rows, dim, dim, dim}}, m->stream);
+static hipError_t rows_8bit(const cs_model* m, const Workspace& w, const bf16* x, long rows, int dim) {
+  hipError_t s = hipSuccess;
+  for (long r = 0; r < rows && s == hipSuccess; r += ROWS_8BIT) {
+    const int n = (int)std::min(ROWS_8BIT, rows - r);
+    s = i8_quantise({x + r * dim, nullptr, w.u8 + r * dim, w.s8 + r, {CS_BF16, n, dim, dim, dim}}, m->stream);
+  }
+  return s;
 }
 
 // One transformer evaluation for n_slots streams.  Stream s reads latent

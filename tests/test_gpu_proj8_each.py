@@ -124,3 +124,22 @@ def test_skip_schedules_are_those_of_the_compute_type(tau):
             same += 1
             assert rel_l2(eight.latents[s], native.latents[s]) < FAR
     print("streams with one schedule:", same, "computed", eight.computed, native.computed, flush=True)
+
+
+@pytest.mark.parametrize("proj", [B.CS_PROJ_NATIVE, B.CS_PROJ_8BIT])
+def test_more_tokens_than_a_launch_has_rows(proj):
+    """2^24 tokens with a feed-forward wider than 2048: a workgroup a row would pass a launch's 2^32 work items.  A
+    latent is bitwise what it is alone."""
+    m = dataclasses.replace(synth.MODELS["tiny"], n_blocks=1, hidden=64, heads=2, ffn=2112, lat_f=1, lat_h=128, lat_w=128,
+                            dtype=synth.DTYPE_BF16)
+    n = 4096
+    assert n * m.tokens == 1 << 24
+    x = torch.randn(n, m.latent_numel, generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    ctx = torch.from_numpy(synth.make_context(m, 35)).cuda()
+    gm = GpuModel(m, synth.make_weights(m, init="stress"), proj=proj)
+    v = gm.velocity(x, 0.5, ctx)
+    for i in (0, 2047, 2048, n - 1):
+        assert torch.equal(gm.velocity(x[i:i + 1], 0.5, ctx)[0], v[i]), i
+    gm.close()
+    del v
+    torch.cuda.empty_cache()
