@@ -452,9 +452,9 @@ typedef struct {
  * to 3.4e38 or more gives its bias.  weight, bias: fp32 [groups][dim], NULL for 1 and 0.  mean,
  * rstd: fp32 [groups * rows], written for the backward pass, or NULL.  y_scale: the rows' scales
  * where y_dtype is CS_I8 (else not read).  y may be x (same pointer, type and stride).  NaN: a row that is
- * not finite or whose values add up to 3.4e38 or more, and with eps 0 one without variance.  groups *
- * rows is below 2^30, and a call fits a launch of fewer than 2^32 work items (else CS_E_UNSUPPORTED): below
- * 2^24 rows, 2^26 up to 2048 channels. */
+ * not finite or whose values add up to 3.4e38 or more, a value that lies as far from its row's mean, and
+ * with eps 0 a row without variance.  groups * rows is below 2^30, and a call fits a launch of fewer than 2^32 work items (else CS_E_UNSUPPORTED): below
+ * 2^24 rows, 2^26 - 3 up to 2048 channels. */
 cs_status cs_layer_norm(const cs_layer_norm_desc* desc, const void* x, const float* weight, const float* bias, void* y,
                         float* y_scale, float* mean, float* rstd, void* stream);
 
@@ -487,7 +487,7 @@ cs_status cs_layer_norm_backward(const cs_layer_norm_grad_desc* desc, const void
  * (of the exact quotients, halfway ones to the even code), within -127..127; it stands for
  * code * scale.  A row of zeros, or whose scale underflows to 0, has scale 0 and codes 0; one that holds an
  * infinity or a NaN has scale NaN and codes 0.  cs_layer_norm writes the same of its results.  Rows are
- * below 2^24 (2^26 up to 2048 channels, to codes 2^22 beyond 16384; else CS_E_UNSUPPORTED). */
+ * below 2^24 (2^26 - 3 up to 2048 channels, to codes 2^22 beyond 16384; else CS_E_UNSUPPORTED). */
 typedef struct {
   int32_t dtype, rows, dim;
   int64_t x_row, q_row;

@@ -49,7 +49,8 @@ static constexpr TileCost TILE_COST[N_TILES] = {
 // measured shapes (1 to 65,520 rows; N and K of projections at widths 256 to 5120, and odd ones),
 // weights from HBM.  Against the best tile of each it costs 0.9% on average, 13% at most.  12,480 x
 // 1536 x 8960 takes 191 us with 256 x 256 tiles, 154 with 160 x 256; 1560 x 4608 x 1536 25.7 and
-// 18.5; 32,760 x 13,824 x 5120 1790 us with 256 x 256 (2.59 PFLOP/s) and 2124 with 128 x 128.
+// 18.5; 32,760 x 13,824 x 5120 1790 us with 256 x 256 and 2124 with 128 x 128, on one machine (others
+// take 1770 to 1890 with the former).
 // Residual updates are taken to add what they add in bf16.
 static constexpr TileCost TILE_COST_I8[N_TILES] = {
     {256, 256, 1, 0.912, 1.320, 5.06, 11.57, 16.20},

@@ -143,7 +143,8 @@ hipError_t layer_norm(const LayerNormArgs& a, hipStream_t st) {
 // TB/s) and 5.0.
 int ln_part_rows(int rows) {
   // About 512 parts of a long group, so that one alone fills the card, 16 rows at least: what is
-  // written and read of the sums, 16 bytes a channel and part, stays a tenth of the rows' bytes.  Rows
+  // written and read of the sums, 16 bytes a channel and part, is then a twelfth of the rows' bytes in fp32, a
+  // sixth in bf16, half as much again where dx is not wanted.  Rows
   // of the group alone decide, so that its gradients do not depend on other groups.  Up to 32 rows are
   // one part, whose sums are the gradient: the second launch costs more than 16 rows do.  256 rows at most:
   // a part's sums are fp32, so that more would lose digits (at 8 M rows, in parts of 16,384, 1024 half

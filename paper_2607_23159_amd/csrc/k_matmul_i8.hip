@@ -5,8 +5,8 @@
 // The kernels are those of the other types: a 16-byte chunk holds 16 codes where it holds 8 bf16, and
 // v_mfma_i32_16x16x64_i8 takes it in the cycles of v_mfma_f32_16x16x32_bf16, so a K slice of 128 bytes is
 // 128 deep and the loads, LDS reads and products of a slice stay as they are.  32,760 x 13,824 x
-// 5120: 1.80 ms, 2.58 P operations/s at 1.93 GHz with the matrix pipe busy 64% of the cycles (bf16:
-// 1.3 P); 12,480 x 1536 x 8960 142 us, 57% busy.
+// 5120 with the GELU: 1.77 to 1.89 ms (machines differ), 2.45 to 2.61 P operations/s at 1.93 GHz with the matrix pipe busy
+// 64% of the cycles (bf16: 1.3 P); 12,480 x 1536 x 8960 140 to 155 us, 57% busy.
 #include "gemm_kernel.hpp"
 #include "gemm_tile.hpp"
 #include "ops.hpp"
