@@ -13,7 +13,7 @@ from oracle import dit as odit
 from paper_2607_23159_amd import binding as B
 from paper_2607_23159_amd import synth
 from paper_2607_23159_amd.search import GpuModel, run_rollout
-from parity import rel_l2
+from parity import check_ranking, rel_l2
 from test_gpu_proj8 import FAR, PROJECTIONS, rounded, run
 
 
@@ -143,3 +143,22 @@ def test_more_tokens_than_a_launch_has_rows(proj):
     gm.close()
     del v
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("name,n_cand", [("tiny", 16), ("wan_mid", 8)])
+def test_rankings_are_those_of_the_compute_type(name, n_cand):
+    """A score is a random projection of the latent, over the root of its size: scores differ by a normal value of the
+    latents' difference in the mean square.  Five of its deviations are allowed, and swaps where the native gap is below
+    twice that."""
+    wl = synth.make_workload(name, init="paper", dtype=synth.DTYPE_BF16, n_cand=n_cand, mode=synth.CACHE_OFF)
+    runs = []
+    for proj in (B.CS_PROJ_8BIT, B.CS_PROJ_NATIVE):
+        gm = GpuModel(wl.model, wl.weights, proj=proj)
+        runs.append(run_rollout(gm, wl))
+        gm.close()
+    eight, native = runs
+    off = np.sqrt(((eight.latents.astype(np.float64) - native.latents) ** 2).reshape(n_cand, -1).mean(-1))
+    assert (np.abs(np.asarray(eight.scores) - native.scores) <= 5 * off).all()
+    check_ranking(eight.scores, native.scores, 10 * off.max())
+    print(name, "rho", B.cs_rank(eight.scores, native.scores)[2], "scores off", np.abs(np.asarray(eight.scores) - native.scores).max(),
+          "latents", rel_l2(eight.latents, native.latents), flush=True)
