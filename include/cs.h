@@ -453,8 +453,8 @@ typedef struct {
  * rstd: fp32 [groups * rows], written for the backward pass, or NULL.  y_scale: the rows' scales
  * where y_dtype is CS_I8 (else not read).  y may be x (same pointer, type and stride).  NaN: a row that is
  * not finite or whose values add up to 3.4e38 or more, a value that lies as far from its row's mean, and
- * with eps 0 a row without variance.  groups * rows is below 2^30, and a call fits a launch of fewer than 2^32 work items (else CS_E_UNSUPPORTED): below
- * 2^24 rows, 2^26 - 3 up to 2048 channels. */
+ * with eps 0 a row without variance.  groups * rows is below 2^30, and a call fits a launch of fewer
+ * than 2^32 work items: below 2^24 rows, 2^26 - 3 up to 2048 channels (else CS_E_UNSUPPORTED). */
 cs_status cs_layer_norm(const cs_layer_norm_desc* desc, const void* x, const float* weight, const float* bias, void* y,
                         float* y_scale, float* mean, float* rstd, void* stream);
 
